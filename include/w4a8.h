@@ -46,7 +46,9 @@ typedef enum {
     W4A8_ERR_UNSUPPORTED_ARCH = 5,  /* current device is not sm_100 */
     W4A8_ERR_CUDA = 6,              /* a CUDA runtime or driver call failed */
     W4A8_ERR_TIMEOUT = 7,           /* a bounded wait inside a kernel ran out */
-    W4A8_ERR_BAD_BLOB = 8           /* `packed` does not hold a blob of this N, K, group */
+    W4A8_ERR_BAD_BLOB = 8,          /* `packed` does not hold a blob of this N, K, group */
+    W4A8_ERR_BAD_TABLE = 9          /* a page number, sequence length or row offset that a kernel
+                                       met lies outside the cache, the page table or the call */
 } w4a8_status;
 
 /* Which kernel w4a8_linear_ex runs.  AUTO picks by shape. */
@@ -186,6 +188,28 @@ typedef enum { W4A8_NORM_RMS = 0, W4A8_NORM_LAYER = 1 } w4a8_norm;
 w4a8_status w4a8_norm_quantize_act(const void *X_f16, const float *norm_weight,
                                    const float *norm_bias, int norm_kind, float eps, int M, int K,
                                    int8_t *Xq, float *tok_scale, void *stream);
+
+/* 16- and 32-bit floating types of the calls below. */
+typedef enum { W4A8_F16 = 0, W4A8_BF16 = 1, W4A8_F32 = 2 } w4a8_dtype;
+
+/* w4a8_norm_quantize_act with the residual addition in front of it: what stands between two
+ * sub-blocks of a decoder layer (the output of one's last linear joins the residual stream, the
+ * normalised stream is the next one's INT8 input), in one pass.
+ *   X              [M][K] W4A8_F16 or W4A8_BF16 (x_type), the branch (e.g. w4a8_linear's output).
+ *   residual       [M][K] W4A8_F16, W4A8_BF16 or W4A8_F32 (res_type), the stream.
+ *   residual_out   [M][K] res_type: residual + X, added in binary32 and rounded once to res_type.
+ *                  May be `residual` itself (in place); any other overlap is not allowed.
+ *   norm_weight, norm_bias, norm_kind, eps, K <= 16384, Xq, tok_scale   as in
+ *                  w4a8_norm_quantize_act, applied to the values stored in residual_out.
+ * Precision: mean, variance (of the binary32 differences from the rounded mean) and reciprocal
+ * root in binary64 from the elements on, mean and root rounded once to binary32; everything per
+ * element in binary32, one rounding per operation.  (w4a8_norm_quantize_act takes sums inside
+ * runs of eight features in binary32, so its root can differ from this call's by one binary32
+ * step.) */
+w4a8_status w4a8_add_norm_quantize_act(const void *X, int x_type, const void *residual, int res_type,
+                                       void *residual_out, const float *norm_weight,
+                                       const float *norm_bias, int norm_kind, float eps, int M,
+                                       int K, int8_t *Xq, float *tok_scale, void *stream);
 
 /* Scratch bytes w4a8_linear needs for this shape (always >= 256: the first 256 bytes
  * hold the status block read by w4a8_poll_status).  The caller zero-fills the workspace
@@ -366,6 +390,88 @@ w4a8_status w4a8_attn_pv(const int8_t *Pq, const float *p_scale, const void *pac
                          int H, int D, void *O_bf16, void *workspace, size_t workspace_bytes,
                          void *stream);
 
+/* ---- a paged key / value cache in dINT4, written token by token, and attention over it ----
+ * Where w4a8_pack_value quantizes the values of a whole sequence per channel, a cache that grows
+ * by a token at a time has only the token to take a range from: here every key and value vector
+ * (one token, one head, D elements) is quantized by itself with the dINT4 quantizer of Eq. 5,
+ *   lo = min(0, min x), hi = max(0, max x), step = (hi/2 - lo/2) / 6.5 rounded to 20 significant
+ *   bits (1 when the quotient is below 2^-100: such a vector is stored as zeros), r = 1 / step,
+ *   z = clamp(rint(-lo * r), 0, 13), and per element u = x * r: +-1/2 when 1/4 < |u| <= 3/4, else
+ *   clamp(rint(u) + z, 0, 13) - z; the stored value is that level times step
+ * (binary32, one rounding per operation, round half to even).
+ *
+ * The cache is caller-owned memory of num_pages pages; a page holds page_size token slots (16, 32,
+ * 64, ... up to 1024, a power of two) for kv_heads heads of dimension D = 64 or 128, and takes
+ * w4a8_kv_page_bytes(page_size, kv_heads, D) bytes = kv_heads * page_size * (D + 8).  It needs no
+ * initialisation, and pages can be copied byte for byte.  Layout: [head][page_size / 16] blocks of
+ * 16 tokens; a block = key codes [16][D/2], value codes [2][8][8][D/16] (half of the block, slice of
+ * D/8 elements, token of the half, bytes), 16 key words, 16 value words.  A word is the binary32
+ * step with its last four mantissa bits replaced by z.  A code is the level's rank 0..15 among
+ * -z .. 13-z, +-1/2 in ascending order; the ranks r0..r3 of four consecutive elements form the 16-bit
+ * number r0 + 16 r1 + 256 r2 + 4096 r3, stored rotated left by two bits.
+ *
+ * Batch arguments shared by the three calls:
+ *   page_table  [batch][max_pages] INT32: page of tokens i * page_size .. of each sequence.  Entries
+ *               that no visited token needs are not read.
+ *   kv_lens     [batch] INT32, tokens of each sequence INCLUDING this call's rows.
+ *   cu_rows     [batch + 1] INT32, ascending from 0: rows cu_rows[b] .. cu_rows[b+1] - 1 of the call
+ *               belong to sequence b and are its last positions, kv_lens[b] - n_b + i.  NULL: one
+ *               row per sequence (rows = batch).  Rows from cu_rows[batch] on (padding) are
+ *               neither read nor written.  A row whose position would be negative is ignored by
+ *               append, read back as zeros and attends to nothing.
+ *   rows        rows of the call (the first dimension of K, V, Q and the outputs).
+ *   *_stride    distance of two rows in elements (a multiple of 8; at least heads * D), so that K,
+ *               V and Q may be slices of one wider projection output.
+ *   workspace   zero-filled once (w4a8_workspace_init); a page number outside [0, num_pages), a
+ *               position beyond max_pages pages, a negative length or row offsets outside the call
+ *               are reported through its status block (W4A8_ERR_BAD_TABLE); what such a row
+ *               produces is undefined, but no access leaves the buffers.  append and read need
+ *               its first 256 bytes only, so the three calls can share one.  Calls that may
+ *               overlap on the device, two captured graphs among them, need separate
+ *               workspaces.
+ * Two rows of one append must not name the same slot (two sequences that share their last
+ * page). */
+size_t w4a8_kv_page_bytes(int page_size, int kv_heads, int head_dim);
+
+/* Quantizes the rows' keys and values into their slots.  K, V: [rows][kv_heads][D] W4A8_F16 or
+ * W4A8_BF16. */
+w4a8_status w4a8_kv_append(const void *K, const void *V, int dtype, long long k_stride,
+                           long long v_stride, void *cache, int num_pages, int page_size,
+                           int kv_heads, int head_dim, const int32_t *page_table, int max_pages,
+                           const int32_t *kv_lens, const int32_t *cu_rows, int batch, int rows,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* Reads the rows' keys and values back, level * step in binary32 rounded once to dtype (W4A8_F16 or
+ * W4A8_BF16; values beyond its range become the largest finite ones).
+ * K_out, V_out: [rows][kv_heads][D], contiguous. */
+w4a8_status w4a8_kv_read(const void *cache, int num_pages, int page_size, int kv_heads, int head_dim,
+                         const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                         const int32_t *cu_rows, int batch, int rows, void *K_out, void *V_out,
+                         int dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Attention of the rows' queries over the cached keys and values of their sequences, without
+ * expanding the cache in memory:  o = sum_j p_j v_j,  p = softmax_j(scale * q . k_j).
+ *   Q          [rows][q_heads][D] W4A8_F16 or W4A8_BF16 (q_type); q_heads a multiple of kv_heads,
+ *              query head h reads key head h / (q_heads / kv_heads).
+ *   scale      > 0 (1 / sqrt(D) as a rule).
+ *   causal     non-zero: a row sees positions up to its own; zero: the whole sequence.
+ *   window     > 0: a row sees only positions above its own minus window; 0: no limit.
+ *   O          out [rows][q_heads][D] W4A8_F16 (what w4a8_quantize_act takes next) or W4A8_BF16
+ *              (o_type).  A row that sees no key gets zeros.
+ *   lse        out [rows][q_heads] FP32, natural logarithm of the softmax's denominator
+ *              (-inf for a row that sees no key), or NULL.
+ * Precision: scores, maxima and sums in binary32; the weights p enter the value product in
+ * binary16.  The result does not depend on how the work was scheduled.
+ *   workspace >= w4a8_kv_attention_workspace_bytes(rows, batch, q_heads, kv_heads, D). */
+size_t w4a8_kv_attention_workspace_bytes(int rows, int batch, int q_heads, int kv_heads,
+                                         int head_dim);
+w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, const void *cache,
+                              int num_pages, int page_size, int kv_heads, int head_dim,
+                              const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                              const int32_t *cu_rows, int batch, int rows, int q_heads, float scale,
+                              int causal, int window, void *O, int o_type, float *lse,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
 /* w4a8_linear_asym for any group_size: with group_size 128 the token's zero-point leaves every
  * group's integer sum before that sum is scaled,
  *   acc_g[m][n] = sum_{k in g} Xq[m][k] * t2(code[n][k]) - tok_zero[m] * rowsum[g][n],
@@ -396,7 +502,8 @@ w4a8_status w4a8_unpack_codes_bits(const void *packed, int N, int K, int group_s
                                    uint8_t *codes, float *scales, uint8_t *zeros, void *stream);
 
 /* Synchronizes `stream`, then reads and clears the status block of `workspace`:
- * W4A8_OK, W4A8_ERR_TIMEOUT or W4A8_ERR_BAD_BLOB (first failure since the last poll).
+ * W4A8_OK, W4A8_ERR_TIMEOUT, W4A8_ERR_BAD_BLOB or W4A8_ERR_BAD_TABLE (first failure since the
+ * last poll).
  * A kernel that gave up (W4A8_ERR_TIMEOUT) may leave split-K tile counters behind in the
  * workspace: run w4a8_workspace_init on it before the next call, else a later split-K call can
  * reduce partial tiles too early.  The output of a call that reported a failure is undefined. */

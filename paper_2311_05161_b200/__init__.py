@@ -14,4 +14,6 @@ from .binding import (  # noqa: F401
     norm_quantize_act, NORM_RMS, NORM_LAYER, dint_table,
     pack_value, attn_pv, new_attn_pv_workspace,
     interleave_gate_up, linear_swiglu, new_linear_swiglu_workspace, linear_asym_group,
+    add_norm_quantize_act, new_kv_cache, kv_page_bytes, new_kv_workspace, kv_attention_workspace_bytes,
+    kv_append, kv_read, kv_attention,
 )

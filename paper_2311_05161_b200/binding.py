@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libw4a8.so")
 STATUS_NAMES = {
     0: "W4A8_OK", 1: "W4A8_ERR_NULL", 2: "W4A8_ERR_SHAPE", 3: "W4A8_ERR_ALIGN",
     4: "W4A8_ERR_BUFFER_TOO_SMALL", 5: "W4A8_ERR_UNSUPPORTED_ARCH", 6: "W4A8_ERR_CUDA",
-    7: "W4A8_ERR_TIMEOUT", 8: "W4A8_ERR_BAD_BLOB",
+    7: "W4A8_ERR_TIMEOUT", 8: "W4A8_ERR_BAD_BLOB", 9: "W4A8_ERR_BAD_TABLE",
 }
 PATH_AUTO, PATH_SIMPLE, PATH_TCGEN05, PATH_GEMV = 0, 1, 2, 3
 
@@ -34,6 +34,8 @@ EXPORTS = (
     "w4a8_packed_bytes_bits", "w4a8_pack_weights_bits", "w4a8_unpack_codes_bits", "w4a8_dint_table_bits",
     "w4a8_pack_value", "w4a8_attn_pv", "w4a8_attn_pv_workspace_bytes",
     "w4a8_linear_swiglu", "w4a8_linear_swiglu_workspace_bytes", "w4a8_linear_asym_group",
+    "w4a8_add_norm_quantize_act", "w4a8_kv_page_bytes", "w4a8_kv_append", "w4a8_kv_read",
+    "w4a8_kv_attention", "w4a8_kv_attention_workspace_bytes",
 )
 
 
@@ -115,6 +117,20 @@ def _load() -> ctypes.CDLL:
     lib.w4a8_linear_asym.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, vp, vp, vp, sz, vp, op]
     lib.w4a8_linear_asym_group.restype = ci
     lib.w4a8_linear_asym_group.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, sz, vp, op]
+    ll = ctypes.c_longlong
+    lib.w4a8_add_norm_quantize_act.restype = ci
+    lib.w4a8_add_norm_quantize_act.argtypes = [vp, ci, vp, ci, vp, vp, vp, ci, cf, ci, ci, vp, vp, vp]
+    lib.w4a8_kv_page_bytes.restype = sz
+    lib.w4a8_kv_page_bytes.argtypes = [ci, ci, ci]
+    lib.w4a8_kv_append.restype = ci
+    lib.w4a8_kv_append.argtypes = [vp, vp, ci, ll, ll, vp, ci, ci, ci, ci, vp, ci, vp, vp, ci, ci, vp, sz, vp]
+    lib.w4a8_kv_read.restype = ci
+    lib.w4a8_kv_read.argtypes = [vp, ci, ci, ci, ci, vp, ci, vp, vp, ci, ci, vp, vp, ci, vp, sz, vp]
+    lib.w4a8_kv_attention_workspace_bytes.restype = sz
+    lib.w4a8_kv_attention_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+    lib.w4a8_kv_attention.restype = ci
+    lib.w4a8_kv_attention.argtypes = [vp, ci, ll, vp, ci, ci, ci, ci, vp, ci, vp, vp, ci, ci, ci, cf, ci, ci,
+                                      vp, ci, vp, vp, sz, vp]
     lib.w4a8_linear_acc_i32.restype = ci
     lib.w4a8_linear_acc_i32.argtypes = [vp, vp, ci, ci, ci, ci, vp, vp, sz, vp, op]
     lib.w4a8_unpack_codes.restype = ci
@@ -235,6 +251,61 @@ def norm_quantize_act(X, norm_weight, norm_bias=None, kind: int = NORM_RMS, eps:
     _check(lib.w4a8_norm_quantize_act(_ptr(X), _ptr(norm_weight), _ptr(norm_bias), kind, eps, M, K,
                                       _ptr(Xq), _ptr(tok), _stream()), "w4a8_norm_quantize_act")
     return Xq, tok
+
+
+_DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+
+
+def _here(what, first, *others):
+    """The tensors live on the current device: the library launches on that device's stream."""
+    at = first.device
+    if at.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: tensors on {at}, current device is cuda:{torch.cuda.current_device()}")
+    for t in others:
+        if t is not None and t.device != at:
+            raise ValueError(f"{what}: tensors on {at} and {t.device}")
+
+
+def _is(t, shape, what):
+    if t is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{what}: expected shape {shape}, got {tuple(t.shape)}")
+    return t
+
+
+def _dev16(t, what, contiguous=True):
+    if not t.is_cuda or t.dtype not in (torch.float16, torch.bfloat16) or (contiguous and not t.is_contiguous()):
+        raise TypeError(f"{what}: expected a CUDA tensor of float16 or bfloat16{', contiguous' if contiguous else ''}")
+    return t
+
+
+def add_norm_quantize_act(X, residual, norm_weight, norm_bias=None, kind: int = NORM_RMS, eps: float = 1e-5,
+                          residual_out=None, out=None):
+    """residual + X, then RMSNorm / LayerNorm and the token-wise INT8 quantizer of the sum, in one pass:
+    X [M, K] float16 / bfloat16, residual [M, K] float16 / bfloat16 / float32 ->
+    (Xq [M, K] int8, tok_scale [M] float32, residual_out [M, K] of residual's type).  In place with
+    `residual_out=residual`."""
+    X = _dev16(X, "X")
+    if residual.dtype not in _DTYPES:
+        raise TypeError("residual: expected float16, bfloat16 or float32")
+    residual = _dev(residual, residual.dtype, "residual")
+    norm_weight = _dev(norm_weight, torch.float32, "norm_weight")
+    norm_bias = _dev(norm_bias, torch.float32, "norm_bias")
+    M, K = X.shape
+    _is(residual, (M, K), "residual")
+    _is(norm_weight, (K,), "norm_weight")
+    _is(norm_bias, (K,), "norm_bias")
+    residual_out = torch.empty_like(residual) if residual_out is None else _is(
+        _dev(residual_out, residual.dtype, "residual_out"), (M, K), "residual_out")
+    if out is None:
+        out = (torch.empty((M, K), dtype=torch.int8, device=X.device),
+               torch.empty((M,), dtype=torch.float32, device=X.device))
+    Xq, tok = _is(_dev(out[0], torch.int8, "Xq"), (M, K), "Xq"), _is(_dev(out[1], torch.float32, "tok_scale"), (M,), "tok_scale")
+    _here("add_norm_quantize_act", X, residual, norm_weight, norm_bias, residual_out, Xq, tok)
+    _check(lib.w4a8_add_norm_quantize_act(
+        X.data_ptr(), _DTYPES[X.dtype], residual.data_ptr(), _DTYPES[residual.dtype], residual_out.data_ptr(),
+        norm_weight.data_ptr(), _ptr(norm_bias), kind, eps, M, K, Xq.data_ptr(), tok.data_ptr(), _stream()),
+        "w4a8_add_norm_quantize_act")
+    return Xq, tok, residual_out
 
 
 def linear_workspace_bytes(M: int, N: int, K: int, group: int = 0, opts: Opts | None = None) -> int:
@@ -443,6 +514,111 @@ def attn_pv(Pq, p_scale, packed, D: int, workspace, out=None):
         out = torch.empty((T, H, D), dtype=torch.bfloat16, device=Pq.device)
     _check(lib.w4a8_attn_pv(_ptr(Pq), _ptr(p_scale), _ptr(packed), T, S, H, D, _ptr(out),
                             _ptr(workspace), workspace.numel(), _stream()), "w4a8_attn_pv")
+    return out
+
+
+def kv_page_bytes(page_size: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib.w4a8_kv_page_bytes(page_size, kv_heads, head_dim))
+
+
+def new_kv_cache(num_pages: int, page_size: int, kv_heads: int, head_dim: int, device="cuda"):
+    """A paged dINT4 key / value cache: uint8 [num_pages, page_bytes], not initialised."""
+    nbytes = kv_page_bytes(page_size, kv_heads, head_dim)
+    if nbytes == 0:
+        raise W4A8Error(2, "w4a8_kv_page_bytes")
+    return torch.empty((num_pages, nbytes), dtype=torch.uint8, device=device)
+
+
+def kv_attention_workspace_bytes(rows: int, batch: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib.w4a8_kv_attention_workspace_bytes(rows, batch, q_heads, kv_heads, head_dim))
+
+
+def new_kv_workspace(rows: int, batch: int, q_heads: int, kv_heads: int, head_dim: int, device="cuda"):
+    """Workspace of the three cache calls for up to `rows` rows of `batch` sequences."""
+    nbytes = kv_attention_workspace_bytes(rows, batch, q_heads, kv_heads, head_dim)
+    if nbytes == 0:
+        raise W4A8Error(2, "w4a8_kv_attention_workspace_bytes")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    workspace_init(ws)
+    return ws
+
+
+def _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, head_dim, rows, workspace, what, *tensors):
+    """Checks of the arguments that the cache calls share: (num_pages, page_size, max_pages, batch)."""
+    _dev(cache, torch.uint8, "cache")
+    _dev(page_table, torch.int32, "page_table")
+    _dev(kv_lens, torch.int32, "kv_lens")
+    _dev(cu_rows, torch.int32, "cu_rows")
+    _dev(workspace, torch.uint8, "workspace")
+    batch, max_pages = page_table.shape
+    _is(kv_lens, (batch,), "kv_lens")
+    _is(cu_rows, (batch + 1,), "cu_rows")
+    num_pages, nbytes = cache.shape
+    page_size = nbytes // (kv_heads * (head_dim + 8)) if kv_heads > 0 else 0
+    if nbytes != kv_page_bytes(page_size, kv_heads, head_dim):
+        raise ValueError(f"{what}: pages of {nbytes} bytes do not hold {kv_heads} heads of {head_dim}")
+    _here(what, cache, page_table, kv_lens, cu_rows, workspace, *tensors)
+    return num_pages, page_size, max_pages, batch
+
+
+def _rows_of(t, what):
+    """[rows, heads, D] whose rows may be slices of wider ones: the row stride in elements."""
+    _dev16(t, what, contiguous=False)
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise TypeError(f"{what}: expected [rows, heads, D] with contiguous heads")
+    # torch leaves the stride of a dimension of one row without meaning
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def kv_append(K, V, cache, page_table, kv_lens, workspace, cu_rows=None):
+    """Quantizes the rows' keys and values (K, V [rows, kv_heads, D] float16 / bfloat16; rows may be strided)
+    into the cache.  Rows cu_rows[b] .. cu_rows[b + 1] - 1 are the last positions of sequence b, whose
+    length kv_lens[b] counts them already; without cu_rows, one row per sequence."""
+    ks, vs = _rows_of(K, "K"), _rows_of(V, "V")
+    rows, kv_heads, D = K.shape
+    if V.dtype != K.dtype:
+        raise TypeError("V: expected the type of K")
+    _is(V, (rows, kv_heads, D), "V")
+    n, P, mp, batch = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, D, rows, workspace, "kv_append", K, V)
+    _check(lib.w4a8_kv_append(K.data_ptr(), V.data_ptr(), _DTYPES[K.dtype], ks, vs, cache.data_ptr(), n, P,
+                              kv_heads, D, page_table.data_ptr(), mp, kv_lens.data_ptr(), _ptr(cu_rows), batch,
+                              rows, workspace.data_ptr(), workspace.numel(), _stream()), "w4a8_kv_append")
+
+
+def kv_read(cache, page_table, kv_lens, rows: int, kv_heads: int, head_dim: int, workspace, cu_rows=None,
+            dtype=torch.float16, out=None):
+    """Reads the keys and values of `rows` rows (numbered as in kv_append) back:
+    (K, V) [rows, kv_heads, D] of `dtype`."""
+    if out is None:
+        out = (torch.empty((rows, kv_heads, head_dim), dtype=dtype, device=cache.device),
+               torch.empty((rows, kv_heads, head_dim), dtype=dtype, device=cache.device))
+    K, V = (_is(_dev16(t, "out"), (rows, kv_heads, head_dim), "out") for t in out)
+    if K.dtype != V.dtype:
+        raise TypeError("out: expected two tensors of one type")
+    n, P, mp, batch = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, head_dim, rows, workspace, "kv_read", K, V)
+    _check(lib.w4a8_kv_read(cache.data_ptr(), n, P, kv_heads, head_dim, page_table.data_ptr(), mp,
+                            kv_lens.data_ptr(), _ptr(cu_rows), batch, rows, K.data_ptr(), V.data_ptr(),
+                            _DTYPES[K.dtype], workspace.data_ptr(), workspace.numel(), _stream()), "w4a8_kv_read")
+    return K, V
+
+
+def kv_attention(Q, cache, page_table, kv_lens, kv_heads: int, workspace, cu_rows=None, scale=None,
+                 causal: bool = True, window: int = 0, dtype=torch.float16, out=None, lse=None):
+    """Attention of Q [rows, q_heads, D] (float16 / bfloat16; rows may be strided) over the cache:
+    O [rows, q_heads, D] of `dtype`.  scale: 1 / sqrt(D) by default; lse: a [rows, q_heads] float32
+    tensor that receives the logarithms of the softmax denominators."""
+    qs = _rows_of(Q, "Q")
+    rows, q_heads, D = Q.shape
+    if out is None:
+        out = torch.empty((rows, q_heads, D), dtype=dtype, device=Q.device)
+    _is(_dev16(out, "out"), (rows, q_heads, D), "out")
+    _is(_dev(lse, torch.float32, "lse"), (rows, q_heads), "lse")
+    n, P, mp, batch = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, D, rows, workspace, "kv_attention", Q, out, lse)
+    _check(lib.w4a8_kv_attention(
+        Q.data_ptr(), _DTYPES[Q.dtype], qs, cache.data_ptr(), n, P, kv_heads, D, page_table.data_ptr(), mp,
+        kv_lens.data_ptr(), _ptr(cu_rows), batch, rows, q_heads, D ** -0.5 if scale is None else scale,
+        int(causal), window, out.data_ptr(), _DTYPES[out.dtype], _ptr(lse), workspace.data_ptr(),
+        workspace.numel(), _stream()), "w4a8_kv_attention")
     return out
 
 

@@ -1,5 +1,6 @@
 // extern "C" entry points: argument validation and dispatch.  See include/w4a8.h.
 #include "common.cuh"
+#include "kv_cache.cuh"
 
 using namespace w4a8;
 
@@ -131,6 +132,46 @@ w4a8_status linear_common(const int8_t *Xq, const float *tok_scale, const void *
                                  acc, static_cast<uint8_t *>(workspace), plan, st, zp);
 }
 
+inline bool is_16bit(int type) { return type == W4A8_F16 || type == W4A8_BF16; }
+
+bool kv_shape_ok(int page_size, int heads, int D)
+{
+    return (D == 64 || D == 128) && heads >= 1 && heads <= 4096 && page_size >= 16 && page_size <= 1024 &&
+           (page_size & (page_size - 1)) == 0;
+}
+
+// What the three cache calls check alike; the cache and batch descriptions when all is well.
+w4a8_status kv_common(const void *cache, int num_pages, int page_size, int heads, int D,
+                      const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                      const int32_t *cu_rows, int batch, int rows, void *workspace,
+                      size_t workspace_bytes, KvCache *c, KvBatch *bt)
+{
+    if (!cache || !page_table || !kv_lens || !workspace) return W4A8_ERR_NULL;
+    if (!kv_shape_ok(page_size, heads, D) || num_pages < 1 || max_pages < 1 || batch < 1 || rows < 1)
+        return W4A8_ERR_SHAPE;
+    // positions are 32-bit; one launch's rows x heads stay within a grid
+    if ((long long)max_pages * page_size >= (1ll << 31) || (long long)rows * heads >= (1ll << 31))
+        return W4A8_ERR_SHAPE;
+    if (!cu_rows && rows != batch) return W4A8_ERR_SHAPE;
+    if (!aligned(cache, 16) || !aligned(page_table, 4) || !aligned(kv_lens, 4) || !aligned(cu_rows, 4) ||
+        !aligned(workspace, 256))
+        return W4A8_ERR_ALIGN;
+    if (workspace_bytes < sizeof(StatusBlock)) return W4A8_ERR_BUFFER_TOO_SMALL;
+    c->pages = static_cast<uint8_t *>(const_cast<void *>(cache));
+    c->num_pages = num_pages;
+    c->page_shift = 0;
+    while ((1 << c->page_shift) < page_size) ++c->page_shift;
+    c->heads = heads;
+    c->D = D;
+    bt->page_table = page_table;
+    bt->kv_lens = kv_lens;
+    bt->cu_rows = cu_rows;
+    bt->max_pages = max_pages;
+    bt->batch = batch;
+    bt->rows = rows;
+    return W4A8_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -212,6 +253,27 @@ w4a8_status w4a8_norm_quantize_act(const void *X_f16, const float *norm_weight,
     const cudaError_t e = launch_norm_quantize_act(
         static_cast<const __half *>(X_f16), norm_weight, norm_bias, norm_kind == W4A8_NORM_LAYER, eps,
         M, K, Xq, tok_scale, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
+}
+
+w4a8_status w4a8_add_norm_quantize_act(const void *X, int x_type, const void *residual, int res_type,
+                                       void *residual_out, const float *norm_weight,
+                                       const float *norm_bias, int norm_kind, float eps, int M,
+                                       int K, int8_t *Xq, float *tok_scale, void *stream)
+{
+    if (!X || !residual || !residual_out || !norm_weight || !Xq || !tok_scale) return W4A8_ERR_NULL;
+    if (M < 1 || K < 128 || K % 128 != 0 || K > 16384) return W4A8_ERR_SHAPE;
+    if (norm_kind != W4A8_NORM_RMS && norm_kind != W4A8_NORM_LAYER) return W4A8_ERR_SHAPE;
+    if (!is_16bit(x_type) || (!is_16bit(res_type) && res_type != W4A8_F32)) return W4A8_ERR_SHAPE;
+    if (!(eps > 0.0f)) return W4A8_ERR_SHAPE;
+    if (!aligned(X, 16) || !aligned(residual, 16) || !aligned(residual_out, 16) || !aligned(norm_weight, 16) ||
+        !aligned(norm_bias, 16) || !aligned(Xq, 16) || !aligned(tok_scale, 4))
+        return W4A8_ERR_ALIGN;
+    const w4a8_status arch = check_arch();
+    if (arch != W4A8_OK) return arch;
+    const cudaError_t e = launch_add_norm_quantize_act(
+        X, x_type, residual, res_type, residual_out, norm_weight, norm_bias, norm_kind == W4A8_NORM_LAYER,
+        eps, M, K, Xq, tok_scale, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
 }
 
@@ -437,6 +499,107 @@ w4a8_status w4a8_attn_pv(const int8_t *Pq, const float *p_scale, const void *pac
                                  static_cast<cudaStream_t>(stream));
 }
 
+// ---- paged dINT4 key / value cache ----
+size_t w4a8_kv_page_bytes(int page_size, int kv_heads, int head_dim)
+{
+    if (!kv_shape_ok(page_size, kv_heads, head_dim)) return 0;
+    return (size_t)kv_heads * page_size * (head_dim + 8);
+}
+
+w4a8_status w4a8_kv_append(const void *K, const void *V, int dtype, long long k_stride,
+                           long long v_stride, void *cache, int num_pages, int page_size,
+                           int kv_heads, int head_dim, const int32_t *page_table, int max_pages,
+                           const int32_t *kv_lens, const int32_t *cu_rows, int batch, int rows,
+                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!K || !V) return W4A8_ERR_NULL;
+    KvCache c;
+    KvBatch bt;
+    const w4a8_status s = kv_common(cache, num_pages, page_size, kv_heads, head_dim, page_table, max_pages,
+                                    kv_lens, cu_rows, batch, rows, workspace, workspace_bytes, &c, &bt);
+    if (s != W4A8_OK) return s;
+    const long long least = (long long)kv_heads * head_dim;
+    if (!is_16bit(dtype) || k_stride < least || v_stride < least || k_stride % 8 != 0 || v_stride % 8 != 0)
+        return W4A8_ERR_SHAPE;
+    if (!aligned(K, 16) || !aligned(V, 16)) return W4A8_ERR_ALIGN;
+    const w4a8_status arch = check_arch();
+    if (arch != W4A8_OK) return arch;
+    const cudaError_t e = launch_kv_append(K, V, dtype == W4A8_BF16, k_stride, v_stride, c, bt,
+                                           static_cast<StatusBlock *>(workspace),
+                                           static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
+}
+
+w4a8_status w4a8_kv_read(const void *cache, int num_pages, int page_size, int kv_heads, int head_dim,
+                         const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                         const int32_t *cu_rows, int batch, int rows, void *K_out, void *V_out,
+                         int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!K_out || !V_out) return W4A8_ERR_NULL;
+    KvCache c;
+    KvBatch bt;
+    const w4a8_status s = kv_common(cache, num_pages, page_size, kv_heads, head_dim, page_table, max_pages,
+                                    kv_lens, cu_rows, batch, rows, workspace, workspace_bytes, &c, &bt);
+    if (s != W4A8_OK) return s;
+    if (!is_16bit(dtype)) return W4A8_ERR_SHAPE;
+    if (!aligned(K_out, 16) || !aligned(V_out, 16)) return W4A8_ERR_ALIGN;
+    const w4a8_status arch = check_arch();
+    if (arch != W4A8_OK) return arch;
+    const cudaError_t e = launch_kv_read(c, bt, K_out, V_out, dtype == W4A8_BF16,
+                                         static_cast<StatusBlock *>(workspace),
+                                         static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
+}
+
+static bool kv_attention_shape_ok(int rows, int batch, int q_heads, int kv_heads, int head_dim)
+{
+    return kv_shape_ok(16, kv_heads, head_dim) && rows >= 1 && batch >= 1 && q_heads >= kv_heads &&
+           q_heads <= 65535 && q_heads % kv_heads == 0 && (long long)rows * q_heads < (1ll << 31);
+}
+
+size_t w4a8_kv_attention_workspace_bytes(int rows, int batch, int q_heads, int kv_heads, int head_dim)
+{
+    if (!kv_attention_shape_ok(rows, batch, q_heads, kv_heads, head_dim)) return 0;
+    return kv_attention_workspace(rows, batch, q_heads, kv_heads, head_dim);
+}
+
+w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, const void *cache,
+                              int num_pages, int page_size, int kv_heads, int head_dim,
+                              const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                              const int32_t *cu_rows, int batch, int rows, int q_heads, float scale,
+                              int causal, int window, void *O, int o_type, float *lse,
+                              void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!Q || !O) return W4A8_ERR_NULL;
+    KvAttnArgs a;
+    const w4a8_status s =
+        kv_common(cache, num_pages, page_size, kv_heads, head_dim, page_table, max_pages, kv_lens, cu_rows,
+                  batch, rows, workspace, workspace_bytes, &a.cache, &a.batch);
+    if (s != W4A8_OK) return s;
+    if (!kv_attention_shape_ok(rows, batch, q_heads, kv_heads, head_dim)) return W4A8_ERR_SHAPE;
+    if (!is_16bit(q_type) || !is_16bit(o_type) || q_stride < (long long)q_heads * head_dim || q_stride % 8 != 0)
+        return W4A8_ERR_SHAPE;
+    if (!(scale > 0.0f) || scale > 3.0e38f || window < 0) return W4A8_ERR_SHAPE;
+    if (!aligned(Q, 16) || !aligned(O, 16) || !aligned(lse, 4)) return W4A8_ERR_ALIGN;
+    if (workspace_bytes < kv_attention_workspace(rows, batch, q_heads, kv_heads, head_dim))
+        return W4A8_ERR_BUFFER_TOO_SMALL;
+    const w4a8_status arch = check_arch();
+    if (arch != W4A8_OK) return arch;
+    a.Q = Q;
+    a.q_bf16 = q_type == W4A8_BF16;
+    a.q_stride = q_stride;
+    a.q_heads = q_heads;
+    a.scale = scale;
+    a.causal = causal != 0;
+    a.window = window;
+    a.O = O;
+    a.o_bf16 = o_type == W4A8_BF16;
+    a.lse = lse;
+    const cudaError_t e = launch_kv_attention(a, static_cast<uint8_t *>(workspace),
+                                              static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
+}
+
 w4a8_status w4a8_linear_acc_i32(const int8_t *Xq, const void *packed, int M, int N, int K,
                                 int group_size, int32_t *acc, void *workspace,
                                 size_t workspace_bytes, void *stream, const w4a8_opts *opts)
@@ -535,7 +698,8 @@ w4a8_status w4a8_poll_status(void *workspace, void *stream)
         return W4A8_ERR_CUDA;
     if (host[0] == 0) return W4A8_OK;
     if (cudaMemset(workspace, 0, sizeof(StatusBlock)) != cudaSuccess) return W4A8_ERR_CUDA;
-    return host[0] == W4A8_ERR_BAD_BLOB ? W4A8_ERR_BAD_BLOB : W4A8_ERR_TIMEOUT;
+    if (host[0] == W4A8_ERR_BAD_BLOB) return W4A8_ERR_BAD_BLOB;
+    return host[0] == W4A8_ERR_BAD_TABLE ? W4A8_ERR_BAD_TABLE : W4A8_ERR_TIMEOUT;
 }
 
 void w4a8_dint4_table(int z, int8_t *out) { w4a8_dint4_table_fmt(z, 1, out); }

@@ -123,7 +123,7 @@ __host__ __device__ inline size_t code3_word_offset(const BlobLayout &L, int n, 
 // status block (first 256 bytes of a workspace)
 // ---------------------------------------------------------------------------
 struct StatusBlock {
-    int status;       // 0, W4A8_ERR_TIMEOUT or W4A8_ERR_BAD_BLOB: first failure wins
+    int status;       // 0, W4A8_ERR_TIMEOUT, _BAD_BLOB or _BAD_TABLE: first failure wins
     int where;        // site code of the wait that gave up
     int block;        // CTA that reported
     int pad[61];
@@ -304,6 +304,10 @@ cudaError_t launch_quantize_act_asym(const __half *X, const float *inv_s, int M,
 cudaError_t launch_norm_quantize_act(const __half *X, const float *weight, const float *bias,
                                      int layer_norm, float eps, int M, int K, int8_t *Xq,
                                      float *tok_scale, cudaStream_t st);
+cudaError_t launch_add_norm_quantize_act(const void *X, int x_type, const void *residual, int res_type,
+                                         void *residual_out, const float *weight, const float *bias,
+                                         int layer_norm, float eps, int M, int K, int8_t *Xq,
+                                         float *tok_scale, cudaStream_t st);
 cudaError_t launch_weight_rowsum(const uint8_t *blob, const BlobLayout &L, int32_t *rowsum,
                                  cudaStream_t st);
 cudaError_t launch_linear_simple(const int8_t *Xq, const float *tok_scale, const uint8_t *blob,

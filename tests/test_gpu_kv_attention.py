@@ -1,0 +1,224 @@
+"""Attention over the paged dINT4 cache against binary64 attention over the values it holds."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2311_05161_b200 as w4a8
+from kv_util import Batch, attention_reference, check_attention, filled_cache, vectors
+from util import Guarded
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+def run(lens, rows, P, Hq, H, D, q_type=F16, o_type=F16, causal=True, window=0, pad=0, seed=0, q_scale=1.0, v_scale=1.0,
+        scale=None):
+    bt = Batch(lens, rows, P, pad, seed=seed)
+    cache = filled_cache(bt, H, D, seed=seed + 5, scale=v_scale)
+    Q = (q_scale * torch.randn(bt.rows, Hq, D, generator=torch.Generator().manual_seed(seed + 9))).to(q_type).cuda()
+    ws = Guarded((w4a8.kv_attention_workspace_bytes(bt.rows, len(lens), Hq, H, D),), torch.uint8)
+    w4a8.workspace_init(ws.t)
+    out, lse = Guarded((bt.rows, Hq, D), o_type), Guarded((bt.rows, Hq), torch.float32)
+    out.t.fill_(7.0)
+    lse.t.fill_(7.0)
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+
+    def call():
+        w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws.t, cu_rows=bt.cu, scale=scale, causal=causal, window=window,
+                          out=out.t, lse=lse.t)
+        w4a8.check_status(ws.t)
+        return out.t.clone()
+
+    O = call()
+    out.check("O")
+    lse.check("lse")
+    ws.check("workspace")
+    o, want_lse, allow = attention_reference(Q, cache, bt, H, scale, causal, window)
+    n = bt.used
+    check_attention(O[:n], o[:n], allow[:n], o_type)
+    got_lse = lse.t[:n].cpu().double()
+    finite = torch.isfinite(want_lse[:n])
+    assert torch.equal(finite, torch.isfinite(got_lse))
+    # ln of the denominator: the scores' allowance again, and binary32
+    qsum = Q[:n].cpu().double().abs().sum(-1)
+    off = (D / 16 + 4) * 2.0 ** -23 * 30 * qsum * 2.0 * v_scale * scale + 2.0 ** -19 * (1 + want_lse[:n].abs())
+    assert bool(((got_lse - want_lse[:n]).abs()[finite] <= off[finite]).all())
+    assert bool((O[n:] == 7.0).all()) and bool((lse.t[n:] == 7.0).all())      # padding rows
+    assert torch.equal(call(), O)                                              # the same bits again
+    return O
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,H", [(1, 1), (4, 4), (8, 2), (5, 1), (7, 1), (16, 2), (16, 1), (24, 1), (12, 3)])
+def test_decode_head_layouts(D, Hq, H):
+    run([1, 0, 15, 16, 17, 100, 33], None, 16, Hq, H, D)
+
+
+@pytest.mark.parametrize("q_type", [F16, BF16])
+@pytest.mark.parametrize("o_type", [F16, BF16])
+def test_types(q_type, o_type):
+    run([70, 3, 129], None, 32, 8, 2, 128, q_type, o_type)
+    run([70, 3, 129], [4, 3, 9], 32, 8, 2, 64, q_type, o_type)
+
+
+@pytest.mark.parametrize("P", [16, 32, 64, 128, 1024])
+def test_page_sizes(P):
+    run([1000, 1, 64, 63, 65, 513], None, P, 8, 2, 128, BF16)
+
+
+@pytest.mark.parametrize("rows", [[2, 1, 0, 5], [17, 3, 1, 33], [64, 64, 64, 64]])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [0, 1, 21])
+def test_several_rows_per_sequence(rows, causal, window):
+    run([130, 3, 40, 64], rows, 32, 6, 2, 64, causal=causal, window=window, pad=2)
+    if window != 1:
+        run([130, 3, 40, 64], rows, 32, 4, 1, 128, BF16, BF16, causal=causal, window=window)
+
+
+def test_rows_that_see_nothing():
+    """More rows than tokens: the rows in front of position 0 get zeros; an empty sequence too."""
+    O = run([2, 0, 5], [6, 3, 1], 16, 4, 2, 64)
+    assert bool((O[:4] == 0).all()) and bool((O[6:9] == 0).all()) and bool((O[4:6] != 0).any())
+
+
+@pytest.mark.parametrize("window", [1, 7, 16, 100, 5000])
+def test_window_decode(window):
+    run([1, 40, 300, 129], None, 16, 8, 2, 128, window=window)
+
+
+def test_long_sequence_and_split():
+    run([40001], None, 64, 8, 2, 128, BF16, BF16)
+    run([9000, 1, 33, 2500], [1, 1, 3, 2], 64, 4, 4, 64)
+
+
+def test_many_sequences():
+    rng = np.random.default_rng(3)
+    run([int(v) for v in rng.integers(0, 90, 300)], None, 16, 4, 2, 64)
+
+
+@pytest.mark.parametrize("q_scale", [1e-3, 30.0])
+def test_flat_and_peaked_weights(q_scale):
+    run([257, 1000], None, 64, 8, 2, 128, q_scale=q_scale)
+    run([257, 100], [33, 100], 64, 8, 2, 128, q_scale=q_scale)
+
+
+@pytest.mark.parametrize("v_scale", [2.0 ** -14, 200.0])
+def test_small_and_large_cached_values(v_scale):
+    run([257, 31], None, 64, 8, 2, 128, F16, BF16, v_scale=v_scale, scale=0.1 / v_scale)
+
+
+def test_garbage_behind_the_sequence_is_not_seen():
+    """Slots behind a sequence's end and unused pages hold words that are infinities and NaN."""
+    H, D, P = 2, 128, 64
+    for lens, rows in (([5, 70, 64, 17], None), ([5, 70, 64, 17], [5, 40, 2, 17])):
+        bt = Batch(lens, rows, P)
+        cache = filled_cache(bt, H, D)
+        Q = torch.randn(bt.rows, 8, D, generator=torch.Generator().manual_seed(1)).to(F16).cuda()
+        ws = w4a8.new_kv_workspace(bt.rows, 4, 8, H, D)
+        want = w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, cu_rows=bt.cu).clone()
+        raw = cache.view(bt.num_pages, H, P // 16, 16 * (D + 8))
+        seen = torch.zeros(bt.num_pages, P, dtype=torch.bool)
+        for b, n in enumerate(lens):
+            for j in range(n):
+                seen[bt.table_host[b, j // P], j % P] = True
+        words = raw[..., 16 * D:].contiguous().view(torch.int32).view(bt.num_pages, H, P // 16, 2, 16)
+        hidden = (~seen).view(bt.num_pages, 1, P // 16, 1, 16).cuda().expand_as(words)
+        for bits in (0x7F800000, 0x7FFFFFFF, -1):
+            words[hidden] = bits
+            raw[..., 16 * D:] = words.view(torch.uint8).reshape(bt.num_pages, H, P // 16, 128)
+            got = w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, cu_rows=bt.cu)
+            w4a8.check_status(ws)
+            assert torch.equal(got, want)
+
+
+def test_strided_queries_other_stream_and_graph():
+    """Queries as a slice of a wider projection; on another stream; captured and replayed on new lengths."""
+    H, D, P, Hq = 2, 128, 32, 8
+    bt = Batch([200, 90, 31], None, P)
+    cache = filled_cache(bt, H, D)
+    wide = vectors((3, Hq + 2 * H, D), 4, F16).cuda()
+    Q = wide[:, :Hq]
+    ws = w4a8.new_kv_workspace(3, 3, Hq, H, D)
+    want = w4a8.kv_attention(Q.contiguous(), cache, bt.table, bt.kv_lens, H, ws)
+    assert torch.equal(w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws), want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = torch.empty_like(want)
+    with torch.cuda.stream(side):
+        w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, out=out)
+    for lens in ([200, 90, 31], [1, 0, 17], [150, 90, 1]):
+        bt.kv_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        graph.replay()
+        got = out.clone()
+        bt.lens = lens
+        o, _, allow = attention_reference(Q, cache, bt, H, 1 / math.sqrt(D))
+        check_attention(got, o, allow, F16)
+    w4a8.check_status(ws)
+
+
+def test_bad_tables_are_reported():
+    H, D, P = 2, 64, 16
+    cache = w4a8.new_kv_cache(4, P, H, D).fill_(0)
+    ws = w4a8.new_kv_workspace(8, 2, 4, H, D)
+
+    def i32(*v):
+        return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+    good = i32(0, 1).view(2, 1)
+    for rows in (2, 8):
+        Q = vectors((rows, 4, D), 1, F16).cuda()
+        ok = None if rows == 2 else i32(0, 4, 8)
+        for table, lens, cu in ((i32(4, 1).view(2, 1), i32(3, 3), ok), (i32(0, -1).view(2, 1), i32(9, 9), ok),
+                                (good, i32(3, 17), ok), (good, i32(-1, 3), ok), (good, i32(3, 3), i32(0, 1, 50)),
+                                (good, i32(3, 3), i32(0, -4, 2))):
+            w4a8.kv_attention(Q, cache, table, lens, H, ws, cu_rows=cu)
+            assert w4a8.poll_status(ws) == 9, (rows, table, lens, cu)
+        w4a8.kv_attention(Q, cache, good, i32(9, 9), H, ws, cu_rows=ok)
+        w4a8.check_status(ws)
+
+
+def test_decoder_step_through_the_public_calls():
+    """qkv linear -> append -> attention -> quantizer -> output linear -> residual + norm + quantizer, three
+    steps of two sequences, against the same step with dequantized tensors in binary64."""
+    from paper_2311_05161_b200 import synth
+    Hq, H, D, K, P = 4, 2, 64, 256, 16
+    qkv_n = (Hq + 2 * H) * D
+    g = torch.Generator().manual_seed(0)
+    lay1, lay2 = synth.make_layer(K, qkv_n, 2, seed=1), synth.make_layer(Hq * D, K, 2, seed=2)
+    p1, p2 = (w4a8.pack_weights(torch.from_numpy(l["W"]).cuda()) for l in (lay1, lay2))
+    ws1, ws2 = w4a8.new_workspace(2, qkv_n, K), w4a8.new_workspace(2, K, Hq * D)
+    ws = w4a8.new_kv_workspace(2, 2, Hq, H, D)
+    bt = Batch([13, 20], None, P)
+    cache = filled_cache(bt, H, D)
+    stream = torch.randn(2, K, generator=g).cuda()
+    weight = torch.ones(K, device="cuda")
+    Xq, tok = w4a8.quantize_act(torch.randn(2, K, generator=g).half().cuda())
+    for step in range(3):
+        lens = [14 + step, 21 + step]
+        bt.lens = lens
+        bt.kv_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        qkv = w4a8.linear(Xq, tok, p1, None, qkv_n, 0, ws1).view(2, Hq + 2 * H, D)
+        w4a8.kv_append(qkv[:, Hq:Hq + H], qkv[:, Hq + H:], cache, bt.table, bt.kv_lens, ws)
+        Q = qkv[:, :Hq]
+        o = w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws)
+        want, _, allow = attention_reference(Q, cache, bt, H, D ** -0.5)
+        check_attention(o, want, allow, F16)
+        Oq, otok = w4a8.quantize_act(o.view(2, Hq * D))
+        y = w4a8.linear(Oq, otok, p2, None, K, 0, ws2)
+        before = stream.clone()
+        Xq, tok, stream = w4a8.add_norm_quantize_act(y, stream, weight, residual_out=stream)
+        assert torch.equal(stream, before + y.float())
+        x = stream.double()
+        x = x / torch.sqrt((x * x).mean(-1, keepdim=True) + float(np.float32(1e-5)))
+        # half a code, and the binary32 roundings of x and of its product with 127 / amax
+        assert bool(((Xq.double() * tok.double()[:, None] - x).abs() <= (0.5 + 127 * 2.0 ** -21) * tok.double()[:, None]).all())
+    for w in (ws, ws1, ws2):
+        w4a8.check_status(w)
