@@ -1,105 +1,749 @@
-// Attention over the 4-bit cache: one CTA per row and query head, one pass over the keys with the
-// running maximum and sum of the softmax, everything in binary32 on the CUDA cores.
+// Attention over the 4-bit cache, decode form: a few query rows per sequence, many keys.
+//
+// The work is one scan of the cached blocks (16 tokens of one head, 2176 bytes for D = 128), each
+// expanded once from 4 bits to binary16 in registers and used twice on the tensor cores: the scores
+// S^T = K Q^T (tokens x query rows) and the output O^T = V^T P^T (elements x query rows), both with
+// mma.m16n8k16, so that up to eight query rows (the heads that share a key head, times the rows
+// of a sequence) ride on one expansion.  With the cache as the MMA's 16-row operand no part of the
+// instruction is spent on padding the few rows to 16, and a thread owns one or two tokens, whose
+// zero-points are then plain register constants.
+//
+// Expansion of eight codes (one word): five or six logic instructions put each rank i into the
+// mantissa of 16 + i (binary16), then two packed instructions make the level: with x = i - z - 1,
+// level = x - 2 sat(x / 4 + 1/2) + 1, so h = 16 + i, s = fma.sat(h, 1/4, -15/4 - z/4) and h - 2 s is the
+// level plus 16 + z.  That offset is a constant per token: the score accumulator starts from
+// -(16 + z) sum(q), and one extra MMA per block sums (16 + z) p for the output.  At the bandwidth of
+// the memory the SMs have about 2.9 lane instructions per code; this takes 2.
+//
+// Softmax: the weight of token j for the value product is 2^(s_j + log2(step_j) - m), with the value's
+// step folded into the exponent, so that it fits binary16 whatever the steps' sizes; the
+// denominator sums 2^(s_j - m) in binary32.  m is a running reference and no exact maximum: it moves
+// only when a weight would exceed 2^8 (one vote per block instead of a reduction).
+//
+// Schedule: the blocks of all (sequence, key head, row tile) items form one list, which the
+// CTAs share evenly whatever the lengths are (every CTA computes the list's prefix sums from the
+// lengths on the device); an item that several CTAs share leaves partial results in the
+// workspace and the last of them to finish joins all parts in list order, so the result does not
+// depend on who is last.  Inside a CTA the warps take blocks in turn, each with its own ring of
+// bulk copies.
 #include "kv_cache.cuh"
 
 namespace w4a8 {
 
 namespace {
 
-constexpr int kThreads = 128;
+constexpr unsigned long long kWaitNs = 2000000000ull;      // limit of every bounded wait
+constexpr uint32_t kSuspendHintNs = 1000;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kNoReference = -1.0e30f;
+constexpr float kSlack = 8.0f;                             // weights stay below 2^8
+constexpr int kWaitSite = 900;
 
-__device__ __forceinline__ float load16(const void *p, size_t i, int bf16)
+__device__ __forceinline__ uint32_t smem_addr(const void *p)
 {
-    return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i])
-                : __half2float(static_cast<const __half *>(p)[i]);
+    return (uint32_t)__cvta_generic_to_shared(p);
+}
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(kSuspendHintNs)
+        : "memory");
+    return ok != 0;
+}
+__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity)
+{
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
+    do {
+        if (try_wait(bar, parity)) return true;
+        asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    } while (t - t0 < kWaitNs);
+    return false;
+}
+__device__ __forceinline__ void copy_block(uint32_t dst, const uint8_t *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) kv_attention_kernel(KvAttnArgs a, StatusBlock *sb)
+__device__ __forceinline__ float ex2(float x)
 {
-    __shared__ float q[D], p[kThreads], red[kThreads / 32], vstep[kThreads];
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float lg2(float x)
+{
+    float y;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t perm(uint32_t a, uint32_t b, uint32_t sel)
+{
+    uint32_t d;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
+    return d;
+}
+__device__ __forceinline__ uint32_t hfma2_sat(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t d;
+    asm("fma.rn.sat.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t d;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_half2(float a, float b)
+{
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
+    return d;
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v)
+{
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t a0, const uint32_t a1, const uint32_t a2,
+                                      const uint32_t a3, const uint32_t b0, const uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+                 "{%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+constexpr uint32_t kNibble = 0x03C003C0u;    // bits 6-9 of both halves
+constexpr uint32_t kSixteen = 0x4C004C00u;   // 16.0 twice
+constexpr uint32_t kQuarter = 0x34003400u, kMinusQuarter = 0xB400B400u, kMinusTwo = 0xC000C000u;
+
+// Sixteen plus zero-point, as a pair of binary16 numbers, from a pair of zero-points.
+__device__ __forceinline__ uint32_t offset_pair(uint32_t zz) { return (zz << 6) | kSixteen; }
+// The constant of the saturated term: 1/4 - (16 + z) / 4.
+__device__ __forceinline__ uint32_t sat_constant(uint32_t off) { return hfma2(off, kMinusQuarter, kQuarter); }
+
+__device__ __forceinline__ uint32_t expand_pair(uint32_t bits, uint32_t c)
+{
+    const uint32_t h = (bits & kNibble) | kSixteen;
+    return hfma2(hfma2_sat(h, kQuarter, c), kMinusTwo, h);
+}
+// The four ranks of each 16-bit half of w -> four pairs (rank k of the low half, of the high half) as
+// levels plus 16 + z.
+__device__ __forceinline__ void expand(uint32_t w, uint32_t c, uint32_t (&o)[4])
+{
+    const uint32_t sw = perm(w, w, 0x2301u);         // the bytes of each half swapped
+    o[0] = expand_pair(w << 4, c);
+    o[1] = expand_pair(w, c);
+    o[2] = expand_pair(sw << 4, c);
+    o[3] = expand_pair(sw, c);
+}
+
+// What one launch needs beside the arguments.
+struct Schedule {
+    StatusBlock *sb;
+    int *counters;             // [workers]
+    float *partials;           // [workers][2] parts of R * (D + 2) numbers
+    int min_units;             // least share of a CTA
+};
+
+// One sequence's part of the work list.
+struct Seq {
+    int row0, n, len;          // rows of the call, tokens
+    int first, blocks;         // blocks that any of its rows can see
+    int tiles;                 // row tiles per key head
+    __device__ long long unit_count(int heads) const
+    {
+        return n > 0 ? (long long)heads * tiles * max(blocks, 1) : 0;
+    }
+};
+
+template <int R>
+__device__ __forceinline__ Seq load_seq(const KvAttnArgs &a, int b, int group, StatusBlock *sb)
+{
+    const KvBatch &bt = a.batch;
+    Seq s;
+    s.len = __ldg(bt.kv_lens + b);
+    s.row0 = bt.cu_rows ? __ldg(bt.cu_rows + b) : b;
+    const int row1 = bt.cu_rows ? __ldg(bt.cu_rows + b + 1) : b + 1;
+    s.n = row1 - s.row0;
+    const int most = bt.max_pages << a.cache.page_shift;
+    if (s.len < 0 || s.len > most || s.row0 < 0 || row1 > bt.rows || row1 < s.row0) {
+        report_failure(sb, W4A8_ERR_BAD_TABLE, b);
+        s.len = min(max(s.len, 0), most);
+        if (s.row0 < 0 || row1 > bt.rows || row1 < s.row0) s.n = 0;
+    }
+    const int lo = a.window > 0 ? max(0, s.len - s.n + 1 - a.window) : 0;
+    s.first = lo >> 4;
+    s.blocks = max(0, ((s.len + 15) >> 4) - s.first);
+    s.tiles = (int)(((long long)s.n * group + R - 1) / R);
+    return s;
+}
+
+template <int D, int NT, int WARPS>
+struct Shape {
+    static constexpr int R = 8 * NT;                       // query rows of a tile
+    static constexpr int kBlockBytes = 16 * (D + 8);
+    static constexpr int kStages = D == 128 ? 6 : 10;      // copies in flight per warp
+    static constexpr int kRing = WARPS * kStages * kBlockBytes;
+    static constexpr int kPad = D + 4;
+    static constexpr int kJoin = WARPS * R * kPad * 4;     // overlays the ring between items
+    static constexpr int kBig = kRing > kJoin ? kRing : kJoin;
+    static constexpr int kSmem = (kBig + WARPS * kStages * 8 + 127) / 128 * 128;
+    static constexpr int kCtas = NT == 1 ? 16 / WARPS : (WARPS <= 12 ? 12 / WARPS : 1);
+    static_assert(kCtas * (kSmem + 2048) <= 232448, "shared memory of an SM");
+};
+
+template <int D, int NT, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, Shape<D, NT, WARPS>::kCtas)
+kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
+{
+    using S = Shape<D, NT, WARPS>;
+    constexpr int R = S::R, KW = D / 32, KT = D / 16, BB = S::kBlockBytes, THREADS = WARPS * 32;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ long long warp_units[WARPS], found_off;
+    __shared__ int found_b, last_part;
+    __shared__ float row_m[WARPS][R], row_l[WARPS][R], tile_m[R], tile_l[R];
+    __shared__ int row_hi[R], row_lo[R];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const uint32_t ring = smem_addr(smem) + warp * S::kStages * BB;
+    const uint8_t *ring_ptr = smem + warp * S::kStages * BB;
+    const uint32_t bars = smem_addr(smem) + S::kBig + warp * S::kStages * 8;
+    if (lane < S::kStages) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + lane * 8) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncwarp();
     allow_dependents();
     dependent_wait();
-    const int row = blockIdx.x, head = blockIdx.y, tid = threadIdx.x;
+
     const KvBatch &bt = a.batch;
-    const int b = kv_sequence_of(bt, row);
-    if (b >= bt.batch) return;
-    bool ok;
-    const int pos = kv_position_of(bt, b, row, ok);
-    if (!ok && tid == 0) report_failure(sb, W4A8_ERR_BAD_TABLE, row);
-    const int hi = !ok || pos < 0 ? 0 : (a.causal ? pos + 1 : __ldg(bt.kv_lens + b));
-    const int lo = a.window > 0 ? max(0, pos + 1 - a.window) : 0;
-    for (int d = tid; d < D; d += kThreads)
-        q[d] = load16(a.Q, (size_t)(row * a.q_stride) + (size_t)head * D + d, a.q_bf16);
+    const int heads = a.cache.heads, group = a.q_heads / heads;
+    // ---- this CTA's share of the work list ----
+    const int chunk = (bt.batch + THREADS - 1) / THREADS;
+    const int b_first = min(bt.batch, tid * chunk), b_last = min(bt.batch, b_first + chunk);
+    long long mine = 0;
+    for (int b = b_first; b < b_last; ++b) mine += load_seq<R>(a, b, group, sc.sb).unit_count(heads);
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) warp_units[warp] = incl;
     __syncthreads();
-    const int kvh = head / (a.q_heads / a.cache.heads);
-    float m = -INFINITY, sum = 0.0f, acc = 0.0f;
-    const float scale = a.scale;
-    for (int base = lo & ~15; base < hi; base += kThreads) {
-        const int j = base + tid;
-        float sc = -INFINITY;
-        const uint8_t *blk = nullptr;
-        if (j >= lo && j < hi) {
-            const int page = kv_page_of(a.cache, bt, b, j);
-            if (page < 0) report_failure(sb, W4A8_ERR_BAD_TABLE, row);
-            else blk = kv_block_at(a.cache, page, kvh, j & ((1 << a.cache.page_shift) - 1));
-        }
-        vstep[tid] = 0.0f;
-        if (blk) {
-            const uint32_t wk = *reinterpret_cast<const uint32_t *>(blk + kv_word_offset(D, 0, j & 15));
-            float dot = 0.0f;
-            for (int w = 0; w < D / 8; ++w) {
-                const uint32_t c = *reinterpret_cast<const uint32_t *>(blk + kv_code_offset(D, 0, j & 15, w));
-                for (int e = 0; e < 8; ++e)
-                    dot = fmaf(q[8 * w + e], kv_level(kv_rank_at(c, e), (int)(wk & 15u)), dot);
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+        if (w < warp) incl += warp_units[w];
+        total += warp_units[w];
+    }
+    const long long per = max((total + gridDim.x - 1) / (long long)gridDim.x, (long long)sc.min_units);
+    const long long begin = (long long)blockIdx.x * per, end = min(total, begin + per);
+    if (begin >= total) return;
+    if (begin >= incl - mine && begin < incl) {
+        long long at = incl - mine;
+        for (int b = b_first; b < b_last; ++b) {
+            const long long u = load_seq<R>(a, b, group, sc.sb).unit_count(heads);
+            if (begin < at + u) {
+                found_b = b;
+                found_off = begin - at;
+                break;
             }
-            sc = dot * __uint_as_float(wk & ~15u) * scale;
+            at += u;
         }
-        float mx = sc;
-        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        if ((tid & 31) == 0) red[tid >> 5] = mx;
-        __syncthreads();
-        mx = m;
-        for (int w = 0; w < kThreads / 32; ++w) mx = fmaxf(mx, red[w]);
-        const float keep = mx == -INFINITY ? 1.0f : expf(m - mx);
-        m = mx;
-        p[tid] = sc == -INFINITY ? 0.0f : expf(sc - m);
-        __syncthreads();
-        sum *= keep;
-        acc *= keep;
-        const int n = min(kThreads, hi - base);
-        for (int i = 0; i < n; ++i) {
-            sum += p[i];
-            const int j2 = base + i;
-            if (tid < D && p[i] != 0.0f) {
-                const int page = kv_page_of(a.cache, bt, b, j2);
-                const uint8_t *bl = kv_block_at(a.cache, page, kvh, j2 & ((1 << a.cache.page_shift) - 1));
-                const uint32_t wv = *reinterpret_cast<const uint32_t *>(bl + kv_word_offset(D, 1, j2 & 15));
-                const uint32_t c = *reinterpret_cast<const uint32_t *>(bl + kv_code_offset(D, 1, j2 & 15, tid >> 3));
-                acc = fmaf(p[i], kv_level(kv_rank_at(c, tid & 7), (int)(wv & 15u)) * __uint_as_float(wv & ~15u), acc);
+    }
+    __syncthreads();
+    int b = found_b;
+    long long off = found_off;             // units of sequence b in front of this CTA's next one
+    int stage = 0;
+    uint32_t parity = 0;
+    int pending = 0;                       // requested copies that have not been waited for
+    bool dead = false;                     // a copy did not arrive in time: nothing more is requested
+
+    for (long long u = begin; u < end;) {
+        const Seq s = load_seq<R>(a, b, group, sc.sb);
+        const long long all = s.unit_count(heads);
+        if (off >= all) {
+            off -= all;
+            ++b;
+            continue;
+        }
+        const int item_units = max(s.blocks, 1);
+        const int item = (int)(off / item_units), in_item = (int)(off - (long long)item * item_units);
+        const int h = item / s.tiles, tile = item - h * s.tiles;
+        const int count = (int)min((long long)(item_units - in_item), end - u);
+        const bool whole = count == item_units;
+        const long long item_begin = u - in_item;
+
+        // rows of this tile: r = tile * R + i is row r / group of the sequence, query head r % group
+        const int rows_here = min(R, (int)((long long)s.n * group - (long long)tile * R));
+        const int i_first = tile * R / group, i_last = (tile * R + rows_here - 1) / group;
+        const int pos0 = s.len - s.n;
+        // a row sees [row_lo, row_hi); one in front of position 0 sees nothing
+        auto hi_of = [&](int i) { return pos0 + i < 0 ? 0 : a.causal ? pos0 + i + 1 : s.len; };
+        const int hi_max = hi_of(i_last), hi_min = hi_of(i_first);
+        const int lo_min = a.window > 0 ? max(0, pos0 + i_first + 1 - a.window) : 0;
+        const int lo_max = a.window > 0 ? max(0, pos0 + i_last + 1 - a.window) : 0;
+        if (tid < R) {
+            const int i = (tile * R + tid) / group;
+            const bool in = tid < rows_here;
+            row_hi[tid] = in ? hi_of(i) : s.len;
+            row_lo[tid] = in && a.window > 0 ? pos0 + i + 1 - a.window : 0;
+        }
+        // blocks of the share that some row of the tile sees, and this warp's among them
+        const int k0 = max(s.first + in_item, lo_min >> 4);
+        const int k1 = min(s.first + min(in_item + count, s.blocks), (hi_max + 15) >> 4);
+        const int nk = k1 > k0 + warp ? (k1 - k0 - warp + WARPS - 1) / WARPS : 0;
+        const int32_t *table = bt.page_table + (size_t)b * bt.max_pages;
+        const uint8_t *head_base = a.cache.pages + ((size_t)h << a.cache.page_shift) * (D + 8);
+        const int in_page = (1 << (a.cache.page_shift - 4)) - 1;
+        int page = 0;
+        auto load_pages = [&](int k) {       // pages of this warp's blocks k .. k + 31, one per lane
+            const int blk = k0 + warp + (k + lane) * WARPS;
+            page = 0;
+            if (blk < k1) {
+                page = __ldg(table + (blk >> (a.cache.page_shift - 4)));
+                if ((unsigned)page >= (unsigned)a.cache.num_pages) {
+                    report_failure(sc.sb, W4A8_ERR_BAD_TABLE, b);
+                    page = 0;
+                }
+            }
+        };
+        auto request = [&](int k, int st) {  // copy this warp's block k into ring slot st
+            if ((k & 31) == 0) load_pages(k);
+            const int p = __shfl_sync(0xffffffffu, page, k & 31);
+            const int blk = k0 + warp + k * WARPS;
+            if (dead) return;
+            ++pending;
+            if (lane == 0)
+                copy_block(ring + st * BB, head_base + (size_t)p * a.cache.page_bytes() + (size_t)(blk & in_page) * BB, BB,
+                           bars + st * 8);
+        };
+        {
+            int st = stage;
+            for (int k = 0; k < min(nk, S::kStages); ++k) {
+                request(k, st);
+                st = st + 1 == S::kStages ? 0 : st + 1;
             }
         }
+        // ---- queries: this thread's elements D/4 t .. D/4 t + D/4 - 1 of row g of every n-tile, scaled by a
+        // power of two to the top of binary16's range ----
+        uint32_t q[NT][KT][2];
+        float qsum[NT][2], unit;
+        {
+            float amax = 0.0f;
+            uint4 raw[NT][KW];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int r = tile * R + n * 8 + g;
+                const bool in = n * 8 + g < rows_here;
+                const size_t at = in ? (size_t)(s.row0 + r / group) * a.q_stride + (size_t)(h * group + r % group) * D + t * (D / 4) : 0;
+                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + at);
+#pragma unroll
+                for (int w = 0; w < KW; ++w) raw[n][w] = in ? __ldg(p + w) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (int w = 0; w < KW; ++w)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t v = (&raw[n][w].x)[i] & 0x7fff7fffu;
+                        if (a.q_bf16) amax = fmaxf(amax, fmaxf(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)));
+                        else {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v));
+                            amax = fmaxf(amax, fmaxf(f.x, f.y));
+                        }
+                    }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            // amax * 2^-e in [2^14, 2^15); amax >= 2^-126 or 0, both factors normal
+            const int e = min(max((int)((__float_as_uint(amax) >> 23) & 255u) - 127 - 14, -100), 113);
+            const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+            unit = a.scale * kLog2e * __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int w = 0; w < KW; ++w) {
+                    float f[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t v = (&raw[n][w].x)[i];
+                        if (a.q_bf16) {
+                            f[2 * i] = __uint_as_float(v << 16);
+                            f[2 * i + 1] = __uint_as_float(v & 0xffff0000u);
+                        } else {
+                            const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&v));
+                            f[2 * i] = x.x;
+                            f[2 * i + 1] = x.y;
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {            // the order in which expand() gives a word's levels
+                        const uint32_t v = pack_half2(f[k] * down, f[k + 4] * down);
+                        q[n][2 * w + (k >> 1)][k & 1] = v;
+                        const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&v));
+                        sum += x.x + x.y;
+                    }
+                }
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                qsum[n][0] = -__shfl_sync(0xffffffffu, sum, 8 * t);
+                qsum[n][1] = -__shfl_sync(0xffffffffu, sum, 8 * t + 4);
+            }
+        }
+        float o[NT][KT][4], osum[NT][4], ref[NT][2], l[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < KT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[n][i][j] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) osum[n][j] = 0.0f;
+            ref[n][0] = ref[n][1] = kNoReference;
+            l[n][0] = l[n][1] = 0.0f;
+        }
+        __syncthreads();                   // row_hi, row_lo
+        const uint32_t only_g0 = g == 0 ? 0xffffffffu : 0u;
+
+        for (int k = 0; k < nk; ++k) {
+            const uint32_t bar = bars + stage * 8;
+            if (pending > 0) {
+                --pending;
+                if (!try_wait(bar, parity) && !wait_slow(bar, parity)) {
+                    dead = true;
+                    if (lane == 0) report_failure(sc.sb, W4A8_ERR_TIMEOUT, kWaitSite);
+                }
+            }
+            dead = __any_sync(0xffffffffu, dead);
+            const uint8_t *blk = ring_ptr + stage * BB;
+            const uint32_t wk0 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 4 * g);
+            const uint32_t wk1 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 4 * g + 32);
+            const uint32_t wv0 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 64 + 4 * g);
+            const uint32_t wv1 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 64 + 4 * g + 32);
+            const uint2 wva = *reinterpret_cast<const uint2 *>(blk + 16 * D + 64 + 8 * t);
+            const uint2 wvb = *reinterpret_cast<const uint2 *>(blk + 16 * D + 64 + 8 * t + 32);
+            // ---- scores ----
+            float c[NT][4];
+            {
+                const uint32_t z0 = wk0 & 15u, z1 = wk1 & 15u;
+                const float f0 = __uint_as_float(0x41800000u | (z0 << 19)), f1 = __uint_as_float(0x41800000u | (z1 << 19));
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    c[n][0] = f0 * qsum[n][0];
+                    c[n][1] = f0 * qsum[n][1];
+                    c[n][2] = f1 * qsum[n][0];
+                    c[n][3] = f1 * qsum[n][1];
+                }
+                const uint32_t s0 = sat_constant(offset_pair(z0 * 0x10001u)), s1 = sat_constant(offset_pair(z1 * 0x10001u));
+                uint32_t k0w[KW], k1w[KW];
+                const uint8_t *p = blk + g * (D / 2) + t * (D / 8);
+                if constexpr (KW == 4) {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(p), y = *reinterpret_cast<const uint4 *>(p + 4 * D);
+                    k0w[0] = x.x; k0w[1] = x.y; k0w[2] = x.z; k0w[3] = x.w;
+                    k1w[0] = y.x; k1w[1] = y.y; k1w[2] = y.z; k1w[3] = y.w;
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2 *>(p), y = *reinterpret_cast<const uint2 *>(p + 4 * D);
+                    k0w[0] = x.x; k0w[1] = x.y;
+                    k1w[0] = y.x; k1w[1] = y.y;
+                }
+#pragma unroll
+                for (int w = 0; w < KW; ++w) {
+                    uint32_t e0[4], e1[4];
+                    expand(k0w[w], s0, e0);
+                    expand(k1w[w], s1, e1);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        mma16(c[n], e0[0], e1[0], e0[1], e1[1], q[n][2 * w][0], q[n][2 * w][1]);
+                        mma16(c[n], e0[2], e1[2], e0[3], e1[3], q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
+                    }
+                }
+            }
+            // ---- weights ----
+            const float u0 = unit * __uint_as_float(wk0 & ~15u), u1 = unit * __uint_as_float(wk1 & ~15u);
+            const float v0 = lg2(__uint_as_float(wv0 & ~15u)), v1 = lg2(__uint_as_float(wv1 & ~15u));
+            const int j0 = (k0 + warp + k * WARPS) * 16;
+            float wt[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                c[n][0] *= u0;
+                c[n][1] *= u0;
+                c[n][2] *= u1;
+                c[n][3] *= u1;
+                wt[n][0] = c[n][0] + v0;
+                wt[n][1] = c[n][1] + v0;
+                wt[n][2] = c[n][2] + v1;
+                wt[n][3] = c[n][3] + v1;
+            }
+            if (j0 < lo_max || j0 + 16 > hi_min) {           // some row does not see all of the block
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = n * 8 + 2 * t + (i & 1), j = j0 + g + (i >> 1) * 8;
+                        if (j < row_lo[r] || j >= row_hi[r]) c[n][i] = wt[n][i] = -INFINITY;
+                    }
+            }
+            bool over = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                over |= fmaxf(wt[n][0], wt[n][2]) > ref[n][0] + kSlack;
+                over |= fmaxf(wt[n][1], wt[n][3]) > ref[n][1] + kSlack;
+            }
+            if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float m = fmaxf(wt[n][j], wt[n][2 + j]);
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                        m = fmaxf(m, ref[n][j]);
+                        const float keep = ex2(ref[n][j] - m);
+                        ref[n][j] = m;
+                        l[n][j] *= keep;
+                        osum[n][j] *= keep;
+#pragma unroll
+                        for (int i = 0; i < KT; ++i) {
+                            o[n][i][j] *= keep;
+                            o[n][i][2 + j] *= keep;
+                        }
+                    }
+            }
+            uint32_t pb[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                l[n][0] += ex2(c[n][0] - ref[n][0]) + ex2(c[n][2] - ref[n][0]);
+                l[n][1] += ex2(c[n][1] - ref[n][1]) + ex2(c[n][3] - ref[n][1]);
+                pb[n][0] = transpose8(pack_half2(ex2(wt[n][0] - ref[n][0]), ex2(wt[n][1] - ref[n][1])));
+                pb[n][1] = transpose8(pack_half2(ex2(wt[n][2] - ref[n][0]), ex2(wt[n][3] - ref[n][1])));
+            }
+            // ---- values ----
+            {
+                const uint32_t za = offset_pair((wva.x & 15u) | ((wva.y & 15u) << 16));
+                const uint32_t zb = offset_pair((wvb.x & 15u) | ((wvb.y & 15u) << 16));
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma16(osum[n], za & only_g0, 0u, zb & only_g0, 0u, pb[n][0], pb[n][1]);
+                const uint32_t sa = sat_constant(za), sbb = sat_constant(zb);
+                constexpr int VW = D / 64;                   // words per token and slice
+                const uint8_t *p = blk + 8 * D + g * (D / 2) + t * (D / 8);
+                uint32_t xa[2][VW], xb[2][VW];               // [token of the pair][word]
+                if constexpr (VW == 2) {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(p), y = *reinterpret_cast<const uint4 *>(p + 4 * D);
+                    xa[0][0] = x.x; xa[0][1] = x.y; xa[1][0] = x.z; xa[1][1] = x.w;
+                    xb[0][0] = y.x; xb[0][1] = y.y; xb[1][0] = y.z; xb[1][1] = y.w;
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2 *>(p), y = *reinterpret_cast<const uint2 *>(p + 4 * D);
+                    xa[0][0] = x.x; xa[1][0] = x.y;
+                    xb[0][0] = y.x; xb[1][0] = y.y;
+                }
+#pragma unroll
+                for (int w = 0; w < VW; ++w)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t ea[4], eb[4];
+                        const uint32_t sel = half ? 0x7632u : 0x5410u;
+                        expand(perm(xa[0][w], xa[1][w], sel), sa, ea);
+                        expand(perm(xb[0][w], xb[1][w], sel), sbb, eb);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            mma16(o[n][4 * w + 2 * half], ea[0], ea[1], eb[0], eb[1], pb[n][0], pb[n][1]);
+                            mma16(o[n][4 * w + 2 * half + 1], ea[2], ea[3], eb[2], eb[3], pb[n][0], pb[n][1]);
+                        }
+                    }
+            }
+            __syncwarp();                  // every lane is done with the slot
+            if (k + S::kStages < nk) request(k + S::kStages, stage);
+            if (++stage == S::kStages) {
+                stage = 0;
+                parity ^= 1u;
+            }
+        }
+
+        // ---- join the warps: element d of row r of the tile ----
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float v = l[n][j];
+                v += __shfl_xor_sync(0xffffffffu, v, 4);
+                v += __shfl_xor_sync(0xffffffffu, v, 8);
+                v += __shfl_xor_sync(0xffffffffu, v, 16);
+                if (g == 0) {
+                    row_m[warp][n * 8 + 2 * t + j] = ref[n][j];
+                    row_l[warp][n * 8 + 2 * t + j] = v;
+                }
+            }
+        __syncthreads();                   // also: no warp still reads its ring
+        float *join = reinterpret_cast<float *>(smem);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = n * 8 + 2 * t + j;
+                float m = row_m[0][r];
+#pragma unroll
+                for (int w = 1; w < WARPS; ++w) m = fmaxf(m, row_m[w][r]);
+                const float keep = ex2(ref[n][j] - m);
+                const float sum = __shfl_sync(0xffffffffu, osum[n][j], t);
+                float *to = join + ((size_t)warp * R + r) * S::kPad + g * (D / 8);
+#pragma unroll
+                for (int i = 0; i < KT; ++i)
+                    *reinterpret_cast<float2 *>(to + 2 * i) =
+                        make_float2((o[n][i][j] - sum) * keep, (o[n][i][2 + j] - sum) * keep);
+            }
+        if (tid < R) {
+            float m = row_m[0][tid], v = 0.0f;
+#pragma unroll
+            for (int w = 1; w < WARPS; ++w) m = fmaxf(m, row_m[w][tid]);
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) v += row_l[w][tid] * ex2(row_m[w][tid] - m);
+            tile_m[tid] = m;
+            tile_l[tid] = v;
+        }
+        __syncthreads();
+        const int part_size = R * (D + 2);
+        constexpr int kQuads = R * D / 4;
+        auto write_row = [&](int r, int d, float4 v, float m, float lsum) {
+            const int i = tile * R + r;
+            const size_t at = ((size_t)(s.row0 + i / group) * a.q_heads + h * group + i % group) * D + d;
+            const float inv = lsum > 0.0f ? __fdiv_rn(1.0f, lsum) : 0.0f;
+            v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
+            uint2 out;
+            if (a.o_bf16) {
+                const float top = __uint_as_float(0x7f7f0000u);
+                const __nv_bfloat162 x = __floats2bfloat162_rn(fminf(fmaxf(v.x, -top), top), fminf(fmaxf(v.y, -top), top));
+                const __nv_bfloat162 y = __floats2bfloat162_rn(fminf(fmaxf(v.z, -top), top), fminf(fmaxf(v.w, -top), top));
+                out.x = *reinterpret_cast<const uint32_t *>(&x);
+                out.y = *reinterpret_cast<const uint32_t *>(&y);
+            } else {
+                const float top = 65504.0f;
+                out.x = pack_half2(fminf(fmaxf(v.x, -top), top), fminf(fmaxf(v.y, -top), top));
+                out.y = pack_half2(fminf(fmaxf(v.z, -top), top), fminf(fmaxf(v.w, -top), top));
+            }
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.O) + at) = out;
+            if (a.lse && d == 0) a.lse[at / D] = lsum > 0.0f ? (m + lg2(lsum)) * kLn2 : -INFINITY;
+        };
+        float *part = sc.partials + ((size_t)blockIdx.x * 2 + (u == begin ? 0 : 1)) * part_size;
+        for (int i = tid; i < kQuads; i += THREADS) {
+            const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                const float4 x = *reinterpret_cast<const float4 *>(join + ((size_t)w * R + r) * S::kPad + d);
+                v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+            }
+            if (!whole) __stcg(reinterpret_cast<float4 *>(part + 2 * R) + i, v);
+            else if (r < rows_here) write_row(r, d, v, tile_m[r], tile_l[r]);
+        }
+        if (!whole) {
+            if (tid < R) {
+                __stcg(part + tid, tile_m[tid]);
+                __stcg(part + R + tid, tile_l[tid]);
+            }
+            __threadfence();
+            __syncthreads();
+            const int w0 = (int)(item_begin / per), w1 = (int)((item_begin + item_units - 1) / per);
+            if (tid == 0) last_part = atomicAdd(sc.counters + w0, 1) == w1 - w0;
+            __syncthreads();
+            if (last_part) {
+                __threadfence();
+                // part of worker w: its first segment, unless the item begins inside its share
+                const bool inside = item_begin > (long long)w0 * per;
+                const float *first = sc.partials + ((size_t)w0 * 2 + (inside ? 1 : 0)) * part_size;
+                const float *rest = sc.partials + (size_t)w0 * 2 * part_size;
+                const int parts = w1 - w0 + 1;
+                for (int i = tid; i < kQuads; i += THREADS) {
+                    const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+                    if (r >= rows_here) continue;
+                    float m = __ldcg(first + r);
+#pragma unroll 8
+                    for (int p = 1; p < parts; ++p) m = fmaxf(m, __ldcg(rest + (size_t)p * 2 * part_size + r));
+                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    float lsum = 0.0f;
+#pragma unroll 8
+                    for (int p = 0; p < parts; ++p) {
+                        const float *x = p == 0 ? first : rest + (size_t)p * 2 * part_size;
+                        const float keep = ex2(__ldcg(x + r) - m);
+                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(x + 2 * R) + i);
+                        lsum += __ldcg(x + R + r) * keep;
+                        v.x += y.x * keep; v.y += y.y * keep; v.z += y.z * keep; v.w += y.w * keep;
+                    }
+                    write_row(r, d, v, m, lsum);
+                }
+                if (tid == 0) sc.counters[w0] = 0;           // ready for the next call
+            }
+        }
+        u += count;
+        off += count;
+        // the join buffer was written by ordinary stores: order them before the next copies into the ring
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
     }
-    const size_t at = (size_t)row * a.q_heads + head;
-    if (tid < D) {
-        const float o = sum > 0.0f ? acc / sum : 0.0f;
-        if (a.o_bf16) static_cast<__nv_bfloat16 *>(a.O)[at * D + tid] = __float2bfloat16_rn(o);
-        else static_cast<__half *>(a.O)[at * D + tid] = __float2half_rn(fminf(fmaxf(o, -65504.0f), 65504.0f));
-    }
-    if (a.lse && tid == 0) a.lse[at] = sum > 0.0f ? m + logf(sum) : -INFINITY;
+}
+
+// Rows per tile and warps per CTA.
+struct Variant {
+    int nt, warps, ctas;
+};
+Variant pick(const KvAttnArgs &a)
+{
+    const int group = a.q_heads / a.cache.heads;
+    const long long rows = (long long)group * ((a.batch.rows + a.batch.batch - 1) / a.batch.batch);
+    Variant v;
+    v.nt = rows > 8 ? 2 : 1;
+    const long long items = (long long)a.batch.batch * a.cache.heads * ((rows + 8 * v.nt - 1) / (8 * v.nt));
+    // few items: every item is split over several CTAs, and wide CTAs leave fewer parts to join;
+    // many: narrow CTAs, whose ends and beginnings overlap with their neighbours' streaming
+    v.warps = items >= 2 * device_sms() ? 4 : (v.nt == 1 ? 16 : 12);
+    v.ctas = device_sms() * ((v.nt == 1 ? 16 : 12) / v.warps);
+    return v;
+}
+
+size_t counters_bytes() { return align_up((size_t)device_sms() * 4 * sizeof(int), 256); }
+
+template <int D, int NT, int WARPS>
+cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
+{
+    using S = Shape<D, NT, WARPS>;
+    const cudaError_t e = cudaFuncSetAttribute(kv_decode_kernel<D, NT, WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_overlapped(kv_decode_kernel<D, NT, WARPS>, dim3(ctas), dim3(WARPS * 32), S::kSmem, st, a, sc);
+}
+template <int D>
+cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, const Variant &v, cudaStream_t st)
+{
+    if (v.nt == 1) return v.warps == 4 ? launch<D, 1, 4>(a, sc, v.ctas, st) : launch<D, 1, 16>(a, sc, v.ctas, st);
+    return v.warps == 4 ? launch<D, 2, 4>(a, sc, v.ctas, st) : launch<D, 2, 12>(a, sc, v.ctas, st);
 }
 
 }  // namespace
 
-size_t kv_attention_workspace(int, int, int, int, int) { return sizeof(StatusBlock); }
+// Status block, a counter per CTA, two partial results per CTA (at most 4 CTAs of one n-tile or 3 of two per SM).
+size_t kv_attention_workspace(int, int, int, int, int D)
+{
+    return sizeof(StatusBlock) + counters_bytes() + (size_t)device_sms() * 3 * 2 * 16 * (D + 2) * sizeof(float);
+}
 
 cudaError_t launch_kv_attention(const KvAttnArgs &a, uint8_t *workspace, cudaStream_t st)
 {
-    StatusBlock *sb = reinterpret_cast<StatusBlock *>(workspace);
-    const dim3 grid(a.batch.rows, a.q_heads);
-    return a.cache.D == 64 ? launch_overlapped(kv_attention_kernel<64>, grid, dim3(kThreads), 0, st, a, sb)
-                           : launch_overlapped(kv_attention_kernel<128>, grid, dim3(kThreads), 0, st, a, sb);
+    const Variant v = pick(a);
+    Schedule sc;
+    sc.sb = reinterpret_cast<StatusBlock *>(workspace);
+    sc.counters = reinterpret_cast<int *>(workspace + sizeof(StatusBlock));
+    sc.partials = reinterpret_cast<float *>(workspace + sizeof(StatusBlock) + counters_bytes());
+    sc.min_units = v.warps;
+    return a.cache.D == 64 ? launch<64>(a, sc, v, st) : launch<128>(a, sc, v, st);
 }
 
 }  // namespace w4a8
