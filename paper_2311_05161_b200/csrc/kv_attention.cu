@@ -8,17 +8,18 @@
 // instruction is spent on padding the few rows to 16, and a thread owns one or two tokens, whose
 // zero-points are then plain register constants.
 //
-// Expansion of eight codes (one word): five or six logic instructions put each rank i into the
-// mantissa of 16 + i (binary16), then two packed instructions make the level: with x = i - z - 1,
-// level = x - 2 sat(x / 4 + 1/2) + 1, so h = 16 + i, s = fma.sat(h, 1/4, -15/4 - z/4) and h - 2 s is the
-// level plus 16 + z.  That offset is a constant per token: the score accumulator starts from
-// -(16 + z) sum(q), and one extra MMA per block sums (16 + z) p for the output.  At the bandwidth of
-// the memory the SMs have about 2.9 lane instructions per code; this takes 2.
+// Expansion of eight codes (one word): with x = i - z - 1 for rank i, the level is
+// x - 2 sat(x / 4 + 1/2) + 1.  Seven logic instructions put each rank into the mantissa of
+// lin = -(16 + i) / 2 (binary16), one packed fma.sat per pair makes the saturated term, and the tensor
+// cores add the two parts: they take both as operands, -2 (lin + sat) = level + 16 + z.  The factor
+// goes into the scale, the offset is a constant per token: the score accumulator starts from it times
+// sum(q), and one extra MMA per block sums (16 + z) p for the output.  At the bandwidth of the memory the
+// SMs have about 2.9 lane instructions per code and the logic pipe half of that; this takes 1.6.
 //
 // Softmax: the weight of token j for the value product is 2^(s_j + log2(step_j) - m), with the value's
 // step folded into the exponent, so that it fits binary16 whatever the steps' sizes; the
 // denominator sums 2^(s_j - m) in binary32.  m is a running reference and no exact maximum: it moves
-// only when a weight would exceed 2^8 (one vote per block instead of a reduction).
+// only when a weight would exceed 2^8 (one vote per 32 tokens instead of a reduction).
 //
 // Schedule: the blocks of all (sequence, key head, row tile) items form one list, which the
 // CTAs share evenly whatever the lengths are (every CTA computes the list's prefix sums from the
@@ -38,6 +39,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoReference = -1.0e30f;
 constexpr float kSlack = 8.0f;                             // weights stay below 2^8
 constexpr int kWaitSite = 900;
+constexpr int kLead = 8;                                   // an item's fixed cost, in units of 32 tokens
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p)
 {
@@ -65,9 +67,12 @@ __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity)
     } while (t - t0 < kWaitNs);
     return false;
 }
-__device__ __forceinline__ void copy_block(uint32_t dst, const uint8_t *src, uint32_t bytes, uint32_t bar)
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_block(uint32_t dst, const uint8_t *src, uint32_t bytes, uint32_t bar)
+{
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                  "l"(src), "r"(bytes), "r"(bar)
                  : "memory");
@@ -82,7 +87,13 @@ __device__ __forceinline__ float ex2(float x)
 __device__ __forceinline__ float lg2(float x)
 {
     float y;
-    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ uint32_t perm(uint32_t a, uint32_t b, uint32_t sel)
@@ -125,28 +136,56 @@ __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t a0, const ui
 }
 
 constexpr uint32_t kNibble = 0x03C003C0u;    // bits 6-9 of both halves
-constexpr uint32_t kSixteen = 0x4C004C00u;   // 16.0 twice
-constexpr uint32_t kQuarter = 0x34003400u, kMinusQuarter = 0xB400B400u, kMinusTwo = 0xC000C000u;
+constexpr uint32_t kMinusEight = 0xC800C800u, kSixteen = 0x4C004C00u;
+constexpr uint32_t kMinusHalf = 0xB800B800u, kQuarter = 0x34003400u, kMinusQuarter = 0xB400B400u;
 
-// Sixteen plus zero-point, as a pair of binary16 numbers, from a pair of zero-points.
-__device__ __forceinline__ uint32_t offset_pair(uint32_t zz) { return (zz << 6) | kSixteen; }
-// The constant of the saturated term: 1/4 - (16 + z) / 4.
+// The constant of the saturated term, 1/4 - (16 + z) / 4, from a pair of binary16 numbers 16 + z.
 __device__ __forceinline__ uint32_t sat_constant(uint32_t off) { return hfma2(off, kMinusQuarter, kQuarter); }
 
-__device__ __forceinline__ uint32_t expand_pair(uint32_t bits, uint32_t c)
+// The four ranks of each 16-bit half of w -> four pairs (rank k of the low half, of the high half), each
+// in two parts that the MMAs add up: lin = -(16 + i) / 2 and sat, -2 (lin + sat) = level + 16 + z.
+// Mask and magic number come in registers that the compiler cannot see through: one logic
+// instruction per pair, where two immediates would take two.
+struct ExpandConsts {
+    uint32_t nibble, minus_eight;
+};
+__device__ __forceinline__ uint32_t pick_rank(uint32_t x, const ExpandConsts &k)
 {
-    const uint32_t h = (bits & kNibble) | kSixteen;
-    return hfma2(hfma2_sat(h, kQuarter, c), kMinusTwo, h);
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(x), "r"(k.nibble), "r"(k.minus_eight));   // (x & b) | c
+    return d;
 }
-// The four ranks of each 16-bit half of w -> four pairs (rank k of the low half, of the high half) as
-// levels plus 16 + z.
-__device__ __forceinline__ void expand(uint32_t w, uint32_t c, uint32_t (&o)[4])
+__device__ __forceinline__ void expand(uint32_t w, uint32_t c, const ExpandConsts &k, uint32_t (&lin)[4], uint32_t (&sat)[4])
 {
     const uint32_t sw = perm(w, w, 0x2301u);         // the bytes of each half swapped
-    o[0] = expand_pair(w << 4, c);
-    o[1] = expand_pair(w, c);
-    o[2] = expand_pair(sw << 4, c);
-    o[3] = expand_pair(sw, c);
+    lin[0] = pick_rank(w << 4, k);
+    lin[1] = pick_rank(w, k);
+    lin[2] = pick_rank(sw << 4, k);
+    lin[3] = pick_rank(sw, k);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sat[i] = hfma2_sat(lin[i], kMinusHalf, c);
+}
+
+// Quotient by a number that the launch fixes: n / d for n < 2^31 (d < 2^16) by one multiplication with
+// ceil(2^(31 + s) / d), 2^s >= d.
+struct Divisor {
+    uint32_t d, mul, shift;
+    explicit Divisor(uint32_t v) : d(v), shift(0)
+    {
+        while ((1u << shift) < v) ++shift;
+        mul = (uint32_t)(((1ull << (31 + shift)) + v - 1) / v);
+    }
+    __device__ __forceinline__ int div(int n) const
+    {
+        return (int)(((unsigned long long)(uint32_t)n * mul) >> (31 + shift));
+    }
+};
+
+// 64-bit quotient that takes the 32-bit path when it can.
+__device__ __forceinline__ long long quotient(long long a, long long b)
+{
+    if (((unsigned long long)(a | b) >> 32) == 0) return (long long)((uint32_t)a / (uint32_t)b);
+    return a / b;
 }
 
 // What one launch needs beside the arguments.
@@ -155,16 +194,20 @@ struct Schedule {
     int *counters;             // [workers]
     float *partials;           // [workers][2] parts of R * (D + 2) numbers
     int min_units;             // least share of a CTA
+    int lead;                  // what an item costs beside its units, in units
+    Divisor group;             // query heads per key head
 };
 
 // One sequence's part of the work list.
 struct Seq {
     int row0, n, len;          // rows of the call, tokens
-    int first, blocks;         // blocks that any of its rows can see
+    int first, units;          // units of 32 tokens that any of its rows can see
     int tiles;                 // row tiles per key head
-    __device__ long long unit_count(int heads) const
+    // length of the work list: an item is `lead` places and then its units, at least one
+    __device__ int item_length(int lead) const { return lead + max(units, 1); }
+    __device__ long long list_length(int heads, int lead) const
     {
-        return n > 0 ? (long long)heads * tiles * max(blocks, 1) : 0;
+        return n > 0 ? (long long)heads * tiles * item_length(lead) : 0;
     }
 };
 
@@ -184,24 +227,31 @@ __device__ __forceinline__ Seq load_seq(const KvAttnArgs &a, int b, int group, S
         if (s.row0 < 0 || row1 > bt.rows || row1 < s.row0) s.n = 0;
     }
     const int lo = a.window > 0 ? max(0, s.len - s.n + 1 - a.window) : 0;
-    s.first = lo >> 4;
-    s.blocks = max(0, ((s.len + 15) >> 4) - s.first);
+    s.first = lo >> 5;
+    s.units = max(0, ((s.len + 31) >> 5) - s.first);
     s.tiles = (int)(((long long)s.n * group + R - 1) / R);
     return s;
+}
+
+// The lanes that share a row's elements.
+__device__ __forceinline__ uint32_t row_lanes(int lane, int per_row)
+{
+    return ((1u << per_row) - 1u) << (lane / per_row * per_row);
 }
 
 template <int D, int NT, int WARPS>
 struct Shape {
     static constexpr int R = 8 * NT;                       // query rows of a tile
     static constexpr int kBlockBytes = 16 * (D + 8);
-    static constexpr int kStages = D == 128 ? 6 : 10;      // copies in flight per warp
-    static constexpr int kRing = WARPS * kStages * kBlockBytes;
+    static constexpr int kUnitBytes = 2 * kBlockBytes;     // 32 tokens
+    static constexpr int kStages = D == 128 ? 3 : 5;       // units in flight per warp
+    static constexpr int kRing = WARPS * kStages * kUnitBytes;
     static constexpr int kPad = D + 4;
     static constexpr int kJoin = WARPS * R * kPad * 4;     // overlays the ring between items
     static constexpr int kBig = kRing > kJoin ? kRing : kJoin;
     static constexpr int kSmem = (kBig + WARPS * kStages * 8 + 127) / 128 * 128;
     static constexpr int kCtas = NT == 1 ? 16 / WARPS : (WARPS <= 12 ? 12 / WARPS : 1);
-    static_assert(kCtas * (kSmem + 2048) <= 232448, "shared memory of an SM");
+    static_assert(kCtas * (kSmem + 5 * 1024) <= 232448, "shared memory of an SM");
 };
 
 template <int D, int NT, int WARPS>
@@ -209,15 +259,17 @@ __global__ void __launch_bounds__(WARPS * 32, Shape<D, NT, WARPS>::kCtas)
 kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
 {
     using S = Shape<D, NT, WARPS>;
-    constexpr int R = S::R, KW = D / 32, KT = D / 16, BB = S::kBlockBytes, THREADS = WARPS * 32;
+    constexpr int R = S::R, KW = D / 32, KT = D / 16, BB = S::kBlockBytes, UB = S::kUnitBytes, THREADS = WARPS * 32, LPV = D / 8;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long warp_units[WARPS], found_off;
     __shared__ int found_b, last_part;
     __shared__ float row_m[WARPS][R], row_l[WARPS][R], tile_m[R], tile_l[R];
     __shared__ int row_hi[R], row_lo[R];
+    __shared__ __align__(16) uint32_t q_rows[R][LPV][4];
+    __shared__ float q_sum[R], q_unit[R];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const uint32_t ring = smem_addr(smem) + warp * S::kStages * BB;
-    const uint8_t *ring_ptr = smem + warp * S::kStages * BB;
+    const uint32_t ring = smem_addr(smem) + warp * S::kStages * UB;
+    const uint8_t *ring_ptr = smem + warp * S::kStages * UB;
     const uint32_t bars = smem_addr(smem) + S::kBig + warp * S::kStages * 8;
     if (lane < S::kStages) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + lane * 8) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -226,12 +278,12 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     dependent_wait();
 
     const KvBatch &bt = a.batch;
-    const int heads = a.cache.heads, group = a.q_heads / heads;
+    const int heads = a.cache.heads, group = (int)sc.group.d;
     // ---- this CTA's share of the work list ----
     const int chunk = (bt.batch + THREADS - 1) / THREADS;
     const int b_first = min(bt.batch, tid * chunk), b_last = min(bt.batch, b_first + chunk);
     long long mine = 0;
-    for (int b = b_first; b < b_last; ++b) mine += load_seq<R>(a, b, group, sc.sb).unit_count(heads);
+    for (int b = b_first; b < b_last; ++b) mine += load_seq<R>(a, b, group, sc.sb).list_length(heads, sc.lead);
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -246,13 +298,13 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         if (w < warp) incl += warp_units[w];
         total += warp_units[w];
     }
-    const long long per = max((total + gridDim.x - 1) / (long long)gridDim.x, (long long)sc.min_units);
+    const long long per = max(quotient(total + gridDim.x - 1, gridDim.x), (long long)sc.min_units);
     const long long begin = (long long)blockIdx.x * per, end = min(total, begin + per);
     if (begin >= total) return;
     if (begin >= incl - mine && begin < incl) {
         long long at = incl - mine;
         for (int b = b_first; b < b_last; ++b) {
-            const long long u = load_seq<R>(a, b, group, sc.sb).unit_count(heads);
+            const long long u = load_seq<R>(a, b, group, sc.sb).list_length(heads, sc.lead);
             if (begin < at + u) {
                 found_b = b;
                 found_off = begin - at;
@@ -266,27 +318,31 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     long long off = found_off;             // units of sequence b in front of this CTA's next one
     int stage = 0;
     uint32_t parity = 0;
-    int pending = 0;                       // requested copies that have not been waited for
     bool dead = false;                     // a copy did not arrive in time: nothing more is requested
 
     for (long long u = begin; u < end;) {
         const Seq s = load_seq<R>(a, b, group, sc.sb);
-        const long long all = s.unit_count(heads);
+        const long long all = s.list_length(heads, sc.lead);
         if (off >= all) {
             off -= all;
             ++b;
             continue;
         }
-        const int item_units = max(s.blocks, 1);
-        const int item = (int)(off / item_units), in_item = (int)(off - (long long)item * item_units);
-        const int h = item / s.tiles, tile = item - h * s.tiles;
-        const int count = (int)min((long long)(item_units - in_item), end - u);
+        const int length = s.item_length(sc.lead), item_units = length - sc.lead;
+        const int item = (int)quotient(off, length), at = (int)(off - (long long)item * length);
+        const int h = (int)quotient(item, s.tiles), tile = item - h * s.tiles;
+        // this CTA's units [in_item, in_item + count) of the item
+        const int here = (int)min((long long)(length - at), end - u);
+        const int in_item = max(at - sc.lead, 0), count = max(at + here - sc.lead, 0) - in_item;
+        const long long first_unit = u - at + sc.lead;       // the item's units on the list
+        u += here;
+        off += here;
+        if (count <= 0) continue;          // its share ends inside the item's lead
         const bool whole = count == item_units;
-        const long long item_begin = u - in_item;
 
         // rows of this tile: r = tile * R + i is row r / group of the sequence, query head r % group
-        const int rows_here = min(R, (int)((long long)s.n * group - (long long)tile * R));
-        const int i_first = tile * R / group, i_last = (tile * R + rows_here - 1) / group;
+        const int rows_here = (int)min((long long)R, (long long)s.n * group - (long long)tile * R);
+        const int i_first = sc.group.div(tile * R), i_last = sc.group.div(tile * R + rows_here - 1);
         const int pos0 = s.len - s.n;
         // a row sees [row_lo, row_hi); one in front of position 0 sees nothing
         auto hi_of = [&](int i) { return pos0 + i < 0 ? 0 : a.causal ? pos0 + i + 1 : s.len; };
@@ -294,39 +350,41 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         const int lo_min = a.window > 0 ? max(0, pos0 + i_first + 1 - a.window) : 0;
         const int lo_max = a.window > 0 ? max(0, pos0 + i_last + 1 - a.window) : 0;
         if (tid < R) {
-            const int i = (tile * R + tid) / group;
+            const int i = sc.group.div(tile * R + tid);
             const bool in = tid < rows_here;
             row_hi[tid] = in ? hi_of(i) : s.len;
             row_lo[tid] = in && a.window > 0 ? pos0 + i + 1 - a.window : 0;
         }
-        // blocks of the share that some row of the tile sees, and this warp's among them
-        const int k0 = max(s.first + in_item, lo_min >> 4);
-        const int k1 = min(s.first + min(in_item + count, s.blocks), (hi_max + 15) >> 4);
+        // units of the share that some row of the tile sees, and this warp's among them
+        const int k0 = max(s.first + in_item, lo_min >> 5);
+        const int k1 = min(s.first + min(in_item + count, s.units), (hi_max + 31) >> 5);
         const int nk = k1 > k0 + warp ? (k1 - k0 - warp + WARPS - 1) / WARPS : 0;
+        const int last_block = (s.len - 1) >> 4;
         const int32_t *table = bt.page_table + (size_t)b * bt.max_pages;
         const uint8_t *head_base = a.cache.pages + ((size_t)h << a.cache.page_shift) * (D + 8);
-        const int in_page = (1 << (a.cache.page_shift - 4)) - 1;
-        int page = 0;
-        auto load_pages = [&](int k) {       // pages of this warp's blocks k .. k + 31, one per lane
-            const int blk = k0 + warp + (k + lane) * WARPS;
-            page = 0;
-            if (blk < k1) {
-                page = __ldg(table + (blk >> (a.cache.page_shift - 4)));
-                if ((unsigned)page >= (unsigned)a.cache.num_pages) {
-                    report_failure(sc.sb, W4A8_ERR_BAD_TABLE, b);
-                    page = 0;
-                }
+        const int page_bits = a.cache.page_shift - 4, in_page = (1 << page_bits) - 1;   // in blocks
+        const size_t page_bytes = a.cache.page_bytes();
+        // byte offsets of the blocks of this warp's next 16 units: lane 2 i + j has block j of the i-th (a
+        // block behind the sequence's end: the one in front of it again)
+        size_t where = 0;
+        int requested = 0;                 // units of this item whose copies were started
+        auto look_up = [&](int k) {
+            const int blk = min(2 * (k0 + warp + (k + (lane >> 1)) * WARPS) + (lane & 1), last_block);
+            int page = __ldg(table + (blk >> page_bits));
+            if ((unsigned)page >= (unsigned)a.cache.num_pages) {
+                report_failure(sc.sb, W4A8_ERR_BAD_TABLE, b);
+                page = 0;
             }
+            where = (size_t)page * page_bytes + (size_t)(blk & in_page) * BB;
         };
-        auto request = [&](int k, int st) {  // copy this warp's block k into ring slot st
-            if ((k & 31) == 0) load_pages(k);
-            const int p = __shfl_sync(0xffffffffu, page, k & 31);
-            const int blk = k0 + warp + k * WARPS;
+        auto request = [&](int k, int st) {  // copy this warp's unit k into ring slot st
+            if ((k & 15) == 0) look_up(k);
             if (dead) return;
-            ++pending;
-            if (lane == 0)
-                copy_block(ring + st * BB, head_base + (size_t)p * a.cache.page_bytes() + (size_t)(blk & in_page) * BB, BB,
-                           bars + st * 8);
+            ++requested;
+            const size_t from = __shfl_sync(0xffffffffu, where, 2 * (k & 15) + (lane & 1));
+            if (lane == 0) expect_bytes(bars + st * 8, UB);
+            __syncwarp();
+            if (lane < 2) copy_block(ring + st * UB + lane * BB, head_base + from, BB, bars + st * 8);
         };
         {
             int st = stage;
@@ -335,69 +393,67 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 st = st + 1 == S::kStages ? 0 : st + 1;
             }
         }
-        // ---- queries: this thread's elements D/4 t .. D/4 t + D/4 - 1 of row g of every n-tile, scaled by a
-        // power of two to the top of binary16's range ----
-        uint32_t q[NT][KT][2];
-        float qsum[NT][2], unit;
-        {
-            float amax = 0.0f;
-            uint4 raw[NT][KW];
+        // ---- queries, shared by the warps: a lane takes eight elements of a row, scales them by a power of two
+        // to the top of binary16's range and leaves them as the four pairs that expand() gives of a word ----
+        for (int r = warp * (32 / LPV) + lane / LPV; r < R; r += WARPS * (32 / LPV)) {
+            const int i = sc.group.div(tile * R + r), head = h * group + tile * R + r - i * group;
+            uint4 raw = make_uint4(0u, 0u, 0u, 0u);
+            if (r < rows_here)
+                raw = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + (size_t)(s.row0 + i) * a.q_stride +
+                                                            (size_t)head * D) + lane % LPV);
+            float f[8], amax = 0.0f;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int r = tile * R + n * 8 + g;
-                const bool in = n * 8 + g < rows_here;
-                const size_t at = in ? (size_t)(s.row0 + r / group) * a.q_stride + (size_t)(h * group + r % group) * D + t * (D / 4) : 0;
-                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + at);
-#pragma unroll
-                for (int w = 0; w < KW; ++w) raw[n][w] = in ? __ldg(p + w) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-                for (int w = 0; w < KW; ++w)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t v = (&raw[n][w].x)[i] & 0x7fff7fffu;
-                        if (a.q_bf16) amax = fmaxf(amax, fmaxf(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)));
-                        else {
-                            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v));
-                            amax = fmaxf(amax, fmaxf(f.x, f.y));
-                        }
-                    }
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t v = (&raw.x)[k];
+                if (a.q_bf16) {
+                    f[2 * k] = __uint_as_float(v << 16);
+                    f[2 * k + 1] = __uint_as_float(v & 0xffff0000u);
+                } else {
+                    const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&v));
+                    f[2 * k] = x.x;
+                    f[2 * k + 1] = x.y;
+                }
+                amax = fmaxf(amax, fmaxf(fabsf(f[2 * k]), fabsf(f[2 * k + 1])));
             }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            for (int o = LPV / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(row_lanes(lane, LPV), amax, o));
             // amax * 2^-e in [2^14, 2^15); amax >= 2^-126 or 0, both factors normal
             const int e = min(max((int)((__float_as_uint(amax) >> 23) & 255u) - 127 - 14, -100), 113);
             const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-            unit = a.scale * kLog2e * __uint_as_float((uint32_t)(127 + e) << 23);
+            uint4 pairs;
+            float sum = 0.0f;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float sum = 0.0f;
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t v = pack_half2(f[k] * down, f[k + 4] * down);
+                (&pairs.x)[k] = v;
+                const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&v));
+                sum += x.x + x.y;
+            }
 #pragma unroll
-                for (int w = 0; w < KW; ++w) {
-                    float f[8];
+            for (int o = LPV / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(row_lanes(lane, LPV), sum, o);
+            *reinterpret_cast<uint4 *>(&q_rows[r][lane % LPV][0]) = pairs;
+            if (lane % LPV == 0) {
+                q_sum[r] = 0.5f * sum;
+                q_unit[r] = -2.0f * (a.scale * kLog2e) * __uint_as_float((uint32_t)(127 + e) << 23);
+            }
+        }
+        __syncthreads();                   // also row_hi, row_lo
+        uint32_t q[NT][KT][2];
+        float qsum[NT][2], unit[NT][2];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t v = (&raw[n][w].x)[i];
-                        if (a.q_bf16) {
-                            f[2 * i] = __uint_as_float(v << 16);
-                            f[2 * i + 1] = __uint_as_float(v & 0xffff0000u);
-                        } else {
-                            const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&v));
-                            f[2 * i] = x.x;
-                            f[2 * i + 1] = x.y;
-                        }
-                    }
+        for (int n = 0; n < NT; ++n) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {            // the order in which expand() gives a word's levels
-                        const uint32_t v = pack_half2(f[k] * down, f[k + 4] * down);
-                        q[n][2 * w + (k >> 1)][k & 1] = v;
-                        const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&v));
-                        sum += x.x + x.y;
-                    }
-                }
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                qsum[n][0] = -__shfl_sync(0xffffffffu, sum, 8 * t);
-                qsum[n][1] = -__shfl_sync(0xffffffffu, sum, 8 * t + 4);
+            for (int w = 0; w < KW; ++w) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(&q_rows[n * 8 + g][t * KW + w][0]);
+                q[n][2 * w][0] = v.x;
+                q[n][2 * w][1] = v.y;
+                q[n][2 * w + 1][0] = v.z;
+                q[n][2 * w + 1][1] = v.w;
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                qsum[n][j] = q_sum[n * 8 + 2 * t + j];
+                unit[n][j] = q_unit[n * 8 + 2 * t + j];
             }
         }
         float o[NT][KT][4], osum[NT][4], ref[NT][2], l[NT][2];
@@ -412,39 +468,41 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
             ref[n][0] = ref[n][1] = kNoReference;
             l[n][0] = l[n][1] = 0.0f;
         }
-        __syncthreads();                   // row_hi, row_lo
+        ExpandConsts ek = {kNibble, kMinusEight};
+        asm volatile("" : "+r"(ek.nibble), "+r"(ek.minus_eight));
         const uint32_t only_g0 = g == 0 ? 0xffffffffu : 0u;
 
         for (int k = 0; k < nk; ++k) {
             const uint32_t bar = bars + stage * 8;
-            if (pending > 0) {
-                --pending;
-                if (!try_wait(bar, parity) && !wait_slow(bar, parity)) {
+            if (k < requested) {
+                const bool ok = try_wait(bar, parity) || wait_slow(bar, parity);
+                if (!__all_sync(0xffffffffu, ok)) {
+                    if (!dead && lane == 0) report_failure(sc.sb, W4A8_ERR_TIMEOUT, kWaitSite);
                     dead = true;
-                    if (lane == 0) report_failure(sc.sb, W4A8_ERR_TIMEOUT, kWaitSite);
                 }
             }
-            dead = __any_sync(0xffffffffu, dead);
-            const uint8_t *blk = ring_ptr + stage * BB;
-            const uint32_t wk0 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 4 * g);
-            const uint32_t wk1 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 4 * g + 32);
-            const uint32_t wv0 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 64 + 4 * g);
-            const uint32_t wv1 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 64 + 4 * g + 32);
-            const uint2 wva = *reinterpret_cast<const uint2 *>(blk + 16 * D + 64 + 8 * t);
-            const uint2 wvb = *reinterpret_cast<const uint2 *>(blk + 16 * D + 64 + 8 * t + 32);
-            // ---- scores ----
-            float c[NT][4];
-            {
-                const uint32_t z0 = wk0 & 15u, z1 = wk1 & 15u;
-                const float f0 = __uint_as_float(0x41800000u | (z0 << 19)), f1 = __uint_as_float(0x41800000u | (z1 << 19));
+            const uint8_t *slot = ring_ptr + stage * UB;
+            // ---- scores: wt = the weight's exponent, before the reference is taken off ----
+            float wt[2][NT][4], inv[2][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint8_t *blk = slot + j * BB;
+                const uint32_t wk0 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 4 * g);
+                const uint32_t wk1 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 4 * g + 32);
+                const uint32_t z0 = (wk0 & 15u) * 0x00400040u + kSixteen, z1 = (wk1 & 15u) * 0x00400040u + kSixteen;
+                const uint32_t s0 = sat_constant(z0), s1 = sat_constant(z1);
+                const float f0 = __low2float(*reinterpret_cast<const __half2 *>(&z0));
+                const float f1 = __low2float(*reinterpret_cast<const __half2 *>(&z1));
+                float c[NT][4], cs[NT][4];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     c[n][0] = f0 * qsum[n][0];
                     c[n][1] = f0 * qsum[n][1];
                     c[n][2] = f1 * qsum[n][0];
                     c[n][3] = f1 * qsum[n][1];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) cs[n][i] = 0.0f;
                 }
-                const uint32_t s0 = sat_constant(offset_pair(z0 * 0x10001u)), s1 = sat_constant(offset_pair(z1 * 0x10001u));
                 uint32_t k0w[KW], k1w[KW];
                 const uint8_t *p = blk + g * (D / 2) + t * (D / 8);
                 if constexpr (KW == 4) {
@@ -458,53 +516,62 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 }
 #pragma unroll
                 for (int w = 0; w < KW; ++w) {
-                    uint32_t e0[4], e1[4];
-                    expand(k0w[w], s0, e0);
-                    expand(k1w[w], s1, e1);
+                    uint32_t l0[4], l1[4], e0[4], e1[4];
+                    expand(k0w[w], s0, ek, l0, e0);
+                    expand(k1w[w], s1, ek, l1, e1);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        mma16(c[n], e0[0], e1[0], e0[1], e1[1], q[n][2 * w][0], q[n][2 * w][1]);
-                        mma16(c[n], e0[2], e1[2], e0[3], e1[3], q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
+                        mma16(c[n], l0[0], l1[0], l0[1], l1[1], q[n][2 * w][0], q[n][2 * w][1]);
+                        mma16(cs[n], e0[0], e1[0], e0[1], e1[1], q[n][2 * w][0], q[n][2 * w][1]);
+                        mma16(c[n], l0[2], l1[2], l0[3], l1[3], q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
+                        mma16(cs[n], e0[2], e1[2], e0[3], e1[3], q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
                     }
+                }
+                const uint32_t wv0 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 64 + 4 * g);
+                const uint32_t wv1 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 64 + 4 * g + 32);
+                const float u0 = __uint_as_float(wk0 & ~15u), u1 = __uint_as_float(wk1 & ~15u);
+                const float t0 = __uint_as_float(wv0 & ~15u), t1 = __uint_as_float(wv1 & ~15u);
+                const float v0 = lg2(t0), v1 = lg2(t1);
+                inv[j][0] = rcp(t0);
+                inv[j][1] = rcp(t1);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    wt[j][n][0] = fmaf(c[n][0] + cs[n][0], u0 * unit[n][0], v0);
+                    wt[j][n][1] = fmaf(c[n][1] + cs[n][1], u0 * unit[n][1], v0);
+                    wt[j][n][2] = fmaf(c[n][2] + cs[n][2], u1 * unit[n][0], v1);
+                    wt[j][n][3] = fmaf(c[n][3] + cs[n][3], u1 * unit[n][1], v1);
+                }
+            }
+            const int j0 = (k0 + warp + k * WARPS) * 32;
+            if (j0 < lo_max || j0 + 32 > hi_min) {           // some row does not see all of the unit
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int r = n * 8 + 2 * t + (i & 1), at = j0 + 16 * j + g + (i >> 1) * 8;
+                            if (at < row_lo[r] || at >= row_hi[r]) wt[j][n][i] = -INFINITY;
+                        }
+                    // behind the sequence's end the words are anything
+                    if (j0 + 16 * j + g >= s.len) inv[j][0] = 0.0f;
+                    if (j0 + 16 * j + g + 8 >= s.len) inv[j][1] = 0.0f;
                 }
             }
             // ---- weights ----
-            const float u0 = unit * __uint_as_float(wk0 & ~15u), u1 = unit * __uint_as_float(wk1 & ~15u);
-            const float v0 = lg2(__uint_as_float(wv0 & ~15u)), v1 = lg2(__uint_as_float(wv1 & ~15u));
-            const int j0 = (k0 + warp + k * WARPS) * 16;
-            float wt[NT][4];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                c[n][0] *= u0;
-                c[n][1] *= u0;
-                c[n][2] *= u1;
-                c[n][3] *= u1;
-                wt[n][0] = c[n][0] + v0;
-                wt[n][1] = c[n][1] + v0;
-                wt[n][2] = c[n][2] + v1;
-                wt[n][3] = c[n][3] + v1;
-            }
-            if (j0 < lo_max || j0 + 16 > hi_min) {           // some row does not see all of the block
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = n * 8 + 2 * t + (i & 1), j = j0 + g + (i >> 1) * 8;
-                        if (j < row_lo[r] || j >= row_hi[r]) c[n][i] = wt[n][i] = -INFINITY;
-                    }
-            }
             bool over = false;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                over |= fmaxf(wt[n][0], wt[n][2]) > ref[n][0] + kSlack;
-                over |= fmaxf(wt[n][1], wt[n][3]) > ref[n][1] + kSlack;
+                const float a0 = fmaxf(fmaxf(wt[0][n][0], wt[0][n][2]), fmaxf(wt[1][n][0], wt[1][n][2]));
+                const float a1 = fmaxf(fmaxf(wt[0][n][1], wt[0][n][3]), fmaxf(wt[1][n][1], wt[1][n][3]));
+                over |= a0 > ref[n][0] + kSlack || a1 > ref[n][1] + kSlack;
             }
             if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        float m = fmaxf(wt[n][j], wt[n][2 + j]);
+                        float m = fmaxf(fmaxf(wt[0][n][j], wt[0][n][2 + j]), fmaxf(wt[1][n][j], wt[1][n][2 + j]));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -520,21 +587,27 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                         }
                     }
             }
-            uint32_t pb[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                l[n][0] += ex2(c[n][0] - ref[n][0]) + ex2(c[n][2] - ref[n][0]);
-                l[n][1] += ex2(c[n][1] - ref[n][1]) + ex2(c[n][3] - ref[n][1]);
-                pb[n][0] = transpose8(pack_half2(ex2(wt[n][0] - ref[n][0]), ex2(wt[n][1] - ref[n][1])));
-                pb[n][1] = transpose8(pack_half2(ex2(wt[n][2] - ref[n][0]), ex2(wt[n][3] - ref[n][1])));
-            }
             // ---- values ----
-            {
-                const uint32_t za = offset_pair((wva.x & 15u) | ((wva.y & 15u) << 16));
-                const uint32_t zb = offset_pair((wvb.x & 15u) | ((wvb.y & 15u) << 16));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t pb[NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float p0 = ex2(wt[j][n][0] - ref[n][0]), p1 = ex2(wt[j][n][1] - ref[n][1]);
+                    const float p2 = ex2(wt[j][n][2] - ref[n][0]), p3 = ex2(wt[j][n][3] - ref[n][1]);
+                    l[n][0] = fmaf(p2, inv[j][1], fmaf(p0, inv[j][0], l[n][0]));
+                    l[n][1] = fmaf(p3, inv[j][1], fmaf(p1, inv[j][0], l[n][1]));
+                    pb[n][0] = transpose8(pack_half2(p0, p1));
+                    pb[n][1] = transpose8(pack_half2(p2, p3));
+                }
+                const uint8_t *blk = slot + j * BB;
+                const uint2 wva = *reinterpret_cast<const uint2 *>(blk + 16 * D + 64 + 8 * t);
+                const uint2 wvb = *reinterpret_cast<const uint2 *>(blk + 16 * D + 64 + 8 * t + 32);
+                const uint32_t za = ((wva.y & 15u) * 0x10000u + (wva.x & 15u)) * 0x40u + kSixteen;
+                const uint32_t zb = ((wvb.y & 15u) * 0x10000u + (wvb.x & 15u)) * 0x40u + kSixteen;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) mma16(osum[n], za & only_g0, 0u, zb & only_g0, 0u, pb[n][0], pb[n][1]);
-                const uint32_t sa = sat_constant(za), sbb = sat_constant(zb);
+                const uint32_t sa = sat_constant(za), sb = sat_constant(zb);
                 constexpr int VW = D / 64;                   // words per token and slice
                 const uint8_t *p = blk + 8 * D + g * (D / 2) + t * (D / 8);
                 uint32_t xa[2][VW], xb[2][VW];               // [token of the pair][word]
@@ -551,12 +624,14 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 for (int w = 0; w < VW; ++w)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        uint32_t ea[4], eb[4];
+                        uint32_t la[4], lb[4], ea[4], eb[4];
                         const uint32_t sel = half ? 0x7632u : 0x5410u;
-                        expand(perm(xa[0][w], xa[1][w], sel), sa, ea);
-                        expand(perm(xb[0][w], xb[1][w], sel), sbb, eb);
+                        expand(perm(xa[0][w], xa[1][w], sel), sa, ek, la, ea);
+                        expand(perm(xb[0][w], xb[1][w], sel), sb, ek, lb, eb);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
+                            mma16(o[n][4 * w + 2 * half], la[0], la[1], lb[0], lb[1], pb[n][0], pb[n][1]);
+                            mma16(o[n][4 * w + 2 * half + 1], la[2], la[3], lb[2], lb[3], pb[n][0], pb[n][1]);
                             mma16(o[n][4 * w + 2 * half], ea[0], ea[1], eb[0], eb[1], pb[n][0], pb[n][1]);
                             mma16(o[n][4 * w + 2 * half + 1], ea[2], ea[3], eb[2], eb[3], pb[n][0], pb[n][1]);
                         }
@@ -600,7 +675,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
 #pragma unroll
                 for (int i = 0; i < KT; ++i)
                     *reinterpret_cast<float2 *>(to + 2 * i) =
-                        make_float2((o[n][i][j] - sum) * keep, (o[n][i][2 + j] - sum) * keep);
+                        make_float2(fmaf(-2.0f, o[n][i][j], -sum) * keep, fmaf(-2.0f, o[n][i][2 + j], -sum) * keep);
             }
         if (tid < R) {
             float m = row_m[0][tid], v = 0.0f;
@@ -615,8 +690,8 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         const int part_size = R * (D + 2);
         constexpr int kQuads = R * D / 4;
         auto write_row = [&](int r, int d, float4 v, float m, float lsum) {
-            const int i = tile * R + r;
-            const size_t at = ((size_t)(s.row0 + i / group) * a.q_heads + h * group + i % group) * D + d;
+            const int i = sc.group.div(tile * R + r);
+            const size_t at = ((size_t)(s.row0 + i) * a.q_heads + h * group + tile * R + r - i * group) * D + d;
             const float inv = lsum > 0.0f ? __fdiv_rn(1.0f, lsum) : 0.0f;
             v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
             uint2 out;
@@ -634,7 +709,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
             *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.O) + at) = out;
             if (a.lse && d == 0) a.lse[at / D] = lsum > 0.0f ? (m + lg2(lsum)) * kLn2 : -INFINITY;
         };
-        float *part = sc.partials + ((size_t)blockIdx.x * 2 + (u == begin ? 0 : 1)) * part_size;
+        float *part = sc.partials + ((size_t)blockIdx.x * 2 + (first_unit <= begin ? 0 : 1)) * part_size;
         for (int i = tid; i < kQuads; i += THREADS) {
             const int r = i / (D / 4), d = (i % (D / 4)) * 4;
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -653,13 +728,13 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
             }
             __threadfence();
             __syncthreads();
-            const int w0 = (int)(item_begin / per), w1 = (int)((item_begin + item_units - 1) / per);
+            const int w0 = (int)quotient(first_unit, per), w1 = (int)quotient(first_unit + item_units - 1, per);
             if (tid == 0) last_part = atomicAdd(sc.counters + w0, 1) == w1 - w0;
             __syncthreads();
             if (last_part) {
                 __threadfence();
                 // part of worker w: its first segment, unless the item begins inside its share
-                const bool inside = item_begin > (long long)w0 * per;
+                const bool inside = first_unit > (long long)w0 * per;
                 const float *first = sc.partials + ((size_t)w0 * 2 + (inside ? 1 : 0)) * part_size;
                 const float *rest = sc.partials + (size_t)w0 * 2 * part_size;
                 const int parts = w1 - w0 + 1;
@@ -684,8 +759,6 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 if (tid == 0) sc.counters[w0] = 0;           // ready for the next call
             }
         }
-        u += count;
-        off += count;
         // the join buffer was written by ordinary stores: order them before the next copies into the ring
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
@@ -705,8 +778,9 @@ Variant pick(const KvAttnArgs &a)
     const long long items = (long long)a.batch.batch * a.cache.heads * ((rows + 8 * v.nt - 1) / (8 * v.nt));
     // few items: every item is split over several CTAs, and wide CTAs leave fewer parts to join;
     // many: narrow CTAs, whose ends and beginnings overlap with their neighbours' streaming
-    v.warps = items >= 2 * device_sms() ? 4 : (v.nt == 1 ? 16 : 12);
-    v.ctas = device_sms() * ((v.nt == 1 ? 16 : 12) / v.warps);
+    const int per_sm = v.nt == 1 ? 16 : 12;
+    v.warps = items >= device_sms() ? 4 : per_sm / 2;
+    v.ctas = device_sms() * (per_sm / v.warps);
     return v;
 }
 
@@ -723,8 +797,8 @@ cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream
 template <int D>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, const Variant &v, cudaStream_t st)
 {
-    if (v.nt == 1) return v.warps == 4 ? launch<D, 1, 4>(a, sc, v.ctas, st) : launch<D, 1, 16>(a, sc, v.ctas, st);
-    return v.warps == 4 ? launch<D, 2, 4>(a, sc, v.ctas, st) : launch<D, 2, 12>(a, sc, v.ctas, st);
+    if (v.nt == 1) return v.warps == 4 ? launch<D, 1, 4>(a, sc, v.ctas, st) : launch<D, 1, 8>(a, sc, v.ctas, st);
+    return v.warps == 4 ? launch<D, 2, 4>(a, sc, v.ctas, st) : launch<D, 2, 6>(a, sc, v.ctas, st);
 }
 
 }  // namespace
@@ -738,11 +812,9 @@ size_t kv_attention_workspace(int, int, int, int, int D)
 cudaError_t launch_kv_attention(const KvAttnArgs &a, uint8_t *workspace, cudaStream_t st)
 {
     const Variant v = pick(a);
-    Schedule sc;
-    sc.sb = reinterpret_cast<StatusBlock *>(workspace);
-    sc.counters = reinterpret_cast<int *>(workspace + sizeof(StatusBlock));
-    sc.partials = reinterpret_cast<float *>(workspace + sizeof(StatusBlock) + counters_bytes());
-    sc.min_units = v.warps;
+    const Schedule sc = {reinterpret_cast<StatusBlock *>(workspace), reinterpret_cast<int *>(workspace + sizeof(StatusBlock)),
+                         reinterpret_cast<float *>(workspace + sizeof(StatusBlock) + counters_bytes()), v.warps, kLead,
+                         Divisor((uint32_t)(a.q_heads / a.cache.heads))};
     return a.cache.D == 64 ? launch<64>(a, sc, v, st) : launch<128>(a, sc, v, st);
 }
 
