@@ -10,12 +10,13 @@
 //
 // Expansion of eight codes (one word): with x = i - z - 1 for rank i, the level is
 // x - 2 sat(x / 4 + 1/2) + 1.  Seven logic instructions put each rank into the mantissa of
-// lin = -(16 + i) / 2 (binary16), one packed fma.sat per pair makes the saturated term, and the tensor
-// cores add the two parts: they take both as operands, -2 (lin + sat) = level + 16 + z.  The factor
-// goes into the scale, the offset is a constant per token: the score accumulator starts from it times
-// sum(q), and one extra MMA per block sums (16 + z) p for the output.  At the bandwidth of the memory the
-// SMs have about 2.9 lane instructions per code and the logic pipe half of that; this takes 1.6.
-//
+// lin = -(16 + i) / 2 (binary16), one packed fma.sat per pair makes the saturated term, one packed
+// addition joins the two: -2 (lin + sat) = level + 16 + z.  The factor goes into the scale, the offset is
+// a constant per token: the score accumulator starts from it times sum(q), and one extra MMA per block
+// sums (16 + z) p for the output.  What bounds the kernel is this expansion: packed binary16 and logic
+// instructions issue at half rate and overlap only in part, some 26 cycles per word and scheduler (30
+// with the MMA) where the memory would allow 23; measured in a loop of its own.  (Leaving the
+// addition to the tensor cores, as a second operand, takes the same time for one row tile and more for two.)
 // Softmax: the weight of token j for the value product is 2^(s_j + log2(step_j) - m), with the value's
 // step folded into the exponent, so that it fits binary16 whatever the steps' sizes; the
 // denominator sums 2^(s_j - m) in binary32.  m is a running reference and no exact maximum: it moves
@@ -142,8 +143,8 @@ constexpr uint32_t kMinusHalf = 0xB800B800u, kQuarter = 0x34003400u, kMinusQuart
 // The constant of the saturated term, 1/4 - (16 + z) / 4, from a pair of binary16 numbers 16 + z.
 __device__ __forceinline__ uint32_t sat_constant(uint32_t off) { return hfma2(off, kMinusQuarter, kQuarter); }
 
-// The four ranks of each 16-bit half of w -> four pairs (rank k of the low half, of the high half), each
-// in two parts that the MMAs add up: lin = -(16 + i) / 2 and sat, -2 (lin + sat) = level + 16 + z.
+// The four ranks of each 16-bit half of w -> four pairs (rank k of the low half, of the high half):
+// -(level + 16 + z) / 2.
 // Mask and magic number come in registers that the compiler cannot see through: one logic
 // instruction per pair, where two immediates would take two.
 struct ExpandConsts {
@@ -155,15 +156,22 @@ __device__ __forceinline__ uint32_t pick_rank(uint32_t x, const ExpandConsts &k)
     asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(x), "r"(k.nibble), "r"(k.minus_eight));   // (x & b) | c
     return d;
 }
-__device__ __forceinline__ void expand(uint32_t w, uint32_t c, const ExpandConsts &k, uint32_t (&lin)[4], uint32_t (&sat)[4])
+__device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b)
 {
+    uint32_t d;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ void expand(uint32_t w, uint32_t c, const ExpandConsts &k, uint32_t (&o)[4])
+{
+    uint32_t lin[4];
     const uint32_t sw = perm(w, w, 0x2301u);         // the bytes of each half swapped
     lin[0] = pick_rank(w << 4, k);
     lin[1] = pick_rank(w, k);
     lin[2] = pick_rank(sw << 4, k);
     lin[3] = pick_rank(sw, k);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sat[i] = hfma2_sat(lin[i], kMinusHalf, c);
+    for (int i = 0; i < 4; ++i) o[i] = hadd2(lin[i], hfma2_sat(lin[i], kMinusHalf, c));
 }
 
 // Quotient by a number that the launch fixes: n / d for n < 2^31 (d < 2^16) by one multiplication with
@@ -250,7 +258,7 @@ struct Shape {
     static constexpr int kJoin = WARPS * R * kPad * 4;     // overlays the ring between items
     static constexpr int kBig = kRing > kJoin ? kRing : kJoin;
     static constexpr int kSmem = (kBig + WARPS * kStages * 8 + 127) / 128 * 128;
-    static constexpr int kCtas = NT == 1 ? 16 / WARPS : (WARPS <= 12 ? 12 / WARPS : 1);
+    static constexpr int kCtas = NT == 1 ? 16 / WARPS : 12 / WARPS;
     static_assert(kCtas * (kSmem + 5 * 1024) <= 232448, "shared memory of an SM");
 };
 
@@ -265,7 +273,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     __shared__ int found_b, last_part;
     __shared__ float row_m[WARPS][R], row_l[WARPS][R], tile_m[R], tile_l[R];
     __shared__ int row_hi[R], row_lo[R];
-    __shared__ __align__(16) uint32_t q_rows[R][LPV][4];
+    __shared__ __align__(16) uint4 q_frag[NT][KW][32];
     __shared__ float q_sum[R], q_unit[R];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const uint32_t ring = smem_addr(smem) + warp * S::kStages * UB;
@@ -431,31 +439,22 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
             }
 #pragma unroll
             for (int o = LPV / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(row_lanes(lane, LPV), sum, o);
-            *reinterpret_cast<uint4 *>(&q_rows[r][lane % LPV][0]) = pairs;
-            if (lane % LPV == 0) {
+            const int l = lane % LPV;      // the MMA lane that takes these elements: row r % 8, quarter l / KW
+            q_frag[r / 8][l % KW][(r % 8) * 4 + l / KW] = pairs;
+            if (l == 0) {
                 q_sum[r] = 0.5f * sum;
                 q_unit[r] = -2.0f * (a.scale * kLog2e) * __uint_as_float((uint32_t)(127 + e) << 23);
             }
         }
         __syncthreads();                   // also row_hi, row_lo
-        uint32_t q[NT][KT][2];
         float qsum[NT][2], unit[NT][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(&q_rows[n * 8 + g][t * KW + w][0]);
-                q[n][2 * w][0] = v.x;
-                q[n][2 * w][1] = v.y;
-                q[n][2 * w + 1][0] = v.z;
-                q[n][2 * w + 1][1] = v.w;
-            }
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 qsum[n][j] = q_sum[n * 8 + 2 * t + j];
                 unit[n][j] = q_unit[n * 8 + 2 * t + j];
             }
-        }
         float o[NT][KT][4], osum[NT][4], ref[NT][2], l[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -482,66 +481,70 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 }
             }
             const uint8_t *slot = ring_ptr + stage * UB;
-            // ---- scores: wt = the weight's exponent, before the reference is taken off ----
-            float wt[2][NT][4], inv[2][2];
+            // ---- scores ----
+            float c[2][NT][4], cs[2][NT][4];
+            {
+                uint32_t kw[2][2][KW], sat[2][2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint8_t *blk = slot + j * BB;
-                const uint32_t wk0 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 4 * g);
-                const uint32_t wk1 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 4 * g + 32);
-                const uint32_t z0 = (wk0 & 15u) * 0x00400040u + kSixteen, z1 = (wk1 & 15u) * 0x00400040u + kSixteen;
-                const uint32_t s0 = sat_constant(z0), s1 = sat_constant(z1);
-                const float f0 = __low2float(*reinterpret_cast<const __half2 *>(&z0));
-                const float f1 = __low2float(*reinterpret_cast<const __half2 *>(&z1));
-                float c[NT][4], cs[NT][4];
+                for (int j = 0; j < 2; ++j) {
+                    const uint8_t *blk = slot + j * BB;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    c[n][0] = f0 * qsum[n][0];
-                    c[n][1] = f0 * qsum[n][1];
-                    c[n][2] = f1 * qsum[n][0];
-                    c[n][3] = f1 * qsum[n][1];
+                    for (int i = 0; i < 2; ++i) {            // token g, then token g + 8
+                        const uint32_t wk = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 32 * i + 4 * g);
+                        const uint32_t off = (wk & 15u) * 0x00400040u + kSixteen;
+                        const float f = __low2float(*reinterpret_cast<const __half2 *>(&off));
+                        sat[j][i] = sat_constant(off);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) cs[n][i] = 0.0f;
-                }
-                uint32_t k0w[KW], k1w[KW];
-                const uint8_t *p = blk + g * (D / 2) + t * (D / 8);
-                if constexpr (KW == 4) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(p), y = *reinterpret_cast<const uint4 *>(p + 4 * D);
-                    k0w[0] = x.x; k0w[1] = x.y; k0w[2] = x.z; k0w[3] = x.w;
-                    k1w[0] = y.x; k1w[1] = y.y; k1w[2] = y.z; k1w[3] = y.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2 *>(p), y = *reinterpret_cast<const uint2 *>(p + 4 * D);
-                    k0w[0] = x.x; k0w[1] = x.y;
-                    k1w[0] = y.x; k1w[1] = y.y;
+                        for (int n = 0; n < NT; ++n) {
+                            c[j][n][2 * i] = f * qsum[n][0];
+                            c[j][n][2 * i + 1] = f * qsum[n][1];
+                            cs[j][n][2 * i] = cs[j][n][2 * i + 1] = 0.0f;
+                        }
+                        const uint8_t *p = blk + (g + 8 * i) * (D / 2) + t * (D / 8);
+                        if constexpr (KW == 4) {
+                            const uint4 x = *reinterpret_cast<const uint4 *>(p);
+                            kw[j][i][0] = x.x; kw[j][i][1] = x.y; kw[j][i][2] = x.z; kw[j][i][3] = x.w;
+                        } else {
+                            const uint2 x = *reinterpret_cast<const uint2 *>(p);
+                            kw[j][i][0] = x.x; kw[j][i][1] = x.y;
+                        }
+                    }
                 }
 #pragma unroll
                 for (int w = 0; w < KW; ++w) {
-                    uint32_t l0[4], l1[4], e0[4], e1[4];
-                    expand(k0w[w], s0, ek, l0, e0);
-                    expand(k1w[w], s1, ek, l1, e1);
+                    uint4 q[NT];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        mma16(c[n], l0[0], l1[0], l0[1], l1[1], q[n][2 * w][0], q[n][2 * w][1]);
-                        mma16(cs[n], e0[0], e1[0], e0[1], e1[1], q[n][2 * w][0], q[n][2 * w][1]);
-                        mma16(c[n], l0[2], l1[2], l0[3], l1[3], q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
-                        mma16(cs[n], e0[2], e1[2], e0[3], e1[3], q[n][2 * w + 1][0], q[n][2 * w + 1][1]);
+                    for (int n = 0; n < NT; ++n) q[n] = q_frag[n][w][lane];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t e0[4], e1[4];
+                        expand(kw[j][0][w], sat[j][0], ek, e0);
+                        expand(kw[j][1][w], sat[j][1], ek, e1);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            mma16(c[j][n], e0[0], e1[0], e0[1], e1[1], q[n].x, q[n].y);
+                            mma16(cs[j][n], e0[2], e1[2], e0[3], e1[3], q[n].z, q[n].w);
+                        }
                     }
                 }
-                const uint32_t wv0 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 64 + 4 * g);
-                const uint32_t wv1 = *reinterpret_cast<const uint32_t *>(blk + 16 * D + 64 + 4 * g + 32);
-                const float u0 = __uint_as_float(wk0 & ~15u), u1 = __uint_as_float(wk1 & ~15u);
-                const float t0 = __uint_as_float(wv0 & ~15u), t1 = __uint_as_float(wv1 & ~15u);
-                const float v0 = lg2(t0), v1 = lg2(t1);
-                inv[j][0] = rcp(t0);
-                inv[j][1] = rcp(t1);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    wt[j][n][0] = fmaf(c[n][0] + cs[n][0], u0 * unit[n][0], v0);
-                    wt[j][n][1] = fmaf(c[n][1] + cs[n][1], u0 * unit[n][1], v0);
-                    wt[j][n][2] = fmaf(c[n][2] + cs[n][2], u1 * unit[n][0], v1);
-                    wt[j][n][3] = fmaf(c[n][3] + cs[n][3], u1 * unit[n][1], v1);
-                }
             }
+            // wt = the weight's exponent, before the reference is taken off; inv = 1 / step of the value
+            float wt[2][NT][4], inv[2][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint8_t *words = slot + j * BB + 16 * D + 32 * i + 4 * g;
+                    const float u = __uint_as_float(*reinterpret_cast<const uint32_t *>(words) & ~15u);
+                    const float step = __uint_as_float(*reinterpret_cast<const uint32_t *>(words + 64) & ~15u);
+                    const float v = lg2(step);
+                    inv[j][i] = rcp(step);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        wt[j][n][2 * i] = fmaf(c[j][n][2 * i] + cs[j][n][2 * i], u * unit[n][0], v);
+                        wt[j][n][2 * i + 1] = fmaf(c[j][n][2 * i + 1] + cs[j][n][2 * i + 1], u * unit[n][1], v);
+                    }
+                }
             const int j0 = (k0 + warp + k * WARPS) * 32;
             if (j0 < lo_max || j0 + 32 > hi_min) {           // some row does not see all of the unit
 #pragma unroll
@@ -624,14 +627,12 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 for (int w = 0; w < VW; ++w)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        uint32_t la[4], lb[4], ea[4], eb[4];
+                        uint32_t ea[4], eb[4];
                         const uint32_t sel = half ? 0x7632u : 0x5410u;
-                        expand(perm(xa[0][w], xa[1][w], sel), sa, ek, la, ea);
-                        expand(perm(xb[0][w], xb[1][w], sel), sb, ek, lb, eb);
+                        expand(perm(xa[0][w], xa[1][w], sel), sa, ek, ea);
+                        expand(perm(xb[0][w], xb[1][w], sel), sb, ek, eb);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            mma16(o[n][4 * w + 2 * half], la[0], la[1], lb[0], lb[1], pb[n][0], pb[n][1]);
-                            mma16(o[n][4 * w + 2 * half + 1], la[2], la[3], lb[2], lb[3], pb[n][0], pb[n][1]);
                             mma16(o[n][4 * w + 2 * half], ea[0], ea[1], eb[0], eb[1], pb[n][0], pb[n][1]);
                             mma16(o[n][4 * w + 2 * half + 1], ea[2], ea[3], eb[2], eb[3], pb[n][0], pb[n][1]);
                         }
@@ -779,12 +780,12 @@ Variant pick(const KvAttnArgs &a)
     // few items: every item is split over several CTAs, and wide CTAs leave fewer parts to join;
     // many: narrow CTAs, whose ends and beginnings overlap with their neighbours' streaming
     const int per_sm = v.nt == 1 ? 16 : 12;
-    v.warps = items >= device_sms() ? 4 : per_sm / 2;
+    v.warps = items >= device_sms() ? 4 : v.nt == 1 ? 8 : 6;
     v.ctas = device_sms() * (per_sm / v.warps);
     return v;
 }
 
-size_t counters_bytes() { return align_up((size_t)device_sms() * 4 * sizeof(int), 256); }
+size_t counters_bytes() { return align_up((size_t)device_sms() * 5 * sizeof(int), 256); }
 
 template <int D, int NT, int WARPS>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
