@@ -151,8 +151,11 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream      # current_stream().cuda_stream at a thirtieth of its cost
+
+
 def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
 
 
 def _check(status: int, what: str):
@@ -254,28 +257,32 @@ def norm_quantize_act(X, norm_weight, norm_bias=None, kind: int = NORM_RMS, eps:
 
 
 _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+_DTYPES16 = (torch.float16, torch.bfloat16)
 
 
-def _here(what, first, *others):
-    """The tensors live on the current device: the library launches on that device's stream."""
-    at = first.device
-    if at.index != torch.cuda.current_device():
-        raise ValueError(f"{what}: tensors on {at}, current device is cuda:{torch.cuda.current_device()}")
-    for t in others:
-        if t is not None and t.device != at:
-            raise ValueError(f"{what}: tensors on {at} and {t.device}")
+def _here(what, *tensors):
+    """The stream of the current device, on which all the tensors live: the library launches there."""
+    at = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"{what}: tensor on {t.device}, current device is cuda:{at}")
+    return _raw_stream(at)
 
 
 def _is(t, shape, what):
-    if t is not None and tuple(t.shape) != shape:
+    if t is not None and t.shape != shape:
         raise ValueError(f"{what}: expected shape {shape}, got {tuple(t.shape)}")
     return t
 
 
 def _dev16(t, what, contiguous=True):
-    if not t.is_cuda or t.dtype not in (torch.float16, torch.bfloat16) or (contiguous and not t.is_contiguous()):
+    if not t.is_cuda or t.dtype not in _DTYPES16 or (contiguous and not t.is_contiguous()):
         raise TypeError(f"{what}: expected a CUDA tensor of float16 or bfloat16{', contiguous' if contiguous else ''}")
     return t
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def add_norm_quantize_act(X, residual, norm_weight, norm_bias=None, kind: int = NORM_RMS, eps: float = 1e-5,
@@ -291,19 +298,21 @@ def add_norm_quantize_act(X, residual, norm_weight, norm_bias=None, kind: int = 
     norm_weight = _dev(norm_weight, torch.float32, "norm_weight")
     norm_bias = _dev(norm_bias, torch.float32, "norm_bias")
     M, K = X.shape
-    _is(residual, (M, K), "residual")
+    _is(residual, X.shape, "residual")
     _is(norm_weight, (K,), "norm_weight")
     _is(norm_bias, (K,), "norm_bias")
-    residual_out = torch.empty_like(residual) if residual_out is None else _is(
-        _dev(residual_out, residual.dtype, "residual_out"), (M, K), "residual_out")
+    if residual_out is None:
+        residual_out = torch.empty_like(residual)
+    else:
+        _is(_dev(residual_out, residual.dtype, "residual_out"), X.shape, "residual_out")
     if out is None:
-        out = (torch.empty((M, K), dtype=torch.int8, device=X.device),
-               torch.empty((M,), dtype=torch.float32, device=X.device))
-    Xq, tok = _is(_dev(out[0], torch.int8, "Xq"), (M, K), "Xq"), _is(_dev(out[1], torch.float32, "tok_scale"), (M,), "tok_scale")
-    _here("add_norm_quantize_act", X, residual, norm_weight, norm_bias, residual_out, Xq, tok)
+        Xq, tok = torch.empty_like(X, dtype=torch.int8), X.new_empty(M, dtype=torch.float32)
+    else:
+        Xq, tok = _is(_dev(out[0], torch.int8, "Xq"), X.shape, "Xq"), _is(_dev(out[1], torch.float32, "tok_scale"), (M,), "tok_scale")
+    stream = _here("add_norm_quantize_act", X, residual, norm_weight, norm_bias, residual_out, Xq, tok)
     _check(lib.w4a8_add_norm_quantize_act(
         X.data_ptr(), _DTYPES[X.dtype], residual.data_ptr(), _DTYPES[residual.dtype], residual_out.data_ptr(),
-        norm_weight.data_ptr(), _ptr(norm_bias), kind, eps, M, K, Xq.data_ptr(), tok.data_ptr(), _stream()),
+        norm_weight.data_ptr(), _at(norm_bias), kind, eps, M, K, Xq.data_ptr(), tok.data_ptr(), stream),
         "w4a8_add_norm_quantize_act")
     return Xq, tok, residual_out
 
@@ -543,22 +552,24 @@ def new_kv_workspace(rows: int, batch: int, q_heads: int, kv_heads: int, head_di
     return ws
 
 
-def _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, head_dim, rows, workspace, what, *tensors):
-    """Checks of the arguments that the cache calls share: (num_pages, page_size, max_pages, batch)."""
+def _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, head_dim, workspace, what, *tensors):
+    """Checks of the arguments that the cache calls share, and those arguments in the library's order:
+    (cache .. kv_heads, D, page table .. batch), workspace and stream."""
     _dev(cache, torch.uint8, "cache")
     _dev(page_table, torch.int32, "page_table")
     _dev(kv_lens, torch.int32, "kv_lens")
-    _dev(cu_rows, torch.int32, "cu_rows")
     _dev(workspace, torch.uint8, "workspace")
     batch, max_pages = page_table.shape
     _is(kv_lens, (batch,), "kv_lens")
-    _is(cu_rows, (batch + 1,), "cu_rows")
+    if cu_rows is not None:
+        _is(_dev(cu_rows, torch.int32, "cu_rows"), (batch + 1,), "cu_rows")
     num_pages, nbytes = cache.shape
-    page_size = nbytes // (kv_heads * (head_dim + 8)) if kv_heads > 0 else 0
-    if nbytes != kv_page_bytes(page_size, kv_heads, head_dim):
+    slot = kv_heads * (head_dim + 8)                   # bytes of a token, all heads
+    if slot <= 0 or nbytes % slot or nbytes != lib.w4a8_kv_page_bytes(nbytes // slot, kv_heads, head_dim):
         raise ValueError(f"{what}: pages of {nbytes} bytes do not hold {kv_heads} heads of {head_dim}")
-    _here(what, cache, page_table, kv_lens, cu_rows, workspace, *tensors)
-    return num_pages, page_size, max_pages, batch
+    stream = _here(what, cache, page_table, kv_lens, cu_rows, workspace, *tensors)
+    return ((cache.data_ptr(), num_pages, nbytes // slot, kv_heads, head_dim, page_table.data_ptr(), max_pages, kv_lens.data_ptr(),
+             _at(cu_rows), batch), (workspace.data_ptr(), workspace.numel(), stream))
 
 
 def _rows_of(t, what):
@@ -578,11 +589,9 @@ def kv_append(K, V, cache, page_table, kv_lens, workspace, cu_rows=None):
     rows, kv_heads, D = K.shape
     if V.dtype != K.dtype:
         raise TypeError("V: expected the type of K")
-    _is(V, (rows, kv_heads, D), "V")
-    n, P, mp, batch = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, D, rows, workspace, "kv_append", K, V)
-    _check(lib.w4a8_kv_append(K.data_ptr(), V.data_ptr(), _DTYPES[K.dtype], ks, vs, cache.data_ptr(), n, P,
-                              kv_heads, D, page_table.data_ptr(), mp, kv_lens.data_ptr(), _ptr(cu_rows), batch,
-                              rows, workspace.data_ptr(), workspace.numel(), _stream()), "w4a8_kv_append")
+    _is(V, K.shape, "V")
+    batch, tail = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, D, workspace, "kv_append", K, V)
+    _check(lib.w4a8_kv_append(K.data_ptr(), V.data_ptr(), _DTYPES[K.dtype], ks, vs, *batch, rows, *tail), "w4a8_kv_append")
 
 
 def kv_read(cache, page_table, kv_lens, rows: int, kv_heads: int, head_dim: int, workspace, cu_rows=None,
@@ -590,15 +599,15 @@ def kv_read(cache, page_table, kv_lens, rows: int, kv_heads: int, head_dim: int,
     """Reads the keys and values of `rows` rows (numbered as in kv_append) back:
     (K, V) [rows, kv_heads, D] of `dtype`."""
     if out is None:
-        out = (torch.empty((rows, kv_heads, head_dim), dtype=dtype, device=cache.device),
-               torch.empty((rows, kv_heads, head_dim), dtype=dtype, device=cache.device))
-    K, V = (_is(_dev16(t, "out"), (rows, kv_heads, head_dim), "out") for t in out)
-    if K.dtype != V.dtype:
+        K = torch.empty((rows, kv_heads, head_dim), dtype=dtype, device=cache.device)
+        V = torch.empty_like(K)
+    else:
+        K, V = (_is(t, (rows, kv_heads, head_dim), "out") for t in out)
+    _dev16(K, "K")
+    if _dev16(V, "V").dtype != K.dtype:
         raise TypeError("out: expected two tensors of one type")
-    n, P, mp, batch = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, head_dim, rows, workspace, "kv_read", K, V)
-    _check(lib.w4a8_kv_read(cache.data_ptr(), n, P, kv_heads, head_dim, page_table.data_ptr(), mp,
-                            kv_lens.data_ptr(), _ptr(cu_rows), batch, rows, K.data_ptr(), V.data_ptr(),
-                            _DTYPES[K.dtype], workspace.data_ptr(), workspace.numel(), _stream()), "w4a8_kv_read")
+    batch, tail = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, head_dim, workspace, "kv_read", K, V)
+    _check(lib.w4a8_kv_read(*batch, rows, K.data_ptr(), V.data_ptr(), _DTYPES[K.dtype], *tail), "w4a8_kv_read")
     return K, V
 
 
@@ -611,14 +620,14 @@ def kv_attention(Q, cache, page_table, kv_lens, kv_heads: int, workspace, cu_row
     rows, q_heads, D = Q.shape
     if out is None:
         out = torch.empty((rows, q_heads, D), dtype=dtype, device=Q.device)
-    _is(_dev16(out, "out"), (rows, q_heads, D), "out")
-    _is(_dev(lse, torch.float32, "lse"), (rows, q_heads), "lse")
-    n, P, mp, batch = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, D, rows, workspace, "kv_attention", Q, out, lse)
-    _check(lib.w4a8_kv_attention(
-        Q.data_ptr(), _DTYPES[Q.dtype], qs, cache.data_ptr(), n, P, kv_heads, D, page_table.data_ptr(), mp,
-        kv_lens.data_ptr(), _ptr(cu_rows), batch, rows, q_heads, D ** -0.5 if scale is None else scale,
-        int(causal), window, out.data_ptr(), _DTYPES[out.dtype], _ptr(lse), workspace.data_ptr(),
-        workspace.numel(), _stream()), "w4a8_kv_attention")
+    else:
+        _is(out, Q.shape, "out")
+    _dev16(out, "out")
+    if lse is not None:
+        _is(_dev(lse, torch.float32, "lse"), (rows, q_heads), "lse")
+    batch, tail = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, D, workspace, "kv_attention", Q, out, lse)
+    _check(lib.w4a8_kv_attention(Q.data_ptr(), _DTYPES[Q.dtype], qs, *batch, rows, q_heads, D ** -0.5 if scale is None else scale,
+                                 int(causal), window, out.data_ptr(), _DTYPES[out.dtype], _at(lse), *tail), "w4a8_kv_attention")
     return out
 
 
