@@ -20,7 +20,7 @@
 // Softmax: the weight of token j for the value product is 2^(s_j + log2(step_j) - m), with the value's
 // step folded into the exponent, so that it fits binary16 whatever the steps' sizes; the
 // denominator sums 2^(s_j - m) in binary32.  m is a running reference and no exact maximum: it moves
-// only when a weight would exceed 2^8 (one vote per 32 tokens instead of a reduction).
+// only when a weight would exceed 2^15 (one vote per 32 tokens instead of a reduction).
 //
 // Schedule: the blocks of all (sequence, key head, row tile) items form one list, which the
 // CTAs share evenly whatever the lengths are (every CTA computes the list's prefix sums from the
@@ -28,46 +28,17 @@
 // workspace and the last of them to finish joins all parts in list order, so the result does not
 // depend on who is last.  Inside a CTA the warps take blocks in turn, each with its own ring of
 // bulk copies.
-#include "kv_cache.cuh"
+#include <atomic>
+
+#include "kv_attention.cuh"
 
 namespace w4a8 {
 
 namespace {
 
-constexpr unsigned long long kWaitNs = 2000000000ull;      // limit of every bounded wait
-constexpr uint32_t kSuspendHintNs = 1000;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kNoReference = -1.0e30f;
-constexpr float kSlack = 8.0f;                             // weights stay below 2^8
 constexpr int kWaitSite = 900;
 constexpr int kLead = 8;                                   // an item's fixed cost, in units of 32 tokens
 
-__device__ __forceinline__ uint32_t smem_addr(const void *p)
-{
-    return (uint32_t)__cvta_generic_to_shared(p);
-}
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity), "r"(kSuspendHintNs)
-        : "memory");
-    return ok != 0;
-}
-__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity)
-{
-    unsigned long long t0, t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
-    do {
-        if (try_wait(bar, parity)) return true;
-        asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    } while (t - t0 < kWaitNs);
-    return false;
-}
 __device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -79,47 +50,11 @@ __device__ __forceinline__ void copy_block(uint32_t dst, const uint8_t *src, uin
                  : "memory");
 }
 
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float lg2(float x)
-{
-    float y;
-    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ float rcp(float x)
 {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-__device__ __forceinline__ uint32_t perm(uint32_t a, uint32_t b, uint32_t sel)
-{
-    uint32_t d;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
-    return d;
-}
-__device__ __forceinline__ uint32_t hfma2_sat(uint32_t a, uint32_t b, uint32_t c)
-{
-    uint32_t d;
-    asm("fma.rn.sat.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-}
-__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c)
-{
-    uint32_t d;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-}
-__device__ __forceinline__ uint32_t pack_half2(float a, float b)
-{
-    uint32_t d;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
-    return d;
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t v)
 {
@@ -136,66 +71,6 @@ __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t a0, const ui
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-constexpr uint32_t kNibble = 0x03C003C0u;    // bits 6-9 of both halves
-constexpr uint32_t kMinusEight = 0xC800C800u, kSixteen = 0x4C004C00u;
-constexpr uint32_t kMinusHalf = 0xB800B800u, kQuarter = 0x34003400u, kMinusQuarter = 0xB400B400u;
-
-// The constant of the saturated term, 1/4 - (16 + z) / 4, from a pair of binary16 numbers 16 + z.
-__device__ __forceinline__ uint32_t sat_constant(uint32_t off) { return hfma2(off, kMinusQuarter, kQuarter); }
-
-// The four ranks of each 16-bit half of w -> four pairs (rank k of the low half, of the high half):
-// -(level + 16 + z) / 2.
-// Mask and magic number come in registers that the compiler cannot see through: one logic
-// instruction per pair, where two immediates would take two.
-struct ExpandConsts {
-    uint32_t nibble, minus_eight;
-};
-__device__ __forceinline__ uint32_t pick_rank(uint32_t x, const ExpandConsts &k)
-{
-    uint32_t d;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(x), "r"(k.nibble), "r"(k.minus_eight));   // (x & b) | c
-    return d;
-}
-__device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b)
-{
-    uint32_t d;
-    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ void expand(uint32_t w, uint32_t c, const ExpandConsts &k, uint32_t (&o)[4])
-{
-    uint32_t lin[4];
-    const uint32_t sw = perm(w, w, 0x2301u);         // the bytes of each half swapped
-    lin[0] = pick_rank(w << 4, k);
-    lin[1] = pick_rank(w, k);
-    lin[2] = pick_rank(sw << 4, k);
-    lin[3] = pick_rank(sw, k);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = hadd2(lin[i], hfma2_sat(lin[i], kMinusHalf, c));
-}
-
-// Quotient by a number that the launch fixes: n / d for n < 2^31 (d < 2^16) by one multiplication with
-// ceil(2^(31 + s) / d), 2^s >= d.
-struct Divisor {
-    uint32_t d, mul, shift;
-    explicit Divisor(uint32_t v) : d(v), shift(0)
-    {
-        while ((1u << shift) < v) ++shift;
-        mul = (uint32_t)(((1ull << (31 + shift)) + v - 1) / v);
-    }
-    __device__ __forceinline__ int div(int n) const
-    {
-        return (int)(((unsigned long long)(uint32_t)n * mul) >> (31 + shift));
-    }
-};
-
-// 64-bit quotient that takes the 32-bit path when it can.
-__device__ __forceinline__ long long quotient(long long a, long long b)
-{
-    if (((unsigned long long)(a | b) >> 32) == 0) return (long long)((uint32_t)a / (uint32_t)b);
-    return a / b;
-}
-
 // What one launch needs beside the arguments.
 struct Schedule {
     StatusBlock *sb;
@@ -207,8 +82,7 @@ struct Schedule {
 };
 
 // One sequence's part of the work list.
-struct Seq {
-    int row0, n, len;          // rows of the call, tokens
+struct Part : Seq {
     int first, units;          // units of 32 tokens that any of its rows can see
     int tiles;                 // row tiles per key head
     // length of the work list: an item is `lead` places and then its units, at least one
@@ -220,22 +94,11 @@ struct Seq {
 };
 
 template <int R>
-__device__ __forceinline__ Seq load_seq(const KvAttnArgs &a, int b, int group, StatusBlock *sb)
+__device__ __forceinline__ Part load_part(const KvAttnArgs &a, int b, int group, StatusBlock *sb)
 {
-    const KvBatch &bt = a.batch;
-    Seq s;
-    s.len = __ldg(bt.kv_lens + b);
-    s.row0 = bt.cu_rows ? __ldg(bt.cu_rows + b) : b;
-    const int row1 = bt.cu_rows ? __ldg(bt.cu_rows + b + 1) : b + 1;
-    s.n = row1 - s.row0;
-    const int most = bt.max_pages << a.cache.page_shift;
-    if (s.len < 0 || s.len > most || s.row0 < 0 || row1 > bt.rows || row1 < s.row0) {
-        report_failure(sb, W4A8_ERR_BAD_TABLE, b);
-        s.len = min(max(s.len, 0), most);
-        if (s.row0 < 0 || row1 > bt.rows || row1 < s.row0) s.n = 0;
-    }
-    const int lo = a.window > 0 ? max(0, s.len - s.n + 1 - a.window) : 0;
-    s.first = lo >> 5;
+    Part s;
+    static_cast<Seq &>(s) = load_seq(a, b, sb);
+    s.first = Sight(a, s).lo(0) >> 5;
     s.units = max(0, ((s.len + 31) >> 5) - s.first);
     s.tiles = (int)(((long long)s.n * group + R - 1) / R);
     return s;
@@ -291,7 +154,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     const int chunk = (bt.batch + THREADS - 1) / THREADS;
     const int b_first = min(bt.batch, tid * chunk), b_last = min(bt.batch, b_first + chunk);
     long long mine = 0;
-    for (int b = b_first; b < b_last; ++b) mine += load_seq<R>(a, b, group, sc.sb).list_length(heads, sc.lead);
+    for (int b = b_first; b < b_last; ++b) mine += load_part<R>(a, b, group, sc.sb).list_length(heads, sc.lead);
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -312,7 +175,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     if (begin >= incl - mine && begin < incl) {
         long long at = incl - mine;
         for (int b = b_first; b < b_last; ++b) {
-            const long long u = load_seq<R>(a, b, group, sc.sb).list_length(heads, sc.lead);
+            const long long u = load_part<R>(a, b, group, sc.sb).list_length(heads, sc.lead);
             if (begin < at + u) {
                 found_b = b;
                 found_off = begin - at;
@@ -329,7 +192,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     bool dead = false;                     // a copy did not arrive in time: nothing more is requested
 
     for (long long u = begin; u < end;) {
-        const Seq s = load_seq<R>(a, b, group, sc.sb);
+        const Part s = load_part<R>(a, b, group, sc.sb);
         const long long all = s.list_length(heads, sc.lead);
         if (off >= all) {
             off -= all;
@@ -351,17 +214,13 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         // rows of this tile: r = tile * R + i is row r / group of the sequence, query head r % group
         const int rows_here = (int)min((long long)R, (long long)s.n * group - (long long)tile * R);
         const int i_first = sc.group.div(tile * R), i_last = sc.group.div(tile * R + rows_here - 1);
-        const int pos0 = s.len - s.n;
-        // a row sees [row_lo, row_hi); one in front of position 0 sees nothing
-        auto hi_of = [&](int i) { return pos0 + i < 0 ? 0 : a.causal ? pos0 + i + 1 : s.len; };
-        const int hi_max = hi_of(i_last), hi_min = hi_of(i_first);
-        const int lo_min = a.window > 0 ? max(0, pos0 + i_first + 1 - a.window) : 0;
-        const int lo_max = a.window > 0 ? max(0, pos0 + i_last + 1 - a.window) : 0;
+        const Sight sight(a, s);
+        const int hi_max = sight.hi(i_last), hi_min = sight.hi(i_first);
+        const int lo_min = sight.lo(i_first), lo_max = sight.lo(i_last);
         if (tid < R) {
             const int i = sc.group.div(tile * R + tid);
-            const bool in = tid < rows_here;
-            row_hi[tid] = in ? hi_of(i) : s.len;
-            row_lo[tid] = in && a.window > 0 ? pos0 + i + 1 - a.window : 0;
+            row_hi[tid] = tid < rows_here ? sight.hi(i) : s.len;
+            row_lo[tid] = tid < rows_here ? sight.lo(i) : 0;
         }
         // units of the share that some row of the tile sees, and this warp's among them
         const int k0 = max(s.first + in_item, lo_min >> 5);
@@ -770,7 +629,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
 struct Variant {
     int nt, warps, ctas;
 };
-Variant pick(const KvAttnArgs &a)
+Variant pick(const KvAttnArgs &a, int sms)
 {
     const int group = a.q_heads / a.cache.heads;
     const long long rows = (long long)group * ((a.batch.rows + a.batch.batch - 1) / a.batch.batch);
@@ -780,19 +639,30 @@ Variant pick(const KvAttnArgs &a)
     // few items: every item is split over several CTAs, and wide CTAs leave fewer parts to join;
     // many: narrow CTAs, whose ends and beginnings overlap with their neighbours' streaming
     const int per_sm = v.nt == 1 ? 16 : 12;
-    v.warps = items >= device_sms() ? 4 : v.nt == 1 ? 8 : 6;
-    v.ctas = device_sms() * (per_sm / v.warps);
+    v.warps = items >= sms ? 4 : per_sm / 2;
+    v.ctas = sms * (per_sm / v.warps);
     return v;
 }
 
-size_t counters_bytes() { return align_up((size_t)device_sms() * 5 * sizeof(int), 256); }
+// The prefill kernel's tile is 256 query rows of one key head.
+bool use_prefill(int rows, int batch, int q_heads, int kv_heads)
+{
+    return (long long)(q_heads / kv_heads) * rows >= 96ll * batch;
+}
+
+constexpr int kMaxDevices = 64;
 
 template <int D, int NT, int WARPS>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
 {
     using S = Shape<D, NT, WARPS>;
-    const cudaError_t e = cudaFuncSetAttribute(kv_decode_kernel<D, NT, WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-    if (e != cudaSuccess) return e;
+    static std::atomic<bool> ready[kMaxDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices || !ready[dev].load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(kv_decode_kernel<D, NT, WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < kMaxDevices) ready[dev].store(true, std::memory_order_release);
+    }
     return launch_overlapped(kv_decode_kernel<D, NT, WARPS>, dim3(ctas), dim3(WARPS * 32), S::kSmem, st, a, sc);
 }
 template <int D>
@@ -804,17 +674,22 @@ cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, const Variant &v, cu
 
 }  // namespace
 
-// Status block, a counter per CTA, two partial results per CTA (at most 4 CTAs of one n-tile or 3 of two per SM).
-size_t kv_attention_workspace(int, int, int, int, int D)
+// Status block, counters, and two partial results per CTA (at most 4 CTAs with one tile of eight rows or
+// 3 with two per SM).
+size_t kv_attention_workspace(int rows, int batch, int q_heads, int kv_heads, int D)
 {
-    return sizeof(StatusBlock) + counters_bytes() + (size_t)device_sms() * 3 * 2 * 16 * (D + 2) * sizeof(float);
+    if (use_prefill(rows, batch, q_heads, kv_heads)) return kv_prefill_workspace(D);
+    const int sms = device_sms();
+    return sizeof(StatusBlock) + kv_counters_bytes(sms) + (size_t)sms * 3 * 2 * 16 * (D + 2) * sizeof(float);
 }
 
 cudaError_t launch_kv_attention(const KvAttnArgs &a, uint8_t *workspace, cudaStream_t st)
 {
-    const Variant v = pick(a);
+    if (use_prefill(a.batch.rows, a.batch.batch, a.q_heads, a.cache.heads)) return launch_kv_prefill(a, workspace, st);
+    const int sms = device_sms();
+    const Variant v = pick(a, sms);
     const Schedule sc = {reinterpret_cast<StatusBlock *>(workspace), reinterpret_cast<int *>(workspace + sizeof(StatusBlock)),
-                         reinterpret_cast<float *>(workspace + sizeof(StatusBlock) + counters_bytes()), v.warps, kLead,
+                         reinterpret_cast<float *>(workspace + sizeof(StatusBlock) + kv_counters_bytes(sms)), v.warps, kLead,
                          Divisor((uint32_t)(a.q_heads / a.cache.heads))};
     return a.cache.D == 64 ? launch<64>(a, sc, v, st) : launch<128>(a, sc, v, st);
 }

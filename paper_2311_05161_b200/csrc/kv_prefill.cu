@@ -1,0 +1,934 @@
+// Attention over the 4-bit cache, prefill form: many query rows per sequence.
+//
+// A CTA works on 256 query rows (the heads that share a key head, times tokens) as two tiles of 128, and
+// walks over the keys in units of 128 tokens.  Both products run on the tensor cores with the accumulators
+// in tensor memory: S = Q K^T (tcgen05 kind::f16, operands in shared memory) and O += P V with P read
+// from tensor memory, where it takes the place of its scores.  Tensor memory is full: two score tiles and
+// two output tiles of 128 columns.
+//
+// Roles: eight softmax warps, a thread per row; four expanding warps, a thread per token, which turn a unit's
+// codes into binary16 operand tiles in shared memory (two buffers each for keys and values); one
+// warp issues the MMAs (sixteen warps in all: 128 registers per thread).  While the softmax of one row tile runs, the MMAs of the other do.
+// Every hand-over is an mbarrier with a bounded wait; a wait that runs out raises a flag that ends all roles.
+//
+// Numbers: key operands are exact levels (times -1/2), the step of a token multiplies its score column.
+// Value operands are level * step, rounded once to binary16, on a power-of-two scale per 32 tokens that
+// the weights' exponents take back.  A thread looks over its row's 128 scores for their maximum first; where a
+// weight would exceed 2^15 against the running reference, it moves the reference and scales the output row
+// in tensor memory.  (One pass that computed the weights at once and again after an overflow was slower:
+// on scores that spread over five bits one unit in eight overflowed in some row of a warp.)
+//
+// Bounds per unit and SM for D = 128: 2048 cycles of MMA (two 128 x 128 x 128 products per row
+// tile), 2048 cycles of exponentials at 16 per cycle, about 1000 cycles of packed binary16 arithmetic to
+// expand 32768 codes: the expansion is shared by 256 rows, which is why the two tiles are one CTA's.
+#include <atomic>
+#include <type_traits>
+
+#include "kv_attention.cuh"
+
+namespace w4a8 {
+
+namespace {
+
+constexpr int kRows = 256, kUnit = 128;
+constexpr int kSoftmaxWarps = 8, kExpandWarps = 4, kMmaWarp = kSoftmaxWarps + kExpandWarps, kListWarp = kMmaWarp + 1;
+constexpr int kWarps = 16, kThreads = 32 * kWarps;         // the last two only help to find the share
+constexpr int kConstSlots = 4;
+constexpr int kLead = 3;                                   // an item's fixed cost, in units
+constexpr int kWaitSite = 950;
+
+// -------------------------------------------------------------------- tensor core wrappers
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Operand descriptors: rows of 128 bytes (64 elements) in 128-byte swizzle, eight rows 1024 bytes apart; the second
+// 64 elements of a row lie one tile of rows further on.  As a K-major operand (queries, keys) a row is
+// an index of M or N; as an MN-major one (values) a row is an index of K and the tiles follow each other
+// along N (leading-dimension offset).  The high word is the same for all; the low one holds address and
+// leading-dimension offset in units of 16 bytes.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t leading)
+{
+    return ((addr & 0x3FFFFu) >> 4) | ((leading >> 4) << 16);
+}
+// D += A B with A in shared memory / in tensor memory, binary16 operands, binary32 accumulator.  (Two 32-bit words
+// per descriptor: a role with few registers issues these.)
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+                 : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_request32(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+}
+// All loads so far have arrived; the registers pass through, so that nothing reads them before.
+__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
+                   "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
+                   "+r"(r[28]), "+r"(r[29])
+                 :
+                 : "memory");
+    asm volatile("" : "+r"(r[30]), "+r"(r[31])::"memory");
+}
+__device__ __forceinline__ void tmem_request16(uint32_t addr, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_arrived16(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
+}
+__device__ __forceinline__ float4 load_shared4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32])
+{
+    tmem_request32(addr, r);
+    tmem_arrived(r);
+}
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Instruction descriptor: binary16 A and B, binary32 D, M = 128; B of the value product is MN-major.
+__host__ __device__ constexpr uint32_t instr_desc(int n, int b_mn_major)
+{
+    return (1u << 4) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+template <int D>
+struct Layout {
+    static constexpr int kHalves = D / 64;                 // 64-element parts of a row
+    static constexpr int kPartBytes = 128 * 128;           // 128 rows of one part
+    static constexpr int kTile = kHalves * kPartBytes;     // 128 rows
+    static constexpr int kOffK = 2 * kTile, kOffV = kOffK + 2 * kTile;
+    static constexpr int kOffConst = kOffV + 2 * kTile;
+    static constexpr int kConstBytes = 128 * 4 + 32;       // step * unit per token; scale exponents and their powers
+    static constexpr int kOffQmax = kOffConst + kConstSlots * kConstBytes;
+    static constexpr int kOffBars = kOffQmax + 2 * kSoftmaxWarps * 4;
+    // barriers
+    static constexpr int kKFull = 0, kKEmpty = 2, kVFull = 4, kVEmpty = 6, kConstFull = 8, kSFull = 12, kPReady = 14, kODone = 16,
+                         kQFull = 18, kQmax = 19, kDrain = 20, kPieceFull = 21, kPieceEmpty = 23, kBars = 25;
+    static constexpr int kSmem = kOffBars + kBars * 8 + 1024;
+    static_assert(kSmem + 1024 <= 232448, "shared memory of an SM");
+};
+
+struct Schedule {
+    StatusBlock *sb;
+    int *counters;             // [workers][8]: one per worker and softmax warp
+    float *partials;           // [workers][2] parts of 256 * (D + 2) numbers
+    Divisor group;
+};
+
+
+// A piece of an item that falls into a CTA's share, as the scheduling warp hands it to the others.
+struct Piece {
+    int b, h, tile, rows;                      // sequence, key head, row tile, its rows
+    int row0, n, len;                          // of the sequence
+    int unit0, count;                          // units to walk; count < 0: no more pieces
+    int whole;                                 // the item lies in this share alone
+    int slot, w0, w1, inside;                  // else: where the part goes, the CTAs that share the item, and
+                                               // whether it begins inside the first one's share
+};
+
+struct Control {
+    volatile int abort;
+    uint32_t tmem;
+    int found_b;
+    long long found_off;
+    long long warp_len[kWarps];
+    Piece piece[2];
+};
+
+__device__ bool wait_long(uint32_t bar, uint32_t parity, Control *ctl, StatusBlock *sb, int where)
+{
+    unsigned long long t0 = 0, t;
+    for (uint32_t i = 1;; ++i) {
+        if (try_wait(bar, parity)) return true;
+        if ((i & 63u) == 0u) {
+            if (ctl->abort) return false;
+            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+            if (t0 == 0) t0 = t;
+            else if (t - t0 > kWaitNs) {
+                ctl->abort = 1;
+                report_failure(sb, W4A8_ERR_TIMEOUT, where);
+                return false;
+            }
+        }
+    }
+}
+// All lanes of a warp wait and agree on the outcome.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, Control *ctl, StatusBlock *sb, int where)
+{
+    return __all_sync(0xffffffffu, try_wait(bar, parity) || wait_long(bar, parity, ctl, sb, where));
+}
+
+// The share of the work list a CTA walks through: the list is, for every sequence, row tile and key
+// head in this order, kLead places and then the units that the tile's rows see (at least one place).
+struct Walk {
+    const KvAttnArgs &a;
+    const Schedule &sc;
+    long long at, end, off;                    // place on the list, end of the share, place inside (sequence, tile)
+    int b, tile;
+    Seq s;
+    bool loaded;
+    // the current piece
+    int h, rows, i_first, first, units, from, count;
+    long long first_unit;                      // the item's first unit on the list
+    bool whole;
+
+    __device__ Walk(const KvAttnArgs &a_, const Schedule &sc_) : a(a_), sc(sc_), loaded(false) {}
+
+    __device__ static int tiles_of(const Seq &s, int group) { return (int)(((long long)s.n * group + kRows - 1) / kRows); }
+    __device__ static void span(const KvAttnArgs &a, const Schedule &sc, const Seq &s, int tile, int &i_first, int &i_last, int &rows,
+                                int &first, int &units)
+    {
+        rows = (int)min((long long)kRows, (long long)s.n * sc.group.d - (long long)tile * kRows);
+        i_first = sc.group.div(tile * kRows);
+        i_last = sc.group.div(tile * kRows + rows - 1);
+        const Sight sight(a, s);
+        first = sight.lo(i_first) >> 7;
+        units = max(0, ((sight.hi(i_last) + kUnit - 1) >> 7) - first);
+    }
+    // places of one sequence
+    __device__ static long long length_of(const KvAttnArgs &a, const Schedule &sc, int b)
+    {
+        const Seq s = load_seq(a, b, sc.sb);
+        const int tiles = tiles_of(s, (int)sc.group.d);
+        long long n = 0;
+        for (int t = 0; t < tiles; ++t) {
+            int i0, i1, rows, first, units;
+            span(a, sc, s, t, i0, i1, rows, first, units);
+            n += (long long)a.cache.heads * (kLead + max(units, 1));
+        }
+        return n;
+    }
+    __device__ void start(int b0, long long off0, long long begin, long long end_)
+    {
+        b = b0;
+        off = off0;
+        at = begin;
+        end = end_;
+        tile = 0;
+    }
+    // Moves to the next piece with at least one unit (or the one place of an item without units).
+    __device__ bool next()
+    {
+        while (at < end) {
+            if (!loaded) {
+                s = load_seq(a, b, sc.sb);
+                loaded = true;
+                tile = 0;
+            }
+            if (tile >= tiles_of(s, (int)sc.group.d)) {
+                ++b;
+                loaded = false;
+                continue;
+            }
+            int i_last;
+            span(a, sc, s, tile, i_first, i_last, rows, first, units);
+            const int body = max(units, 1), length = kLead + body;
+            if (off >= (long long)a.cache.heads * length) {
+                off -= (long long)a.cache.heads * length;
+                ++tile;
+                continue;
+            }
+            h = (int)quotient(off, length);
+            const int in = (int)(off - (long long)h * length);
+            const int here = (int)min((long long)(length - in), end - at);
+            from = max(in - kLead, 0);
+            count = max(in + here - kLead, 0) - from;
+            first_unit = at - in + kLead;
+            at += here;
+            off += here;
+            if (count <= 0) continue;
+            whole = count == body;
+            count = min(count, units - from);  // an item without units has nothing to walk
+            return true;
+        }
+        return false;
+    }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_constant__ KvAttnArgs a, const __grid_constant__ Schedule sc)
+{
+    using L = Layout<D>;
+    extern __shared__ uint8_t raw_smem[];
+    __shared__ Control ctl_store;
+    Control *ctl = &ctl_store;
+    uint8_t *smem = raw_smem + ((1024u - (smem_addr(raw_smem) & 1023u)) & 1023u);
+    const uint32_t base = smem_addr(smem);
+    const uint32_t bars = base + L::kOffBars;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    auto bar = [&](int i) { return bars + 8 * i; };
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(L::kKFull + i), kExpandWarps);
+            mbar_init(bar(L::kKEmpty + i), 1);
+            mbar_init(bar(L::kVFull + i), kExpandWarps);
+            mbar_init(bar(L::kVEmpty + i), 1);
+            mbar_init(bar(L::kSFull + i), 1);
+            mbar_init(bar(L::kPReady + i), 4);
+            mbar_init(bar(L::kODone + i), 1);
+        }
+        for (int i = 0; i < kConstSlots; ++i) mbar_init(bar(L::kConstFull + i), kExpandWarps);
+        mbar_init(bar(L::kQFull), kSoftmaxWarps);
+        mbar_init(bar(L::kQmax), kSoftmaxWarps);
+        mbar_init(bar(L::kDrain), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(L::kPieceFull + i), 1);
+            mbar_init(bar(L::kPieceEmpty + i), kSoftmaxWarps + kExpandWarps + 1);
+        }
+        ctl->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async();
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&ctl->tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    allow_dependents();
+    dependent_wait();
+
+    // ---- this CTA's share of the list ----
+    const int batch = a.batch.batch;
+    const int chunk = (batch + kThreads - 1) / kThreads;
+    const int b_first = min(batch, tid * chunk), b_last = min(batch, b_first + chunk);
+    long long mine = 0;
+    for (int b = b_first; b < b_last; ++b) mine += Walk::length_of(a, sc, b);
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) ctl->warp_len[warp] = incl;
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = ctl->tmem;
+    long long total = 0;
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) incl += ctl->warp_len[w];
+        total += ctl->warp_len[w];
+    }
+    const long long per = max(quotient(total + gridDim.x - 1, gridDim.x), 4ll);
+    const long long begin = (long long)blockIdx.x * per, end = min(total, begin + per);
+    if (begin < total && begin >= incl - mine && begin < incl) {
+        long long at = incl - mine;
+        for (int b = b_first; b < b_last; ++b) {
+            const long long n = Walk::length_of(a, sc, b);
+            if (begin < at + n) {
+                ctl->found_b = b;
+                ctl->found_off = begin - at;
+                break;
+            }
+            at += n;
+        }
+    }
+    __syncthreads();
+    const uint32_t tmem_s = tmem, tmem_o = tmem + 256;
+
+    // 128 registers per thread at launch, split anew among the four warpgroups: 2 x 176 + 88 + 72 = 4 x 128
+    if (warp < kSoftmaxWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        // ------------------------------------------------------------------ softmax: a thread per row
+        const int w = warp >> 2, r = tid;                  // row tile, row of the 256
+        const uint32_t quarter = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes of tensor memory
+        const uint32_t s_addr = tmem_s + w * 128 + quarter, o_addr = tmem_o + w * D + quarter;
+        const uint32_t q_row = base + w * L::kTile + (r & 127) * 128;
+        uint32_t unit_no = 0, item_no = 0;
+        bool ok = true;
+        for (uint32_t piece_no = 0;; ++piece_no) {
+            if (!(ok = wait_warp(bar(L::kPieceFull + (piece_no & 1)), (piece_no >> 1) & 1, ctl, sc.sb, kWaitSite + 12))) break;
+            const volatile Piece &pc = ctl->piece[piece_no & 1];
+            const int count = pc.count;
+            if (count < 0) break;
+            const Seq s = {pc.row0, pc.n, pc.len};
+            const Sight sight(a, s);
+            const int flat = pc.tile * kRows + r, i = sc.group.div(flat);
+            const int head = pc.h * (int)sc.group.d + flat - i * (int)sc.group.d;
+            const bool in = r < pc.rows;
+            const int row_hi = in ? sight.hi(i) : s.len, row_lo = in ? sight.lo(i) : 0;
+            float m = kNoReference, l = 0.0f;
+            if (count > 0) {
+                // ---- queries to the operand tile, scaled by a power of two to the top of binary16's range ----
+                uint4 raw[D / 8];
+                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + (in ? (size_t)(s.row0 + i) * a.q_stride + (size_t)head * D : 0));
+                float amax = 0.0f;
+#pragma unroll
+                for (int k = 0; k < D / 8; ++k) {
+                    raw[k] = in ? __ldg(p + k) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t v = (&raw[k].x)[e] & 0x7fff7fffu;
+                        const float2 x = a.q_bf16 ? make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u))
+                                                  : __half22float2(*reinterpret_cast<const __half2 *>(&v));
+                        amax = fmaxf(amax, fmaxf(x.x, x.y));
+                    }
+                }
+                amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
+                volatile float *qmax = reinterpret_cast<float *>(smem + L::kOffQmax) + (item_no & 1) * kSoftmaxWarps;
+                if (lane == 0) {
+                    qmax[warp] = amax;
+                    mbar_arrive(bar(L::kQmax));
+                }
+                if (!(ok = wait_warp(bar(L::kQmax), item_no & 1, ctl, sc.sb, kWaitSite))) break;
+#pragma unroll
+                for (int k = 0; k < kSoftmaxWarps; ++k) amax = fmaxf(amax, qmax[k]);
+                const int e = min(max((int)((__float_as_uint(amax) >> 23) & 255u) - 127 - 14, -100), 113);
+                const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+                for (int k = 0; k < D / 8; ++k) {
+                    float f[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t v = (&raw[k].x)[j];
+                        const float2 x = a.q_bf16 ? make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u))
+                                                  : __half22float2(*reinterpret_cast<const __half2 *>(&v));
+                        f[2 * j] = x.x * down;
+                        f[2 * j + 1] = x.y * down;
+                    }
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_row + (k >> 3) * L::kPartBytes + (((k & 7) ^ (r & 7)) << 4)),
+                                 "r"(pack_half2(f[0], f[4])), "r"(pack_half2(f[1], f[5])), "r"(pack_half2(f[2], f[6])),
+                                 "r"(pack_half2(f[3], f[7]))
+                                 : "memory");
+                }
+                fence_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(L::kQFull));
+                // rows of this warp's tile: what all of them see
+                const int t_first = sc.group.div(pc.tile * kRows + w * 128);
+                const int t_last = sc.group.div(pc.tile * kRows + max(w * 128, min(pc.rows, w * 128 + 128) - 1));
+                const int hi_min = sight.hi(t_first), lo_max = sight.lo(t_last);
+                int j0 = pc.unit0 * kUnit;
+                for (int u = 0; u < count; ++u, ++unit_no, j0 += kUnit) {
+                    const uint32_t slot = unit_no & (kConstSlots - 1);
+                    if (!(ok = wait_warp(bar(L::kConstFull + slot), (unit_no / kConstSlots) & 1, ctl, sc.sb, kWaitSite + 1) &&
+                               wait_warp(bar(L::kSFull + w), unit_no & 1, ctl, sc.sb, kWaitSite + 2)))
+                        break;
+                    fence_after();
+                    const uint32_t ks_addr = base + L::kOffConst + slot * L::kConstBytes;
+                    const volatile float *scale = reinterpret_cast<const float *>(smem + L::kOffConst + slot * L::kConstBytes) + 128;   // exponents of the four groups' value scales, then 2^-exponent
+                    const bool edge = j0 < lo_max || j0 + kUnit > hi_min;
+                    const int lo_off = j0 - row_lo;
+                    const uint32_t span = (uint32_t)max(row_hi - row_lo, 0);
+                    // f(k, x0 .. x3) on the row's exponents less `ref`, four columns k .. k + 3 at a time; the loads of
+                    // the next sixteen scores are on their way meanwhile
+                    auto for_scores = [&](float ref, auto limited, auto f) {
+                        uint32_t v[2][16];
+                        tmem_request16(s_addr, v[0]);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            tmem_arrived16(v[c & 1]);
+                            if (c < 7) tmem_request16(s_addr + 16 * (c + 1), v[(c + 1) & 1]);
+                            const uint32_t(&y)[16] = v[c & 1];
+                            const float shift = scale[c >> 1] - ref;
+#pragma unroll
+                            for (int k = 0; k < 16; k += 4) {
+                                const float4 s4 = load_shared4(ks_addr + 4 * (16 * c + k));
+                                float x0 = fmaf(__uint_as_float(y[k]), s4.x, shift), x1 = fmaf(__uint_as_float(y[k + 1]), s4.y, shift);
+                                float x2 = fmaf(__uint_as_float(y[k + 2]), s4.z, shift), x3 = fmaf(__uint_as_float(y[k + 3]), s4.w, shift);
+                                if constexpr (decltype(limited)::value) {
+                                    const int j = lo_off + 16 * c + k;
+                                    x0 = (uint32_t)j < span ? x0 : -INFINITY;
+                                    x1 = (uint32_t)(j + 1) < span ? x1 : -INFINITY;
+                                    x2 = (uint32_t)(j + 2) < span ? x2 : -INFINITY;
+                                    x3 = (uint32_t)(j + 3) < span ? x3 : -INFINITY;
+                                }
+                                f(16 * c + k, x0, x1, x2, x3);
+                            }
+                        }
+                    };
+                    float top = -INFINITY;
+                    auto find_top = [&](int, float x0, float x1, float x2, float x3) { top = fmaxf(fmaxf(top, fmaxf(x0, x1)), fmaxf(x2, x3)); };
+                    if (edge) for_scores(0.0f, std::true_type(), find_top);
+                    else for_scores(0.0f, std::false_type(), find_top);
+                    const bool fresh = m == kNoReference;
+                    const bool over = top > (fresh ? kNoReference : m + kSlack);
+                    if (__any_sync(0xffffffffu, over)) {     // move the reference and scale what has been summed
+                        const float to = over ? top : m;
+                        const float keep = fresh ? 0.0f : ex2(m - to);
+                        m = to;
+                        l *= keep;
+                        if (u > 0) {
+#pragma unroll 1
+                            for (int c = 0; c < D / 32; ++c) {
+                                uint32_t v[32];
+                                tmem_load32(o_addr + 32 * c, v);
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * keep);
+                                tmem_store32(o_addr + 32 * c, v);
+                            }
+                        }
+                    }
+                    uint32_t pk[64];
+                    float sum0 = 0.0f, sum1 = 0.0f;
+                    auto weigh = [&](int k, float x0, float x1, float x2, float x3) {
+                        x0 = ex2(x0);
+                        x1 = ex2(x1);
+                        x2 = ex2(x2);
+                        x3 = ex2(x3);
+                        sum0 += x0 + x2;
+                        sum1 += x1 + x3;
+                        pk[k / 2] = pack_half2(x0, x1);
+                        pk[k / 2 + 1] = pack_half2(x2, x3);
+                        if ((k & 31) == 28) {                // a group's weights are on its values' scale
+                            l = fmaf(sum0 + sum1, scale[4 + (k >> 5)], l);
+                            sum0 = sum1 = 0.0f;
+                        }
+                    };
+                    const float ref = m == kNoReference ? 0.0f : m;
+                    if (edge) for_scores(ref, std::true_type(), weigh);
+                    else for_scores(ref, std::false_type(), weigh);
+                    tmem_store32(s_addr, pk);
+                    tmem_store32(s_addr + 32, pk + 32);
+                    tmem_store_wait();
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(L::kPReady + w));
+                }
+                if (!ok) break;
+                if (!(ok = wait_warp(bar(L::kODone + w), item_no & 1, ctl, sc.sb, kWaitSite + 3))) break;
+                fence_after();
+                ++item_no;
+            }
+            // ---- this row's output: -2 O / l, or a part of it ----
+            const bool mine_only = pc.whole;
+            float *part = sc.partials + ((size_t)blockIdx.x * 2 + pc.slot) * (kRows * (D + 2));
+            const float inv = l > 0.0f ? __fdiv_rn(-2.0f, l) : 0.0f;
+            const size_t out_at = ((size_t)(s.row0 + i) * a.q_heads + head) * D;
+            auto store8 = [&](int d, const float (&x)[8]) {          // eight elements in their order
+                uint4 o;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float top = a.o_bf16 ? __uint_as_float(0x7f7f0000u) : 65504.0f;
+                    const float y0 = fminf(fmaxf(x[2 * k], -top), top), y1 = fminf(fmaxf(x[2 * k + 1], -top), top);
+                    if (a.o_bf16) {
+                        const __nv_bfloat162 z = __floats2bfloat162_rn(y0, y1);
+                        (&o.x)[k] = *reinterpret_cast<const uint32_t *>(&z);
+                    } else (&o.x)[k] = pack_half2(y0, y1);
+                }
+                *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.O) + out_at + d) = o;
+            };
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t v[32];
+                if (count > 0) tmem_load32(o_addr + 32 * c, v);
+                else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = 0u;
+                }
+                if (!mine_only) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        __stcg(reinterpret_cast<uint4 *>(part + 2 * kRows + (size_t)r * D + 32 * c + k), make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]));
+                } else if (in) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8) {        // columns hold the elements 0, 4, 1, 5, 2, 6, 3, 7 of eight
+                        const float x[8] = {__uint_as_float(v[k]) * inv, __uint_as_float(v[k + 2]) * inv, __uint_as_float(v[k + 4]) * inv,
+                                            __uint_as_float(v[k + 6]) * inv, __uint_as_float(v[k + 1]) * inv, __uint_as_float(v[k + 3]) * inv,
+                                            __uint_as_float(v[k + 5]) * inv, __uint_as_float(v[k + 7]) * inv};
+                        store8(32 * c + k, x);
+                    }
+                }
+            }
+            const int w0 = pc.w0, w1 = pc.w1, inside = pc.inside;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(L::kPieceEmpty + (piece_no & 1)));
+            if (mine_only) {
+                if (in && a.lse) a.lse[out_at / D] = l > 0.0f ? (m + lg2(l)) * kLn2 : -INFINITY;
+                continue;
+            }
+            __stcg(part + r, m);
+            __stcg(part + kRows + r, l);
+            __threadfence();
+            __syncwarp();
+            int last = 0;
+            if (lane == 0) last = atomicAdd(sc.counters + w0 * kSoftmaxWarps + warp, 1) == w1 - w0;
+            if (!__shfl_sync(0xffffffffu, last, 0)) continue;
+            __threadfence();
+            // the last of this warp's counterparts joins the parts in list order
+            const size_t part_size = kRows * (D + 2);
+            const float *head_part = sc.partials + ((size_t)w0 * 2 + (inside ? 1 : 0)) * part_size;
+            const float *rest = sc.partials + (size_t)w0 * 2 * part_size;
+            const int parts = w1 - w0 + 1;
+            float top = __ldcg(head_part + r);
+            for (int k = 1; k < parts; ++k) top = fmaxf(top, __ldcg(rest + (size_t)k * 2 * part_size + r));
+            float lsum = 0.0f;
+            for (int k = 0; k < parts; ++k) {
+                const float *x = k == 0 ? head_part : rest + (size_t)k * 2 * part_size;
+                lsum += __ldcg(x + kRows + r) * ex2(__ldcg(x + r) - top);
+            }
+            const float join_inv = lsum > 0.0f ? __fdiv_rn(-2.0f, lsum) : 0.0f;
+            if (in) {
+                for (int c = 0; c < D; c += 8) {
+                    float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+                    for (int k = 0; k < parts; ++k) {
+                        const float *x = k == 0 ? head_part : rest + (size_t)k * 2 * part_size;
+                        const float f = ex2(__ldcg(x + r) - top);
+                        const float4 y0 = __ldcg(reinterpret_cast<const float4 *>(x + 2 * kRows + (size_t)r * D + c));
+                        const float4 y1 = __ldcg(reinterpret_cast<const float4 *>(x + 2 * kRows + (size_t)r * D + c) + 1);
+                        acc[0] += y0.x * f; acc[4] += y0.y * f; acc[1] += y0.z * f; acc[5] += y0.w * f;
+                        acc[2] += y1.x * f; acc[6] += y1.y * f; acc[3] += y1.z * f; acc[7] += y1.w * f;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) acc[k] *= join_inv;
+                    store8(c, acc);
+                }
+                if (a.lse) a.lse[out_at / D] = lsum > 0.0f ? (top + lg2(lsum)) * kLn2 : -INFINITY;
+            }
+            if (lane == 0) sc.counters[w0 * kSoftmaxWarps + warp] = 0;       // ready for the next call
+        }
+    } else if (warp < kMmaWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        // ------------------------------------------------------------------ expansion of the codes
+        const int tk = tid - 32 * kSoftmaxWarps, ew = warp - kSoftmaxWarps;
+        constexpr int KV4 = D / 32;                        // 16-byte pieces of a token's key codes
+        constexpr int CB = D / 16;                         // bytes of a value slice
+        ExpandConsts ek = {kNibble, kMinusEight};
+        asm volatile("" : "+r"(ek.nibble), "+r"(ek.minus_eight));
+        const int page_bits = a.cache.page_shift - 4, in_page = (1 << page_bits) - 1;
+        const size_t page_bytes = a.cache.page_bytes();
+        uint32_t unit_no = 0, item_no = 0;
+        bool ok = true;
+        for (uint32_t piece_no = 0;; ++piece_no) {
+            if (!(ok = wait_warp(bar(L::kPieceFull + (piece_no & 1)), (piece_no >> 1) & 1, ctl, sc.sb, kWaitSite + 13))) break;
+            const volatile Piece &pc = ctl->piece[piece_no & 1];
+            const int count = pc.count, unit0 = pc.unit0, len = pc.len, seq = pc.b;
+            const uint8_t *head_base = a.cache.pages + ((size_t)pc.h << a.cache.page_shift) * (D + 8);
+            __syncwarp();
+            if (count >= 0 && lane == 0) mbar_arrive(bar(L::kPieceEmpty + (piece_no & 1)));
+            if (count < 0) break;
+            if (count == 0) continue;
+            const int last_block = (len - 1) >> 4;
+            const int32_t *table = a.batch.page_table + (size_t)seq * a.batch.max_pages;
+            auto page_of = [&](int u) {                    // page of this thread's token of unit u of the piece
+                const int blk = min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block);
+                int page = __ldg(table + (blk >> page_bits));
+                if ((unsigned)page >= (unsigned)a.cache.num_pages) {
+                    report_failure(sc.sb, W4A8_ERR_BAD_TABLE, seq);
+                    page = 0;
+                }
+                return page;
+            };
+            uint4 kc[KV4];
+            uint32_t vc[8][CB / 4], kw = 0, vw = 0;
+            auto block_of = [&](int u, int page) {         // this thread's block of unit u
+                const int blk = min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block);
+                return head_base + (size_t)page * page_bytes + (size_t)(blk & in_page) * (16 * (D + 8));
+            };
+            const int t = tk & 15;
+            auto fetch_keys = [&](const uint8_t *p) {
+                const uint4 *k4 = reinterpret_cast<const uint4 *>(p + t * (D / 2));
+#pragma unroll
+                for (int k = 0; k < KV4; ++k) kc[k] = __ldg(k4 + k);
+                kw = __ldg(reinterpret_cast<const uint32_t *>(p + 16 * D + 4 * t));
+                vw = __ldg(reinterpret_cast<const uint32_t *>(p + 16 * D + 64 + 4 * t));
+            };
+            auto fetch_values = [&](const uint8_t *p) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint8_t *q = p + 8 * D + (((t >> 3) * 8 + k) * 8 + (t & 7)) * CB;
+                    if constexpr (CB == 8) {
+                        const uint2 x = __ldg(reinterpret_cast<const uint2 *>(q));
+                        vc[k][0] = x.x;
+                        vc[k][1] = x.y;
+                    } else vc[k][0] = __ldg(reinterpret_cast<const uint32_t *>(q));
+                }
+            };
+            const uint8_t *block = block_of(0, page_of(0));
+            fetch_keys(block);
+            fetch_values(block);
+            int page = count > 1 ? page_of(1) : 0;
+            if (!(ok = wait_warp(bar(L::kQmax), item_no & 1, ctl, sc.sb, kWaitSite + 4))) break;
+            const volatile float *qmax = reinterpret_cast<const float *>(smem + L::kOffQmax) + (item_no & 1) * kSoftmaxWarps;
+            float amax = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kSoftmaxWarps; ++k) amax = fmaxf(amax, qmax[k]);
+            const int e = min(max((int)((__float_as_uint(amax) >> 23) & 255u) - 127 - 14, -100), 113);
+            const float unit = -2.0f * (a.scale * kLog2e) * __uint_as_float((uint32_t)(127 + e) << 23);
+            ++item_no;
+            // Eight levels (times -1/2) of a code word; off = (16 + z) / 2 twice.
+            auto levels = [&](uint32_t w, uint32_t off, uint32_t (&o)[4]) {
+                const uint32_t sw = perm(w, w, 0x2301u);
+                o[0] = pick_rank(w << 4, ek);
+                o[1] = pick_rank(w, ek);
+                o[2] = pick_rank(sw << 4, ek);
+                o[3] = pick_rank(sw, ek);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t x = hadd2(o[k], off);     // -(x + 1) / 2
+                    o[k] = hadd2(x, hfma2_sat(x, kMinusHalf, kQuarter));
+                }
+            };
+            for (int u = 0; u < count; ++u, ++unit_no) {
+                const uint32_t buf = unit_no & 1, use = (unit_no >> 1) & 1, slot = unit_no & (kConstSlots - 1);
+                const bool there = (unit0 + u) * kUnit + tk < len;
+                const uint32_t row = (uint32_t)tk * 128;
+                // ---- keys ----
+                if (unit_no >= 2 && !(ok = wait_warp(bar(L::kKEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 5))) break;
+                {
+                    const uint32_t off = (kw & 15u) * 0x00400040u + 0x48004800u;
+#pragma unroll
+                    for (int k = 0; k < KV4; ++k)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int c = k * 4 + j;
+                            uint32_t o[4];
+                            levels((&kc[k].x)[j], off, o);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + L::kOffK + buf * L::kTile + (c >> 3) * L::kPartBytes + row + (((c & 7) ^ (tk & 7)) << 4)),
+                                         "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
+                                         : "memory");
+                        }
+                }
+                // the value steps' largest in these 32 tokens gives their scale: steps below 2^11 after it
+                const float step = there ? __uint_as_float(vw & ~15u) : 0.0f;
+                const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(step));
+                const int ev = top ? (int)(top >> 23) - 127 - 10 : 0;
+                float *ks = reinterpret_cast<float *>(smem + L::kOffConst + slot * L::kConstBytes);
+                ks[tk] = there ? __uint_as_float(kw & ~15u) * unit : 0.0f;
+                if (lane == 0) {
+                    ks[128 + ew] = (float)ev;
+                    ks[132 + ew] = __uint_as_float((uint32_t)(127 - ev) << 23);
+                }
+                const uint32_t value_word = vw;
+                if (u + 1 < count) {                       // the next unit's keys travel while the values are expanded
+                    block = block_of(u + 1, page);
+                    fetch_keys(block);
+                    if (u + 2 < count) page = page_of(u + 2);
+                }
+                fence_async();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bar(L::kConstFull + slot));
+                    mbar_arrive(bar(L::kKFull + buf));
+                }
+                // ---- values ----
+                if (unit_no >= 2 && !(ok = wait_warp(bar(L::kVEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 6))) break;
+                {
+                    const uint32_t off = (value_word & 15u) * 0x00400040u + 0x48004800u;
+                    const float vs = step * __uint_as_float((uint32_t)(127 - ev) << 23);
+                    const __half hi = __float2half_rn(vs), lo = __float2half_rn(vs - __half2float(hi));
+                    const __half2 hi2 = __half2half2(hi), lo2 = __half2half2(lo);
+                    const uint32_t h = *reinterpret_cast<const uint32_t *>(&hi2), q = *reinterpret_cast<const uint32_t *>(&lo2);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+#pragma unroll
+                        for (int j = 0; j < CB / 4; ++j) {
+                            const int c = k * (CB / 4) + j;
+                            uint32_t o[4];
+                            levels(vc[k][j], off, o);
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) o[x] = hfma2(o[x], h, hfma2(o[x], q, 0u));   // level * step, rounded once
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + L::kOffV + buf * L::kTile + (c >> 3) * L::kPartBytes + row + (((c & 7) ^ (tk & 7)) << 4)),
+                                         "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
+                                         : "memory");
+                        }
+                }
+                fence_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(L::kVFull + buf));
+                if (u + 1 < count) fetch_values(block);
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        // ------------------------------------------------------------------ MMA issue
+        if (warp == kMmaWarp && lane == 0) {
+            constexpr uint32_t idesc_s = instr_desc(kUnit, 0), idesc_o = instr_desc(D, 1);
+            uint32_t unit_no = 0, item_no = 0;
+            bool ok = true;
+            auto wait = [&](int i, uint32_t parity, int where) {
+                return try_wait(bar(i), parity) || wait_long(bar(i), parity, ctl, sc.sb, kWaitSite + where);
+            };
+            auto scores = [&](int w, uint32_t n) {         // S of row tile w for unit number n
+                uint32_t q = desc_low(base + w * L::kTile, 16), k = desc_low(base + L::kOffK + (n & 1) * L::kTile, 16);
+#pragma unroll 1
+                for (int part = 0; part < L::kHalves; ++part, q += L::kPartBytes >> 4, k += L::kPartBytes >> 4) {
+#pragma unroll
+                    for (uint32_t x = 0; x < 4; ++x) mma_ss(tmem_s + w * 128, q + 2 * x, k + 2 * x, idesc_s, part + x);
+                }
+                commit(bar(L::kSFull + w));
+            };
+            auto output = [&](int w, uint32_t n, uint32_t accumulate) {
+                uint32_t v = desc_low(base + L::kOffV + (n & 1) * L::kTile, L::kPartBytes), p = tmem_s + w * 128;
+#pragma unroll 1
+                for (int part = 0; part < kUnit / 64; ++part, v += 4 * (2048 >> 4), p += 32) {
+#pragma unroll
+                    for (uint32_t x = 0; x < 4; ++x) mma_ts(tmem_o + w * D, p + 8 * x, v + x * (2048 >> 4), idesc_o, accumulate + part + x);
+                }
+            };
+            for (uint32_t piece_no = 0;; ++piece_no) {
+                if (!(ok = wait(L::kPieceFull + (piece_no & 1), (piece_no >> 1) & 1, 14))) break;
+                const int n = reinterpret_cast<const volatile Piece &>(ctl->piece[piece_no & 1]).count;
+                if (n < 0) break;
+                mbar_arrive(bar(L::kPieceEmpty + (piece_no & 1)));
+                if (n == 0) continue;
+                if (!(ok = wait(L::kQFull, item_no & 1, 7) && wait(L::kKFull + (unit_no & 1), (unit_no >> 1) & 1, 8))) break;
+                fence_after();
+                scores(0, unit_no);
+                scores(1, unit_no);
+                commit(bar(L::kKEmpty + (unit_no & 1)));
+                for (int u = 0; u < n; ++u, ++unit_no) {
+                    const uint32_t next = unit_no + 1;
+                    if (!(ok = wait(L::kVFull + (unit_no & 1), (unit_no >> 1) & 1, 9) && wait(L::kPReady, unit_no & 1, 10))) break;
+                    fence_after();
+                    output(0, unit_no, u);
+                    if (u + 1 < n) {
+                        if (!(ok = wait(L::kKFull + (next & 1), (next >> 1) & 1, 8))) break;
+                        fence_after();
+                        scores(0, next);
+                    } else commit(bar(L::kODone));
+                    if (!(ok = wait(L::kPReady + 1, unit_no & 1, 11))) break;
+                    fence_after();
+                    output(1, unit_no, u);
+                    commit(bar(L::kVEmpty + (unit_no & 1)));
+                    if (u + 1 < n) {
+                        scores(1, next);
+                        commit(bar(L::kKEmpty + (next & 1)));
+                    } else commit(bar(L::kODone + 1));
+                }
+                ++item_no;
+            }
+            if (!ok) {                                     // nothing of this CTA may still run when it gives its memory back
+                commit(bar(L::kDrain));
+                unsigned long long t0, t;
+                asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
+                do {
+                    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+                } while (!try_wait(bar(L::kDrain), 0) && t - t0 < kWaitNs / 10);
+            }
+        }
+        if (warp == kListWarp && lane == 0) {
+            // -------------------------------------------------------------- the pieces of this CTA's share
+            Walk walk(a, sc);
+            walk.start(ctl->found_b, ctl->found_off, begin, max(begin, end));
+            for (uint32_t piece_no = 0;; ++piece_no) {
+                const bool more = walk.next();
+                if (piece_no >= 2 && !try_wait(bar(L::kPieceEmpty + (piece_no & 1)), (piece_no >> 1 & 1) ^ 1) &&
+                    !wait_long(bar(L::kPieceEmpty + (piece_no & 1)), (piece_no >> 1 & 1) ^ 1, ctl, sc.sb, kWaitSite + 15))
+                    break;
+                Piece p = {};
+                p.count = -1;
+                if (more) {
+                    const int body = max(walk.units, 1);
+                    p.b = walk.b;
+                    p.h = walk.h;
+                    p.tile = walk.tile;
+                    p.rows = walk.rows;
+                    p.row0 = walk.s.row0;
+                    p.n = walk.s.n;
+                    p.len = walk.s.len;
+                    p.unit0 = walk.first + walk.from;
+                    p.count = walk.count;
+                    p.whole = walk.whole;
+                    p.slot = walk.first_unit <= begin ? 0 : 1;
+                    p.w0 = (int)quotient(walk.first_unit, per);
+                    p.w1 = (int)quotient(walk.first_unit + body - 1, per);
+                    p.inside = walk.first_unit > (long long)p.w0 * per;
+                }
+                ctl->piece[piece_no & 1] = p;
+                mbar_arrive(bar(L::kPieceFull + (piece_no & 1)));
+                if (!more) break;
+            }
+        }
+        __syncwarp();
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+constexpr int kMaxDevices = 64;
+
+template <int D>
+cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
+{
+    static std::atomic<bool> ready[kMaxDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices || !ready[dev].load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(kv_prefill_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D>::kSmem);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < kMaxDevices) ready[dev].store(true, std::memory_order_release);
+    }
+    return launch_overlapped(kv_prefill_kernel<D>, dim3(ctas), dim3(kThreads), Layout<D>::kSmem, st, a, sc);
+}
+
+}  // namespace
+
+// Status block, counters, two parts per CTA.
+size_t kv_prefill_workspace(int D)
+{
+    const int sms = device_sms();
+    return sizeof(StatusBlock) + kv_counters_bytes(sms) + (size_t)sms * 2 * kRows * (D + 2) * sizeof(float);
+}
+
+cudaError_t launch_kv_prefill(const KvAttnArgs &a, uint8_t *workspace, cudaStream_t st)
+{
+    const int sms = device_sms();
+    const Schedule sc = {reinterpret_cast<StatusBlock *>(workspace), reinterpret_cast<int *>(workspace + sizeof(StatusBlock)),
+                         reinterpret_cast<float *>(workspace + sizeof(StatusBlock) + kv_counters_bytes(sms)),
+                         Divisor((uint32_t)(a.q_heads / a.cache.heads))};
+    return a.cache.D == 64 ? launch<64>(a, sc, sms, st) : launch<128>(a, sc, sms, st);
+}
+
+}  // namespace w4a8
