@@ -1,13 +1,15 @@
 // Attention over the 4-bit cache, prefill form: many query rows per sequence.
 //
 // A CTA works on 256 query rows (the heads that share a key head, times tokens) as two tiles of 128, and
-// walks over the keys in units of 128 tokens.  Both products run on the tensor cores with the accumulators
+// walks over the keys in units of 64 tokens.  Both products run on the tensor cores with the accumulators
 // in tensor memory: S = Q K^T (tcgen05 kind::f16, operands in shared memory) and O += P V with P read
-// from tensor memory, where it takes the place of its scores.  Tensor memory is full: two score tiles and
-// two output tiles of 128 columns.
+// from tensor memory, where it takes the place of its scores.  Tensor memory is full: two score buffers of 64
+// columns and an output tile of 128 per row tile.  Two buffers, so that the scores of the next unit are
+// computed while the softmax of this one runs (units of 128 tokens with one buffer left every row tile with
+// a chain of softmax and MMAs: 173 us on the 1024-row chunk below).
 //
-// Roles: eight softmax warps, a thread per row; four expanding warps, a thread per token, which turn a unit's
-// codes into binary16 operand tiles in shared memory (two buffers each for keys and values); one
+// Roles: eight softmax warps, a thread per row; four expanding warps, two threads per token, which turn a unit's
+// codes into binary16 operand tiles in shared memory (four units of keys and values); one
 // warp issues the MMAs (sixteen warps in all: 128 registers per thread).  While the softmax of one row tile runs, the MMAs of the other do.
 // Every hand-over is an mbarrier with a bounded wait; a wait that runs out raises a flag that ends all roles.
 //
@@ -30,11 +32,12 @@ namespace w4a8 {
 
 namespace {
 
-constexpr int kRows = 256, kUnit = 128;
+constexpr int kRows = 256, kUnit = 64, kUnitShift = 6;
 constexpr int kSoftmaxWarps = 8, kExpandWarps = 4, kMmaWarp = kSoftmaxWarps + kExpandWarps, kListWarp = kMmaWarp + 1;
 constexpr int kWarps = 16, kThreads = 32 * kWarps;         // the last two only help to find the share
-constexpr int kConstSlots = 4;
-constexpr int kLead = 3;                                   // an item's fixed cost, in units
+constexpr int kRing = 4;                                   // units of expanded keys, and of values
+constexpr int kConstSlots = 8;                             // more than kRing: a slot is rewritten after its unit's softmax
+constexpr int kLead = 6;                                   // an item's fixed cost, in units
 constexpr int kWaitSite = 950;
 
 // -------------------------------------------------------------------- tensor core wrappers
@@ -120,11 +123,33 @@ __device__ __forceinline__ void tmem_arrived16(uint32_t (&r)[16])
                  :
                  : "memory");
 }
-__device__ __forceinline__ float4 load_shared4(uint32_t addr)
+__device__ __forceinline__ void load_shared_pairs(uint32_t addr, uint64_t &a, uint64_t &b)
 {
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-    return v;
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr));
+}
+// Pairs of binary32 numbers for the packed instructions.
+__device__ __forceinline__ uint64_t pair_bits(uint32_t lo, uint32_t hi)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
+    return d;
+}
+__device__ __forceinline__ uint64_t pair(float lo, float hi) { return pair_bits(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ void unpair(uint64_t v, float &lo, float &hi)
+{
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
 }
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32])
 {
@@ -152,16 +177,18 @@ __host__ __device__ constexpr uint32_t instr_desc(int n, int b_mn_major)
 template <int D>
 struct Layout {
     static constexpr int kHalves = D / 64;                 // 64-element parts of a row
-    static constexpr int kPartBytes = 128 * 128;           // 128 rows of one part
-    static constexpr int kTile = kHalves * kPartBytes;     // 128 rows
-    static constexpr int kOffK = 2 * kTile, kOffV = kOffK + 2 * kTile;
-    static constexpr int kOffConst = kOffV + 2 * kTile;
-    static constexpr int kConstBytes = 128 * 4 + 32;       // step * unit per token; scale exponents and their powers
+    static constexpr int kQPart = 128 * 128, kQTile = kHalves * kQPart;          // 128 query rows
+    static constexpr int kPartBytes = kUnit * 128, kTile = kHalves * kPartBytes; // a unit's keys or values
+    static constexpr int kOffK = 2 * kQTile, kOffV = kOffK + kRing * kTile;
+    static constexpr int kOffConst = kOffV + kRing * kTile;
+    static constexpr int kConstBytes = kUnit * 4 + 16;     // step * unit per token; two groups' scale exponents and powers
     static constexpr int kOffQmax = kOffConst + kConstSlots * kConstBytes;
     static constexpr int kOffBars = kOffQmax + 2 * kSoftmaxWarps * 4;
     // barriers
-    static constexpr int kKFull = 0, kKEmpty = 2, kVFull = 4, kVEmpty = 6, kConstFull = 8, kSFull = 12, kPReady = 14, kODone = 16,
-                         kQFull = 18, kQmax = 19, kDrain = 20, kPieceFull = 21, kPieceEmpty = 23, kBars = 25;
+    static constexpr int kKFull = 0, kKEmpty = kKFull + kRing, kVFull = kKEmpty + kRing, kVEmpty = kVFull + kRing,
+                         kConstFull = kVEmpty + kRing, kSFull = kConstFull + kConstSlots, kPReady = kSFull + 4, kODone = kPReady + 4,
+                         kQFull = kODone + 2, kQmax = kQFull + 1, kDrain = kQmax + 1, kPieceFull = kDrain + 1,
+                         kPieceEmpty = kPieceFull + 2, kBars = kPieceEmpty + 2;
     static constexpr int kSmem = kOffBars + kBars * 8 + 1024;
     static_assert(kSmem + 1024 <= 232448, "shared memory of an SM");
 };
@@ -240,8 +267,8 @@ struct Walk {
         i_first = sc.group.div(tile * kRows);
         i_last = sc.group.div(tile * kRows + rows - 1);
         const Sight sight(a, s);
-        first = sight.lo(i_first) >> 7;
-        units = max(0, ((sight.hi(i_last) + kUnit - 1) >> 7) - first);
+        first = sight.lo(i_first) >> kUnitShift;
+        units = max(0, ((sight.hi(i_last) + kUnit - 1) >> kUnitShift) - first);
     }
     // places of one sequence
     __device__ static long long length_of(const KvAttnArgs &a, const Schedule &sc, int b)
@@ -316,15 +343,17 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     auto bar = [&](int i) { return bars + 8 * i; };
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kRing; ++i) {
             mbar_init(bar(L::kKFull + i), kExpandWarps);
             mbar_init(bar(L::kKEmpty + i), 1);
             mbar_init(bar(L::kVFull + i), kExpandWarps);
             mbar_init(bar(L::kVEmpty + i), 1);
+        }
+        for (int i = 0; i < 4; ++i) {          // row tile, score buffer
             mbar_init(bar(L::kSFull + i), 1);
             mbar_init(bar(L::kPReady + i), 4);
-            mbar_init(bar(L::kODone + i), 1);
         }
+        for (int i = 0; i < 2; ++i) mbar_init(bar(L::kODone + i), 1);
         for (int i = 0; i < kConstSlots; ++i) mbar_init(bar(L::kConstFull + i), kExpandWarps);
         mbar_init(bar(L::kQFull), kSoftmaxWarps);
         mbar_init(bar(L::kQmax), kSoftmaxWarps);
@@ -389,8 +418,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         // ------------------------------------------------------------------ softmax: a thread per row
         const int w = warp >> 2, r = tid;                  // row tile, row of the 256
         const uint32_t quarter = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes of tensor memory
-        const uint32_t s_addr = tmem_s + w * 128 + quarter, o_addr = tmem_o + w * D + quarter;
-        const uint32_t q_row = base + w * L::kTile + (r & 127) * 128;
+        const uint32_t s_base = tmem_s + w * 128 + quarter, o_addr = tmem_o + w * D + quarter;
+        const uint32_t q_row = base + w * L::kQTile + (r & 127) * 128;
         uint32_t unit_no = 0, item_no = 0;
         bool ok = true;
         for (uint32_t piece_no = 0;; ++piece_no) {
@@ -443,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                         f[2 * j] = x.x * down;
                         f[2 * j + 1] = x.y * down;
                     }
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_row + (k >> 3) * L::kPartBytes + (((k & 7) ^ (r & 7)) << 4)),
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_row + (k >> 3) * L::kQPart + (((k & 7) ^ (r & 7)) << 4)),
                                  "r"(pack_half2(f[0], f[4])), "r"(pack_half2(f[1], f[5])), "r"(pack_half2(f[2], f[6])),
                                  "r"(pack_half2(f[3], f[7]))
                                  : "memory");
@@ -457,47 +486,59 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 const int hi_min = sight.hi(t_first), lo_max = sight.lo(t_last);
                 int j0 = pc.unit0 * kUnit;
                 for (int u = 0; u < count; ++u, ++unit_no, j0 += kUnit) {
-                    const uint32_t slot = unit_no & (kConstSlots - 1);
-                    if (!(ok = wait_warp(bar(L::kConstFull + slot), (unit_no / kConstSlots) & 1, ctl, sc.sb, kWaitSite + 1) &&
-                               wait_warp(bar(L::kSFull + w), unit_no & 1, ctl, sc.sb, kWaitSite + 2)))
+                    const uint32_t slot = unit_no % kConstSlots;
+                    if (!(ok = wait_warp(bar(L::kConstFull + slot), unit_no / kConstSlots & 1, ctl, sc.sb, kWaitSite + 1) &&
+                               wait_warp(bar(L::kSFull + 2 * w + (unit_no & 1)), (unit_no >> 1) & 1, ctl, sc.sb, kWaitSite + 2)))
                         break;
                     fence_after();
                     const uint32_t ks_addr = base + L::kOffConst + slot * L::kConstBytes;
-                    const volatile float *scale = reinterpret_cast<const float *>(smem + L::kOffConst + slot * L::kConstBytes) + 128;   // exponents of the four groups' value scales, then 2^-exponent
+                    const volatile float *scale = reinterpret_cast<const float *>(smem + L::kOffConst + slot * L::kConstBytes) + kUnit;   // exponents of the two groups' value scales, then 2^-exponent
+                    const uint32_t s_addr = s_base + (unit_no & 1) * kUnit;
                     const bool edge = j0 < lo_max || j0 + kUnit > hi_min;
-                    const int lo_off = j0 - row_lo;
-                    const uint32_t span = (uint32_t)max(row_hi - row_lo, 0);
-                    // f(k, x0 .. x3) on the row's exponents less `ref`, four columns k .. k + 3 at a time; the loads of
-                    // the next sixteen scores are on their way meanwhile
-                    auto for_scores = [&](float ref, auto limited, auto f) {
+                    // exponents of the row's weights, sixteen columns at a time; the next sixteen scores are on their way meanwhile
+                    uint64_t x[kUnit / 2];                   // pairs
+                    {
                         uint32_t v[2][16];
                         tmem_request16(s_addr, v[0]);
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) {
+                        for (int c = 0; c < kUnit / 16; ++c) {
                             tmem_arrived16(v[c & 1]);
-                            if (c < 7) tmem_request16(s_addr + 16 * (c + 1), v[(c + 1) & 1]);
-                            const uint32_t(&y)[16] = v[c & 1];
-                            const float shift = scale[c >> 1] - ref;
+                            if (c < kUnit / 16 - 1) tmem_request16(s_addr + 16 * (c + 1), v[(c + 1) & 1]);
+                            const float e = scale[c >> 1];
+                            const uint64_t shift = pair(e, e);
 #pragma unroll
                             for (int k = 0; k < 16; k += 4) {
-                                const float4 s4 = load_shared4(ks_addr + 4 * (16 * c + k));
-                                float x0 = fmaf(__uint_as_float(y[k]), s4.x, shift), x1 = fmaf(__uint_as_float(y[k + 1]), s4.y, shift);
-                                float x2 = fmaf(__uint_as_float(y[k + 2]), s4.z, shift), x3 = fmaf(__uint_as_float(y[k + 3]), s4.w, shift);
-                                if constexpr (decltype(limited)::value) {
-                                    const int j = lo_off + 16 * c + k;
-                                    x0 = (uint32_t)j < span ? x0 : -INFINITY;
-                                    x1 = (uint32_t)(j + 1) < span ? x1 : -INFINITY;
-                                    x2 = (uint32_t)(j + 2) < span ? x2 : -INFINITY;
-                                    x3 = (uint32_t)(j + 3) < span ? x3 : -INFINITY;
-                                }
-                                f(16 * c + k, x0, x1, x2, x3);
+                                uint64_t k0, k1;
+                                load_shared_pairs(ks_addr + 4 * (16 * c + k), k0, k1);
+                                x[8 * c + k / 2] = fma_pair(pair_bits(v[c & 1][k], v[c & 1][k + 1]), k0, shift);
+                                x[8 * c + k / 2 + 1] = fma_pair(pair_bits(v[c & 1][k + 2], v[c & 1][k + 3]), k1, shift);
                             }
                         }
-                    };
-                    float top = -INFINITY;
-                    auto find_top = [&](int, float x0, float x1, float x2, float x3) { top = fmaxf(fmaxf(top, fmaxf(x0, x1)), fmaxf(x2, x3)); };
-                    if (edge) for_scores(0.0f, std::true_type(), find_top);
-                    else for_scores(0.0f, std::false_type(), find_top);
+                    }
+                    if (edge) {
+                        const int lo_off = j0 - row_lo;
+                        const uint32_t span = (uint32_t)max(row_hi - row_lo, 0);
+#pragma unroll
+                        for (int k = 0; k < kUnit; k += 2) {
+                            float x0, x1;
+                            unpair(x[k / 2], x0, x1);
+                            x0 = (uint32_t)(lo_off + k) < span ? x0 : -INFINITY;
+                            x1 = (uint32_t)(lo_off + k + 1) < span ? x1 : -INFINITY;
+                            x[k / 2] = pair(x0, x1);
+                        }
+                    }
+                    float top0 = -INFINITY, top1 = -INFINITY;
+#pragma unroll
+                    for (int k = 0; k < kUnit / 2; k += 2) {
+                        float x0, x1, x2, x3;
+                        unpair(x[k], x0, x1);
+                        unpair(x[k + 1], x2, x3);
+                        top0 = fmaxf(top0, fmaxf(x0, x1));
+                        top1 = fmaxf(top1, fmaxf(x2, x3));
+                    }
+                    const float top = fmaxf(top0, top1);
+                    // the product of the unit before (every one is waited for in turn: the barrier knows one phase)
+                    if (u > 0 && !(ok = wait_warp(bar(L::kODone + w), (unit_no + 1) & 1, ctl, sc.sb, kWaitSite + 3))) break;
                     const bool fresh = m == kNoReference;
                     const bool over = top > (fresh ? kNoReference : m + kSlack);
                     if (__any_sync(0xffffffffu, over)) {     // move the reference and scale what has been summed
@@ -506,6 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                         m = to;
                         l *= keep;
                         if (u > 0) {
+                            fence_after();
 #pragma unroll 1
                             for (int c = 0; c < D / 32; ++c) {
                                 uint32_t v[32];
@@ -516,34 +558,33 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                             }
                         }
                     }
-                    uint32_t pk[64];
-                    float sum0 = 0.0f, sum1 = 0.0f;
-                    auto weigh = [&](int k, float x0, float x1, float x2, float x3) {
-                        x0 = ex2(x0);
-                        x1 = ex2(x1);
-                        x2 = ex2(x2);
-                        x3 = ex2(x3);
-                        sum0 += x0 + x2;
-                        sum1 += x1 + x3;
-                        pk[k / 2] = pack_half2(x0, x1);
-                        pk[k / 2 + 1] = pack_half2(x2, x3);
-                        if ((k & 31) == 28) {                // a group's weights are on its values' scale
-                            l = fmaf(sum0 + sum1, scale[4 + (k >> 5)], l);
-                            sum0 = sum1 = 0.0f;
+                    const float ref = m == kNoReference ? 0.0f : -m;
+                    const uint64_t ref2 = pair(ref, ref);
+                    uint32_t pk[kUnit / 2];
+#pragma unroll
+                    for (int c = 0; c < kUnit / 32; ++c) {
+                        uint64_t sum = 0ull;                 // (0, 0)
+#pragma unroll
+                        for (int k = 16 * c; k < 16 * c + 16; ++k) {
+                            float x0, x1;
+                            unpair(add_pair(x[k], ref2), x0, x1);
+                            x0 = ex2(x0);
+                            x1 = ex2(x1);
+                            sum = add_pair(sum, pair(x0, x1));
+                            pk[k] = pack_half2(x0, x1);
                         }
-                    };
-                    const float ref = m == kNoReference ? 0.0f : m;
-                    if (edge) for_scores(ref, std::true_type(), weigh);
-                    else for_scores(ref, std::false_type(), weigh);
+                        float s0, s1;
+                        unpair(sum, s0, s1);
+                        l = fmaf(s0 + s1, scale[2 + c], l);  // a group's weights are on its values' scale
+                    }
                     tmem_store32(s_addr, pk);
-                    tmem_store32(s_addr + 32, pk + 32);
                     tmem_store_wait();
                     fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(L::kPReady + w));
+                    if (lane == 0) mbar_arrive(bar(L::kPReady + 2 * w + (unit_no & 1)));
                 }
                 if (!ok) break;
-                if (!(ok = wait_warp(bar(L::kODone + w), item_no & 1, ctl, sc.sb, kWaitSite + 3))) break;
+                if (!(ok = wait_warp(bar(L::kODone + w), (unit_no + 1) & 1, ctl, sc.sb, kWaitSite + 3))) break;
                 fence_after();
                 ++item_no;
             }
@@ -638,8 +679,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     } else if (warp < kMmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         // ------------------------------------------------------------------ expansion of the codes
-        const int tk = tid - 32 * kSoftmaxWarps, ew = warp - kSoftmaxWarps;
-        constexpr int KV4 = D / 32;                        // 16-byte pieces of a token's key codes
+        const int id = tid - 32 * kSoftmaxWarps, tk = id & (kUnit - 1), half = id >> kUnitShift, group32 = (warp - kSoftmaxWarps) & 1;
+        constexpr int KV4 = D / 64;                        // 16-byte pieces of half a token's key codes
         constexpr int CB = D / 16;                         // bytes of a value slice
         ExpandConsts ek = {kNibble, kMinusEight};
         asm volatile("" : "+r"(ek.nibble), "+r"(ek.minus_eight));
@@ -668,14 +709,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 return page;
             };
             uint4 kc[KV4];
-            uint32_t vc[8][CB / 4], kw = 0, vw = 0;
+            uint32_t vc[4][CB / 4], kw = 0, vw = 0;
             auto block_of = [&](int u, int page) {         // this thread's block of unit u
                 const int blk = min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block);
                 return head_base + (size_t)page * page_bytes + (size_t)(blk & in_page) * (16 * (D + 8));
             };
             const int t = tk & 15;
             auto fetch_keys = [&](const uint8_t *p) {
-                const uint4 *k4 = reinterpret_cast<const uint4 *>(p + t * (D / 2));
+                const uint4 *k4 = reinterpret_cast<const uint4 *>(p + t * (D / 2) + half * (D / 4));
 #pragma unroll
                 for (int k = 0; k < KV4; ++k) kc[k] = __ldg(k4 + k);
                 kw = __ldg(reinterpret_cast<const uint32_t *>(p + 16 * D + 4 * t));
@@ -683,8 +724,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             };
             auto fetch_values = [&](const uint8_t *p) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const uint8_t *q = p + 8 * D + (((t >> 3) * 8 + k) * 8 + (t & 7)) * CB;
+                for (int k = 0; k < 4; ++k) {
+                    const uint8_t *q = p + 8 * D + (((t >> 3) * 8 + half * 4 + k) * 8 + (t & 7)) * CB;
                     if constexpr (CB == 8) {
                         const uint2 x = __ldg(reinterpret_cast<const uint2 *>(q));
                         vc[k][0] = x.x;
@@ -718,18 +759,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 }
             };
             for (int u = 0; u < count; ++u, ++unit_no) {
-                const uint32_t buf = unit_no & 1, use = (unit_no >> 1) & 1, slot = unit_no & (kConstSlots - 1);
+                const uint32_t buf = unit_no % kRing, use = unit_no / kRing & 1, slot = unit_no % kConstSlots;
                 const bool there = (unit0 + u) * kUnit + tk < len;
                 const uint32_t row = (uint32_t)tk * 128;
                 // ---- keys ----
-                if (unit_no >= 2 && !(ok = wait_warp(bar(L::kKEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 5))) break;
+                if (unit_no >= kRing && !(ok = wait_warp(bar(L::kKEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 5))) break;
                 {
                     const uint32_t off = (kw & 15u) * 0x00400040u + 0x48004800u;
 #pragma unroll
                     for (int k = 0; k < KV4; ++k)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const int c = k * 4 + j;
+                            const int c = half * (D / 16) + k * 4 + j;
                             uint32_t o[4];
                             levels((&kc[k].x)[j], off, o);
                             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + L::kOffK + buf * L::kTile + (c >> 3) * L::kPartBytes + row + (((c & 7) ^ (tk & 7)) << 4)),
@@ -742,10 +783,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(step));
                 const int ev = top ? (int)(top >> 23) - 127 - 10 : 0;
                 float *ks = reinterpret_cast<float *>(smem + L::kOffConst + slot * L::kConstBytes);
-                ks[tk] = there ? __uint_as_float(kw & ~15u) * unit : 0.0f;
-                if (lane == 0) {
-                    ks[128 + ew] = (float)ev;
-                    ks[132 + ew] = __uint_as_float((uint32_t)(127 - ev) << 23);
+                if (half == 0) {
+                    ks[tk] = there ? __uint_as_float(kw & ~15u) * unit : 0.0f;
+                    if (lane == 0) {
+                        ks[kUnit + group32] = (float)ev;
+                        ks[kUnit + 2 + group32] = __uint_as_float((uint32_t)(127 - ev) << 23);
+                    }
                 }
                 const uint32_t value_word = vw;
                 if (u + 1 < count) {                       // the next unit's keys travel while the values are expanded
@@ -760,7 +803,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     mbar_arrive(bar(L::kKFull + buf));
                 }
                 // ---- values ----
-                if (unit_no >= 2 && !(ok = wait_warp(bar(L::kVEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 6))) break;
+                if (unit_no >= kRing && !(ok = wait_warp(bar(L::kVEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 6))) break;
                 {
                     const uint32_t off = (value_word & 15u) * 0x00400040u + 0x48004800u;
                     const float vs = step * __uint_as_float((uint32_t)(127 - ev) << 23);
@@ -768,10 +811,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     const __half2 hi2 = __half2half2(hi), lo2 = __half2half2(lo);
                     const uint32_t h = *reinterpret_cast<const uint32_t *>(&hi2), q = *reinterpret_cast<const uint32_t *>(&lo2);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
+                    for (int k = 0; k < 4; ++k)
 #pragma unroll
                         for (int j = 0; j < CB / 4; ++j) {
-                            const int c = k * (CB / 4) + j;
+                            const int c = (half * 4 + k) * (CB / 4) + j;
                             uint32_t o[4];
                             levels(vc[k][j], off, o);
 #pragma unroll
@@ -798,21 +841,20 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 return try_wait(bar(i), parity) || wait_long(bar(i), parity, ctl, sc.sb, kWaitSite + where);
             };
             auto scores = [&](int w, uint32_t n) {         // S of row tile w for unit number n
-                uint32_t q = desc_low(base + w * L::kTile, 16), k = desc_low(base + L::kOffK + (n & 1) * L::kTile, 16);
+                const uint32_t d = tmem_s + w * 128 + (n & 1) * kUnit;
+                uint32_t q = desc_low(base + w * L::kQTile, 16), k = desc_low(base + L::kOffK + n % kRing * L::kTile, 16);
 #pragma unroll 1
-                for (int part = 0; part < L::kHalves; ++part, q += L::kPartBytes >> 4, k += L::kPartBytes >> 4) {
+                for (int part = 0; part < L::kHalves; ++part, q += L::kQPart >> 4, k += L::kPartBytes >> 4) {
 #pragma unroll
-                    for (uint32_t x = 0; x < 4; ++x) mma_ss(tmem_s + w * 128, q + 2 * x, k + 2 * x, idesc_s, part + x);
+                    for (uint32_t x = 0; x < 4; ++x) mma_ss(d, q + 2 * x, k + 2 * x, idesc_s, part + x);
                 }
-                commit(bar(L::kSFull + w));
+                commit(bar(L::kSFull + 2 * w + (n & 1)));
             };
             auto output = [&](int w, uint32_t n, uint32_t accumulate) {
-                uint32_t v = desc_low(base + L::kOffV + (n & 1) * L::kTile, L::kPartBytes), p = tmem_s + w * 128;
-#pragma unroll 1
-                for (int part = 0; part < kUnit / 64; ++part, v += 4 * (2048 >> 4), p += 32) {
+                const uint32_t v = desc_low(base + L::kOffV + n % kRing * L::kTile, L::kPartBytes), p = tmem_s + w * 128 + (n & 1) * kUnit;
 #pragma unroll
-                    for (uint32_t x = 0; x < 4; ++x) mma_ts(tmem_o + w * D, p + 8 * x, v + x * (2048 >> 4), idesc_o, accumulate + part + x);
-                }
+                for (uint32_t x = 0; x < kUnit / 16; ++x) mma_ts(tmem_o + w * D, p + 8 * x, v + x * (2048 >> 4), idesc_o, accumulate + x);
+                commit(bar(L::kODone + w));
             };
             for (uint32_t piece_no = 0;; ++piece_no) {
                 if (!(ok = wait(L::kPieceFull + (piece_no & 1), (piece_no >> 1) & 1, 14))) break;
@@ -820,29 +862,30 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 if (n < 0) break;
                 mbar_arrive(bar(L::kPieceEmpty + (piece_no & 1)));
                 if (n == 0) continue;
-                if (!(ok = wait(L::kQFull, item_no & 1, 7) && wait(L::kKFull + (unit_no & 1), (unit_no >> 1) & 1, 8))) break;
+                if (!(ok = wait(L::kQFull, item_no & 1, 7) && wait(L::kKFull + unit_no % kRing, unit_no / kRing & 1, 8))) break;
                 fence_after();
                 scores(0, unit_no);
                 scores(1, unit_no);
-                commit(bar(L::kKEmpty + (unit_no & 1)));
+                commit(bar(L::kKEmpty + unit_no % kRing));
+                // the scores of a unit are computed while the softmax of the one before runs
                 for (int u = 0; u < n; ++u, ++unit_no) {
                     const uint32_t next = unit_no + 1;
-                    if (!(ok = wait(L::kVFull + (unit_no & 1), (unit_no >> 1) & 1, 9) && wait(L::kPReady, unit_no & 1, 10))) break;
+                    if (u + 1 < n) {
+                        if (!(ok = wait(L::kKFull + next % kRing, next / kRing & 1, 8))) break;
+                        fence_after();
+                        scores(0, next);
+                    }
+                    if (!(ok = wait(L::kVFull + unit_no % kRing, unit_no / kRing & 1, 9) && wait(L::kPReady + (unit_no & 1), (unit_no >> 1) & 1, 10))) break;
                     fence_after();
                     output(0, unit_no, u);
                     if (u + 1 < n) {
-                        if (!(ok = wait(L::kKFull + (next & 1), (next >> 1) & 1, 8))) break;
-                        fence_after();
-                        scores(0, next);
-                    } else commit(bar(L::kODone));
-                    if (!(ok = wait(L::kPReady + 1, unit_no & 1, 11))) break;
+                        scores(1, next);
+                        commit(bar(L::kKEmpty + next % kRing));
+                    }
+                    if (!(ok = wait(L::kPReady + 2 + (unit_no & 1), (unit_no >> 1) & 1, 11))) break;
                     fence_after();
                     output(1, unit_no, u);
-                    commit(bar(L::kVEmpty + (unit_no & 1)));
-                    if (u + 1 < n) {
-                        scores(1, next);
-                        commit(bar(L::kKEmpty + (next & 1)));
-                    } else commit(bar(L::kODone + 1));
+                    commit(bar(L::kVEmpty + unit_no % kRing));
                 }
                 ++item_no;
             }
