@@ -8,9 +8,10 @@
 // computed while the softmax of this one runs (units of 128 tokens with one buffer left every row tile with
 // a chain of softmax and MMAs: 173 us on the 1024-row chunk below).
 //
-// Roles: eight softmax warps, a thread per row; four expanding warps, two threads per token, which turn a unit's
-// codes into binary16 operand tiles in shared memory (four units of keys and values); one
-// warp issues the MMAs (sixteen warps in all: 128 registers per thread).  While the softmax of one row tile runs, the MMAs of the other do.
+// Roles: eight softmax warps, a thread per row; eight expanding warps, four threads per token, which turn a unit's
+// codes into binary16 operand tiles in shared memory (four units of keys and values); two
+// warps issue the MMAs, one for each row tile (a thread issues an MMA per 100 cycles or so beside the busy
+// softmax warps, twice what the MMAs take); one lists the pieces of work.  Twenty warps in all.
 // Every hand-over is an mbarrier with a bounded wait; a wait that runs out raises a flag that ends all roles.
 //
 // Numbers: key operands are exact levels (times -1/2), the step of a token multiplies its score column.
@@ -33,8 +34,8 @@ namespace w4a8 {
 namespace {
 
 constexpr int kRows = 256, kUnit = 64, kUnitShift = 6;
-constexpr int kSoftmaxWarps = 8, kExpandWarps = 4, kMmaWarp = kSoftmaxWarps + kExpandWarps, kListWarp = kMmaWarp + 1;
-constexpr int kWarps = 16, kThreads = 32 * kWarps;         // the last two only help to find the share
+constexpr int kSoftmaxWarps = 8, kExpandWarps = 8, kMmaWarp = kSoftmaxWarps + kExpandWarps, kListWarp = kMmaWarp + 2;
+constexpr int kWarps = 20, kThreads = 32 * kWarps;         // the last one only helps to find the share
 constexpr int kRing = 4;                                   // units of expanded keys, and of values
 constexpr int kConstSlots = 8;                             // more than kRing: a slot is rewritten after its unit's softmax
 constexpr int kLead = 6;                                   // an item's fixed cost, in units
@@ -187,7 +188,7 @@ struct Layout {
     // barriers
     static constexpr int kKFull = 0, kKEmpty = kKFull + kRing, kVFull = kKEmpty + kRing, kVEmpty = kVFull + kRing,
                          kConstFull = kVEmpty + kRing, kSFull = kConstFull + kConstSlots, kPReady = kSFull + 4, kODone = kPReady + 4,
-                         kQFull = kODone + 2, kQmax = kQFull + 1, kDrain = kQmax + 1, kPieceFull = kDrain + 1,
+                         kQFull = kODone + 2, kQmax = kQFull + 2, kDrain = kQmax + 1, kPieceFull = kDrain + 2,
                          kPieceEmpty = kPieceFull + 2, kBars = kPieceEmpty + 2;
     static constexpr int kSmem = kOffBars + kBars * 8 + 1024;
     static_assert(kSmem + 1024 <= 232448, "shared memory of an SM");
@@ -345,22 +346,24 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     if (tid == 0) {
         for (int i = 0; i < kRing; ++i) {
             mbar_init(bar(L::kKFull + i), kExpandWarps);
-            mbar_init(bar(L::kKEmpty + i), 1);
+            mbar_init(bar(L::kKEmpty + i), 2);
             mbar_init(bar(L::kVFull + i), kExpandWarps);
-            mbar_init(bar(L::kVEmpty + i), 1);
+            mbar_init(bar(L::kVEmpty + i), 2);
         }
         for (int i = 0; i < 4; ++i) {          // row tile, score buffer
             mbar_init(bar(L::kSFull + i), 1);
             mbar_init(bar(L::kPReady + i), 4);
         }
-        for (int i = 0; i < 2; ++i) mbar_init(bar(L::kODone + i), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(L::kODone + i), 1);
+            mbar_init(bar(L::kQFull + i), 4);
+            mbar_init(bar(L::kDrain + i), 1);
+        }
         for (int i = 0; i < kConstSlots; ++i) mbar_init(bar(L::kConstFull + i), kExpandWarps);
-        mbar_init(bar(L::kQFull), kSoftmaxWarps);
         mbar_init(bar(L::kQmax), kSoftmaxWarps);
-        mbar_init(bar(L::kDrain), 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(L::kPieceFull + i), 1);
-            mbar_init(bar(L::kPieceEmpty + i), kSoftmaxWarps + kExpandWarps + 1);
+            mbar_init(bar(L::kPieceEmpty + i), kSoftmaxWarps + kExpandWarps + 2);
         }
         ctl->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -412,9 +415,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     __syncthreads();
     const uint32_t tmem_s = tmem, tmem_o = tmem + 256;
 
-    // 128 registers per thread at launch, split anew among the four warpgroups: 2 x 176 + 88 + 72 = 4 x 128
+    // 96 registers per thread at launch, split anew among the five warpgroups: 2 x 136 + 2 x 72 + 64 = 5 x 96
     if (warp < kSoftmaxWarps) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
         // ------------------------------------------------------------------ softmax: a thread per row
         const int w = warp >> 2, r = tid;                  // row tile, row of the 256
         const uint32_t quarter = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes of tensor memory
@@ -479,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 }
                 fence_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(L::kQFull));
+                if (lane == 0) mbar_arrive(bar(L::kQFull + w));
                 // rows of this warp's tile: what all of them see
                 const int t_first = sc.group.div(pc.tile * kRows + w * 128);
                 const int t_last = sc.group.div(pc.tile * kRows + max(w * 128, min(pc.rows, w * 128 + 128) - 1));
@@ -537,8 +540,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                         top1 = fmaxf(top1, fmaxf(x2, x3));
                     }
                     const float top = fmaxf(top0, top1);
-                    // the product of the unit before (every one is waited for in turn: the barrier knows one phase)
-                    if (u > 0 && !(ok = wait_warp(bar(L::kODone + w), (unit_no + 1) & 1, ctl, sc.sb, kWaitSite + 3))) break;
+                    bool behind = u > 0;                     // the product of the unit before has not been waited for
                     const bool fresh = m == kNoReference;
                     const bool over = top > (fresh ? kNoReference : m + kSlack);
                     if (__any_sync(0xffffffffu, over)) {     // move the reference and scale what has been summed
@@ -547,6 +549,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                         m = to;
                         l *= keep;
                         if (u > 0) {
+                            if (!(ok = wait_warp(bar(L::kODone + w), (unit_no + 1) & 1, ctl, sc.sb, kWaitSite + 3))) break;
+                            behind = false;
                             fence_after();
 #pragma unroll 1
                             for (int c = 0; c < D / 32; ++c) {
@@ -579,6 +583,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     }
                     tmem_store32(s_addr, pk);
                     tmem_store_wait();
+                    // every product is waited for in turn (the barrier knows one phase), as late as can be
+                    if (behind && !(ok = wait_warp(bar(L::kODone + w), (unit_no + 1) & 1, ctl, sc.sb, kWaitSite + 3))) break;
                     fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(L::kPReady + 2 * w + (unit_no & 1)));
@@ -677,10 +683,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             if (lane == 0) sc.counters[w0 * kSoftmaxWarps + warp] = 0;       // ready for the next call
         }
     } else if (warp < kMmaWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // ------------------------------------------------------------------ expansion of the codes
-        const int id = tid - 32 * kSoftmaxWarps, tk = id & (kUnit - 1), half = id >> kUnitShift, group32 = (warp - kSoftmaxWarps) & 1;
-        constexpr int KV4 = D / 64;                        // 16-byte pieces of half a token's key codes
+        const int id = tid - 32 * kSoftmaxWarps, tk = id & (kUnit - 1), quarter = id >> kUnitShift, group32 = (warp - kSoftmaxWarps) & 1;
+        constexpr int KW = D / 32;                         // words of a quarter of a token's key codes
         constexpr int CB = D / 16;                         // bytes of a value slice
         ExpandConsts ek = {kNibble, kMinusEight};
         asm volatile("" : "+r"(ek.nibble), "+r"(ek.minus_eight));
@@ -708,24 +714,29 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 }
                 return page;
             };
-            uint4 kc[KV4];
-            uint32_t vc[4][CB / 4], kw = 0, vw = 0;
+            uint32_t kc[KW];
+            uint32_t vc[2][CB / 4], kw = 0, vw = 0;
             auto block_of = [&](int u, int page) {         // this thread's block of unit u
                 const int blk = min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block);
                 return head_base + (size_t)page * page_bytes + (size_t)(blk & in_page) * (16 * (D + 8));
             };
             const int t = tk & 15;
             auto fetch_keys = [&](const uint8_t *p) {
-                const uint4 *k4 = reinterpret_cast<const uint4 *>(p + t * (D / 2) + half * (D / 4));
-#pragma unroll
-                for (int k = 0; k < KV4; ++k) kc[k] = __ldg(k4 + k);
+                const uint8_t *q = p + t * (D / 2) + quarter * (D / 8);
+                if constexpr (KW == 4) {
+                    const uint4 x = __ldg(reinterpret_cast<const uint4 *>(q));
+                    kc[0] = x.x; kc[1] = x.y; kc[2] = x.z; kc[3] = x.w;
+                } else {
+                    const uint2 x = __ldg(reinterpret_cast<const uint2 *>(q));
+                    kc[0] = x.x; kc[1] = x.y;
+                }
                 kw = __ldg(reinterpret_cast<const uint32_t *>(p + 16 * D + 4 * t));
                 vw = __ldg(reinterpret_cast<const uint32_t *>(p + 16 * D + 64 + 4 * t));
             };
             auto fetch_values = [&](const uint8_t *p) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint8_t *q = p + 8 * D + (((t >> 3) * 8 + half * 4 + k) * 8 + (t & 7)) * CB;
+                for (int k = 0; k < 2; ++k) {
+                    const uint8_t *q = p + 8 * D + (((t >> 3) * 8 + quarter * 2 + k) * 8 + (t & 7)) * CB;
                     if constexpr (CB == 8) {
                         const uint2 x = __ldg(reinterpret_cast<const uint2 *>(q));
                         vc[k][0] = x.x;
@@ -767,12 +778,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 {
                     const uint32_t off = (kw & 15u) * 0x00400040u + 0x48004800u;
 #pragma unroll
-                    for (int k = 0; k < KV4; ++k)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int c = half * (D / 16) + k * 4 + j;
+                    for (int k = 0; k < KW; ++k) {
+                            const int c = quarter * KW + k;
                             uint32_t o[4];
-                            levels((&kc[k].x)[j], off, o);
+                            levels(kc[k], off, o);
                             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + L::kOffK + buf * L::kTile + (c >> 3) * L::kPartBytes + row + (((c & 7) ^ (tk & 7)) << 4)),
                                          "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
                                          : "memory");
@@ -783,7 +792,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(step));
                 const int ev = top ? (int)(top >> 23) - 127 - 10 : 0;
                 float *ks = reinterpret_cast<float *>(smem + L::kOffConst + slot * L::kConstBytes);
-                if (half == 0) {
+                if (quarter == 0) {
                     ks[tk] = there ? __uint_as_float(kw & ~15u) * unit : 0.0f;
                     if (lane == 0) {
                         ks[kUnit + group32] = (float)ev;
@@ -811,10 +820,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     const __half2 hi2 = __half2half2(hi), lo2 = __half2half2(lo);
                     const uint32_t h = *reinterpret_cast<const uint32_t *>(&hi2), q = *reinterpret_cast<const uint32_t *>(&lo2);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
+                    for (int k = 0; k < 2; ++k)
 #pragma unroll
                         for (int j = 0; j < CB / 4; ++j) {
-                            const int c = (half * 4 + k) * (CB / 4) + j;
+                            const int c = (quarter * 2 + k) * (CB / 4) + j;
                             uint32_t o[4];
                             levels(vc[k][j], off, o);
 #pragma unroll
@@ -831,30 +840,34 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             }
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         // ------------------------------------------------------------------ MMA issue
-        if (warp == kMmaWarp && lane == 0) {
+        if (warp < kListWarp && lane == 0) {
+            const int w = warp - kMmaWarp;                 // row tile
             constexpr uint32_t idesc_s = instr_desc(kUnit, 0), idesc_o = instr_desc(D, 1);
             uint32_t unit_no = 0, item_no = 0;
             bool ok = true;
             auto wait = [&](int i, uint32_t parity, int where) {
                 return try_wait(bar(i), parity) || wait_long(bar(i), parity, ctl, sc.sb, kWaitSite + where);
             };
-            auto scores = [&](int w, uint32_t n) {         // S of row tile w for unit number n
-                const uint32_t d = tmem_s + w * 128 + (n & 1) * kUnit;
-                uint32_t q = desc_low(base + w * L::kQTile, 16), k = desc_low(base + L::kOffK + n % kRing * L::kTile, 16);
+            const uint32_t q_tile = desc_low(base + w * L::kQTile, 16), s_tile = tmem_s + w * 128, o_tile = tmem_o + w * D;
+            auto scores = [&](uint32_t n) {                // S of unit number n
+                const uint32_t d = s_tile + (n & 1) * kUnit;
+                uint32_t q = q_tile, k = desc_low(base + L::kOffK + n % kRing * L::kTile, 16);
 #pragma unroll 1
                 for (int part = 0; part < L::kHalves; ++part, q += L::kQPart >> 4, k += L::kPartBytes >> 4) {
 #pragma unroll
                     for (uint32_t x = 0; x < 4; ++x) mma_ss(d, q + 2 * x, k + 2 * x, idesc_s, part + x);
                 }
                 commit(bar(L::kSFull + 2 * w + (n & 1)));
+                commit(bar(L::kKEmpty + n % kRing));
             };
-            auto output = [&](int w, uint32_t n, uint32_t accumulate) {
-                const uint32_t v = desc_low(base + L::kOffV + n % kRing * L::kTile, L::kPartBytes), p = tmem_s + w * 128 + (n & 1) * kUnit;
+            auto output = [&](uint32_t n, uint32_t accumulate) {
+                const uint32_t v = desc_low(base + L::kOffV + n % kRing * L::kTile, L::kPartBytes), p = s_tile + (n & 1) * kUnit;
 #pragma unroll
-                for (uint32_t x = 0; x < kUnit / 16; ++x) mma_ts(tmem_o + w * D, p + 8 * x, v + x * (2048 >> 4), idesc_o, accumulate + x);
+                for (uint32_t x = 0; x < kUnit / 16; ++x) mma_ts(o_tile, p + 8 * x, v + x * (2048 >> 4), idesc_o, accumulate + x);
                 commit(bar(L::kODone + w));
+                commit(bar(L::kVEmpty + n % kRing));
             };
             for (uint32_t piece_no = 0;; ++piece_no) {
                 if (!(ok = wait(L::kPieceFull + (piece_no & 1), (piece_no >> 1) & 1, 14))) break;
@@ -862,40 +875,32 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 if (n < 0) break;
                 mbar_arrive(bar(L::kPieceEmpty + (piece_no & 1)));
                 if (n == 0) continue;
-                if (!(ok = wait(L::kQFull, item_no & 1, 7) && wait(L::kKFull + unit_no % kRing, unit_no / kRing & 1, 8))) break;
+                if (!(ok = wait(L::kQFull + w, item_no & 1, 7) && wait(L::kKFull + unit_no % kRing, unit_no / kRing & 1, 8))) break;
                 fence_after();
-                scores(0, unit_no);
-                scores(1, unit_no);
-                commit(bar(L::kKEmpty + unit_no % kRing));
+                scores(unit_no);
                 // the scores of a unit are computed while the softmax of the one before runs
                 for (int u = 0; u < n; ++u, ++unit_no) {
                     const uint32_t next = unit_no + 1;
                     if (u + 1 < n) {
                         if (!(ok = wait(L::kKFull + next % kRing, next / kRing & 1, 8))) break;
                         fence_after();
-                        scores(0, next);
+                        scores(next);
                     }
-                    if (!(ok = wait(L::kVFull + unit_no % kRing, unit_no / kRing & 1, 9) && wait(L::kPReady + (unit_no & 1), (unit_no >> 1) & 1, 10))) break;
+                    if (!(ok = wait(L::kVFull + unit_no % kRing, unit_no / kRing & 1, 9) &&
+                               wait(L::kPReady + 2 * w + (unit_no & 1), (unit_no >> 1) & 1, 10)))
+                        break;
                     fence_after();
-                    output(0, unit_no, u);
-                    if (u + 1 < n) {
-                        scores(1, next);
-                        commit(bar(L::kKEmpty + next % kRing));
-                    }
-                    if (!(ok = wait(L::kPReady + 2 + (unit_no & 1), (unit_no >> 1) & 1, 11))) break;
-                    fence_after();
-                    output(1, unit_no, u);
-                    commit(bar(L::kVEmpty + unit_no % kRing));
+                    output(unit_no, u);
                 }
                 ++item_no;
             }
             if (!ok) {                                     // nothing of this CTA may still run when it gives its memory back
-                commit(bar(L::kDrain));
+                commit(bar(L::kDrain + w));
                 unsigned long long t0, t;
                 asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
                 do {
                     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-                } while (!try_wait(bar(L::kDrain), 0) && t - t0 < kWaitNs / 10);
+                } while (!try_wait(bar(L::kDrain + w), 0) && t - t0 < kWaitNs / 10);
             }
         }
         if (warp == kListWarp && lane == 0) {
