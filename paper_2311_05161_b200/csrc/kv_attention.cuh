@@ -7,7 +7,7 @@
 namespace w4a8 {
 
 constexpr unsigned long long kWaitNs = 2000000000ull;      // limit of every bounded wait
-constexpr uint32_t kSuspendHintNs = 1000;
+constexpr uint32_t kSuspendHintNs = 20000;                 // a waiting thread is woken when the phase completes; until then it stays out of the issue slots
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoReference = -1.0e30f;
 constexpr float kSlack = 15.0f;                            // weights stay below 2^15, within binary16

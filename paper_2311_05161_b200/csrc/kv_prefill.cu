@@ -106,51 +106,38 @@ __device__ __forceinline__ void tmem_arrived(uint32_t (&r)[32])
                  : "memory");
     asm volatile("" : "+r"(r[30]), "+r"(r[31])::"memory");
 }
-__device__ __forceinline__ void tmem_request16(uint32_t addr, uint32_t (&r)[16])
+// 64 columns of this thread's lane.
+__device__ __forceinline__ void tmem_load64(uint32_t addr, float (&r)[64])
 {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+        "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+          "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]),
+          "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]),
+          "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31]),
+          "=f"(r[32]), "=f"(r[33]), "=f"(r[34]), "=f"(r[35]), "=f"(r[36]), "=f"(r[37]), "=f"(r[38]), "=f"(r[39]),
+          "=f"(r[40]), "=f"(r[41]), "=f"(r[42]), "=f"(r[43]), "=f"(r[44]), "=f"(r[45]), "=f"(r[46]), "=f"(r[47]),
+          "=f"(r[48]), "=f"(r[49]), "=f"(r[50]), "=f"(r[51]), "=f"(r[52]), "=f"(r[53]), "=f"(r[54]), "=f"(r[55]),
+          "=f"(r[56]), "=f"(r[57]), "=f"(r[58]), "=f"(r[59]), "=f"(r[60]), "=f"(r[61]), "=f"(r[62]), "=f"(r[63])
         : "r"(addr)
         : "memory");
 }
-__device__ __forceinline__ void tmem_arrived16(uint32_t (&r)[16])
+__device__ __forceinline__ float max3(float a, float b, float c)
 {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
-                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-                 :
-                 : "memory");
-}
-__device__ __forceinline__ void load_shared_pairs(uint32_t addr, uint64_t &a, uint64_t &b)
-{
-    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr));
-}
-// Pairs of binary32 numbers for the packed instructions.
-__device__ __forceinline__ uint64_t pair_bits(uint32_t lo, uint32_t hi)
-{
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-__device__ __forceinline__ uint64_t pair(float lo, float hi) { return pair_bits(__float_as_uint(lo), __float_as_uint(hi)); }
-__device__ __forceinline__ void unpair(uint64_t v, float &lo, float &hi)
+__device__ __forceinline__ float4 load_shared4(uint32_t addr)
 {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b)
-{
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    return v;
 }
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32])
 {
@@ -187,8 +174,8 @@ struct Layout {
     static constexpr int kOffBars = kOffQmax + 2 * kSoftmaxWarps * 4;
     // barriers
     static constexpr int kKFull = 0, kKEmpty = kKFull + kRing, kVFull = kKEmpty + kRing, kVEmpty = kVFull + kRing,
-                         kConstFull = kVEmpty + kRing, kSFull = kConstFull + kConstSlots, kPReady = kSFull + 4, kODone = kPReady + 4,
-                         kQFull = kODone + 2, kQmax = kQFull + 2, kDrain = kQmax + 1, kPieceFull = kDrain + 2,
+                         kSFull = kVEmpty + kRing, kPReady = kSFull + 4, kODone = kPReady + 4,
+                         kQFull = kODone + 4, kQmax = kQFull + 2, kDrain = kQmax + 1, kPieceFull = kDrain + 2,
                          kPieceEmpty = kPieceFull + 2, kBars = kPieceEmpty + 2;
     static constexpr int kSmem = kOffBars + kBars * 8 + 1024;
     static_assert(kSmem + 1024 <= 232448, "shared memory of an SM");
@@ -353,13 +340,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         for (int i = 0; i < 4; ++i) {          // row tile, score buffer
             mbar_init(bar(L::kSFull + i), 1);
             mbar_init(bar(L::kPReady + i), 4);
+            mbar_init(bar(L::kODone + i), 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(L::kODone + i), 1);
             mbar_init(bar(L::kQFull + i), 4);
             mbar_init(bar(L::kDrain + i), 1);
         }
-        for (int i = 0; i < kConstSlots; ++i) mbar_init(bar(L::kConstFull + i), kExpandWarps);
         mbar_init(bar(L::kQmax), kSoftmaxWarps);
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(L::kPieceFull + i), 1);
@@ -425,6 +411,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         const uint32_t q_row = base + w * L::kQTile + (r & 127) * 128;
         uint32_t unit_no = 0, item_no = 0;
         bool ok = true;
+        // The output product of unit number n.  Its barrier (one per parity of n) knows one phase: the product of
+        // n - 2 went to the tensor cores before the scores of n and is complete when these are here, and that of n + 2
+        // cannot start before this warp has delivered later weights.
+        auto wait_output = [&](uint32_t n) {
+            return wait_warp(bar(L::kODone + 2 * w + (n & 1)), (n >> 1) & 1, ctl, sc.sb, kWaitSite + 3);
+        };
         for (uint32_t piece_no = 0;; ++piece_no) {
             if (!(ok = wait_warp(bar(L::kPieceFull + (piece_no & 1)), (piece_no >> 1) & 1, ctl, sc.sb, kWaitSite + 12))) break;
             const volatile Piece &pc = ctl->piece[piece_no & 1];
@@ -490,57 +482,42 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 int j0 = pc.unit0 * kUnit;
                 for (int u = 0; u < count; ++u, ++unit_no, j0 += kUnit) {
                     const uint32_t slot = unit_no % kConstSlots;
-                    if (!(ok = wait_warp(bar(L::kConstFull + slot), unit_no / kConstSlots & 1, ctl, sc.sb, kWaitSite + 1) &&
-                               wait_warp(bar(L::kSFull + 2 * w + (unit_no & 1)), (unit_no >> 1) & 1, ctl, sc.sb, kWaitSite + 2)))
-                        break;
+                    // (the scores were issued behind the unit's keys, and those behind its constants)
+                    if (!(ok = wait_warp(bar(L::kSFull + 2 * w + (unit_no & 1)), (unit_no >> 1) & 1, ctl, sc.sb, kWaitSite + 2))) break;
                     fence_after();
                     const uint32_t ks_addr = base + L::kOffConst + slot * L::kConstBytes;
                     const volatile float *scale = reinterpret_cast<const float *>(smem + L::kOffConst + slot * L::kConstBytes) + kUnit;   // exponents of the two groups' value scales, then 2^-exponent
                     const uint32_t s_addr = s_base + (unit_no & 1) * kUnit;
                     const bool edge = j0 < lo_max || j0 + kUnit > hi_min;
-                    // exponents of the row's weights, sixteen columns at a time; the next sixteen scores are on their way meanwhile
-                    uint64_t x[kUnit / 2];                   // pairs
-                    {
-                        uint32_t v[2][16];
-                        tmem_request16(s_addr, v[0]);
+                    // exponents of the row's weights.  (Scalar instructions: the packed binary32 ones take as long in the
+                    // pipe, and the register moves that align their operands cost more than they saved.)
+                    float x[kUnit];
+                    tmem_load64(s_addr, x);
 #pragma unroll
-                        for (int c = 0; c < kUnit / 16; ++c) {
-                            tmem_arrived16(v[c & 1]);
-                            if (c < kUnit / 16 - 1) tmem_request16(s_addr + 16 * (c + 1), v[(c + 1) & 1]);
-                            const float e = scale[c >> 1];
-                            const uint64_t shift = pair(e, e);
+                    for (int c = 0; c < kUnit / 32; ++c) {
+                        const float shift = scale[c];
 #pragma unroll
-                            for (int k = 0; k < 16; k += 4) {
-                                uint64_t k0, k1;
-                                load_shared_pairs(ks_addr + 4 * (16 * c + k), k0, k1);
-                                x[8 * c + k / 2] = fma_pair(pair_bits(v[c & 1][k], v[c & 1][k + 1]), k0, shift);
-                                x[8 * c + k / 2 + 1] = fma_pair(pair_bits(v[c & 1][k + 2], v[c & 1][k + 3]), k1, shift);
-                            }
+                        for (int k = 32 * c; k < 32 * c + 32; k += 4) {
+                            const float4 f = load_shared4(ks_addr + 4 * k);
+                            x[k] = fmaf(x[k], f.x, shift);
+                            x[k + 1] = fmaf(x[k + 1], f.y, shift);
+                            x[k + 2] = fmaf(x[k + 2], f.z, shift);
+                            x[k + 3] = fmaf(x[k + 3], f.w, shift);
                         }
                     }
                     if (edge) {
                         const int lo_off = j0 - row_lo;
                         const uint32_t span = (uint32_t)max(row_hi - row_lo, 0);
 #pragma unroll
-                        for (int k = 0; k < kUnit; k += 2) {
-                            float x0, x1;
-                            unpair(x[k / 2], x0, x1);
-                            x0 = (uint32_t)(lo_off + k) < span ? x0 : -INFINITY;
-                            x1 = (uint32_t)(lo_off + k + 1) < span ? x1 : -INFINITY;
-                            x[k / 2] = pair(x0, x1);
-                        }
+                        for (int k = 0; k < kUnit; ++k) x[k] = (uint32_t)(lo_off + k) < span ? x[k] : -INFINITY;
                     }
                     float top0 = -INFINITY, top1 = -INFINITY;
 #pragma unroll
-                    for (int k = 0; k < kUnit / 2; k += 2) {
-                        float x0, x1, x2, x3;
-                        unpair(x[k], x0, x1);
-                        unpair(x[k + 1], x2, x3);
-                        top0 = fmaxf(top0, fmaxf(x0, x1));
-                        top1 = fmaxf(top1, fmaxf(x2, x3));
+                    for (int k = 0; k < kUnit; k += 4) {
+                        top0 = max3(top0, x[k], x[k + 1]);
+                        top1 = max3(top1, x[k + 2], x[k + 3]);
                     }
                     const float top = fmaxf(top0, top1);
-                    bool behind = u > 0;                     // the product of the unit before has not been waited for
                     const bool fresh = m == kNoReference;
                     const bool over = top > (fresh ? kNoReference : m + kSlack);
                     if (__any_sync(0xffffffffu, over)) {     // move the reference and scale what has been summed
@@ -549,8 +526,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                         m = to;
                         l *= keep;
                         if (u > 0) {
-                            if (!(ok = wait_warp(bar(L::kODone + w), (unit_no + 1) & 1, ctl, sc.sb, kWaitSite + 3))) break;
-                            behind = false;
+                            if (!(ok = wait_output(unit_no - 1))) break;
                             fence_after();
 #pragma unroll 1
                             for (int c = 0; c < D / 32; ++c) {
@@ -562,35 +538,28 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                             }
                         }
                     }
-                    const float ref = m == kNoReference ? 0.0f : -m;
-                    const uint64_t ref2 = pair(ref, ref);
+                    const float ref = m == kNoReference ? 0.0f : m;
                     uint32_t pk[kUnit / 2];
 #pragma unroll
                     for (int c = 0; c < kUnit / 32; ++c) {
-                        uint64_t sum = 0ull;                 // (0, 0)
+                        float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
-                        for (int k = 16 * c; k < 16 * c + 16; ++k) {
-                            float x0, x1;
-                            unpair(add_pair(x[k], ref2), x0, x1);
-                            x0 = ex2(x0);
-                            x1 = ex2(x1);
-                            sum = add_pair(sum, pair(x0, x1));
-                            pk[k] = pack_half2(x0, x1);
+                        for (int k = 32 * c; k < 32 * c + 32; k += 2) {
+                            const float x0 = ex2(x[k] - ref), x1 = ex2(x[k + 1] - ref);
+                            sum0 += x0;
+                            sum1 += x1;
+                            pk[k / 2] = pack_half2(x0, x1);
                         }
-                        float s0, s1;
-                        unpair(sum, s0, s1);
-                        l = fmaf(s0 + s1, scale[2 + c], l);  // a group's weights are on its values' scale
+                        l = fmaf(sum0 + sum1, scale[2 + c], l);  // a group's weights are on its values' scale
                     }
                     tmem_store32(s_addr, pk);
                     tmem_store_wait();
-                    // every product is waited for in turn (the barrier knows one phase), as late as can be
-                    if (behind && !(ok = wait_warp(bar(L::kODone + w), (unit_no + 1) & 1, ctl, sc.sb, kWaitSite + 3))) break;
                     fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(L::kPReady + 2 * w + (unit_no & 1)));
                 }
                 if (!ok) break;
-                if (!(ok = wait_warp(bar(L::kODone + w), (unit_no + 1) & 1, ctl, sc.sb, kWaitSite + 3))) break;
+                if (!(ok = (count < 2 || wait_output(unit_no - 2)) && wait_output(unit_no - 1))) break;
                 fence_after();
                 ++item_no;
             }
@@ -690,6 +659,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         constexpr int CB = D / 16;                         // bytes of a value slice
         ExpandConsts ek = {kNibble, kMinusEight};
         asm volatile("" : "+r"(ek.nibble), "+r"(ek.minus_eight));
+        // where this thread's operand pieces go in a tile of keys or values
+        uint32_t place[KW];
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+            const int c = quarter * KW + k;
+            place[k] = base + L::kOffK + (c >> 3) * L::kPartBytes + tk * 128 + (((c & 7) ^ (tk & 7)) << 4);
+        }
         const int page_bits = a.cache.page_shift - 4, in_page = (1 << page_bits) - 1;
         const size_t page_bytes = a.cache.page_bytes();
         uint32_t unit_no = 0, item_no = 0;
@@ -772,17 +748,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             for (int u = 0; u < count; ++u, ++unit_no) {
                 const uint32_t buf = unit_no % kRing, use = unit_no / kRing & 1, slot = unit_no % kConstSlots;
                 const bool there = (unit0 + u) * kUnit + tk < len;
-                const uint32_t row = (uint32_t)tk * 128;
                 // ---- keys ----
                 if (unit_no >= kRing && !(ok = wait_warp(bar(L::kKEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 5))) break;
                 {
                     const uint32_t off = (kw & 15u) * 0x00400040u + 0x48004800u;
 #pragma unroll
                     for (int k = 0; k < KW; ++k) {
-                            const int c = quarter * KW + k;
                             uint32_t o[4];
                             levels(kc[k], off, o);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + L::kOffK + buf * L::kTile + (c >> 3) * L::kPartBytes + row + (((c & 7) ^ (tk & 7)) << 4)),
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place[k] + buf * L::kTile),
                                          "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
                                          : "memory");
                         }
@@ -807,10 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 }
                 fence_async();
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(bar(L::kConstFull + slot));
-                    mbar_arrive(bar(L::kKFull + buf));
-                }
+                if (lane == 0) mbar_arrive(bar(L::kKFull + buf));
                 // ---- values ----
                 if (unit_no >= kRing && !(ok = wait_warp(bar(L::kVEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 6))) break;
                 {
@@ -823,12 +794,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     for (int k = 0; k < 2; ++k)
 #pragma unroll
                         for (int j = 0; j < CB / 4; ++j) {
-                            const int c = (quarter * 2 + k) * (CB / 4) + j;
                             uint32_t o[4];
                             levels(vc[k][j], off, o);
 #pragma unroll
                             for (int x = 0; x < 4; ++x) o[x] = hfma2(o[x], h, hfma2(o[x], q, 0u));   // level * step, rounded once
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + L::kOffV + buf * L::kTile + (c >> 3) * L::kPartBytes + row + (((c & 7) ^ (tk & 7)) << 4)),
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place[k * (CB / 4) + j] + (kRing + buf) * L::kTile),
                                          "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
                                          : "memory");
                         }
@@ -866,7 +836,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 const uint32_t v = desc_low(base + L::kOffV + n % kRing * L::kTile, L::kPartBytes), p = s_tile + (n & 1) * kUnit;
 #pragma unroll
                 for (uint32_t x = 0; x < kUnit / 16; ++x) mma_ts(o_tile, p + 8 * x, v + x * (2048 >> 4), idesc_o, accumulate + x);
-                commit(bar(L::kODone + w));
+                commit(bar(L::kODone + 2 * w + (n & 1)));
                 commit(bar(L::kVEmpty + n % kRing));
             };
             for (uint32_t piece_no = 0;; ++piece_no) {
