@@ -202,16 +202,17 @@ struct Piece {
 struct Control {
     volatile int abort;
     uint32_t tmem;
-    int found_b;
+    int found_b, found_tile;
     long long found_off;
     long long warp_len[kWarps];
     Piece piece[2];
 };
 
-__device__ bool wait_long(uint32_t bar, uint32_t parity, Control *ctl, StatusBlock *sb, int where)
+__device__ bool wait_long(uint32_t bar, uint32_t parity, Control *ctl, StatusBlock *sb, int where, int pause)
 {
     unsigned long long t0 = 0, t;
     for (uint32_t i = 1;; ++i) {
+        if (pause) __nanosleep(pause);
         if (try_wait(bar, parity)) return true;
         if ((i & 63u) == 0u) {
             if (ctl->abort) return false;
@@ -226,9 +227,9 @@ __device__ bool wait_long(uint32_t bar, uint32_t parity, Control *ctl, StatusBlo
     }
 }
 // All lanes of a warp wait and agree on the outcome.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, Control *ctl, StatusBlock *sb, int where)
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, Control *ctl, StatusBlock *sb, int where, int pause = 0)
 {
-    return __all_sync(0xffffffffu, try_wait(bar, parity) || wait_long(bar, parity, ctl, sb, where));
+    return __all_sync(0xffffffffu, try_wait(bar, parity) || wait_long(bar, parity, ctl, sb, where, pause));
 }
 
 // The share of the work list a CTA walks through: the list is, for every sequence, row tile and key
@@ -258,26 +259,25 @@ struct Walk {
         first = sight.lo(i_first) >> kUnitShift;
         units = max(0, ((sight.hi(i_last) + kUnit - 1) >> kUnitShift) - first);
     }
-    // places of one sequence
-    __device__ static long long length_of(const KvAttnArgs &a, const Schedule &sc, int b)
+    // Places of the row tiles first_tile + lane of a sequence (0 behind the last).
+    __device__ static long long tile_places(const KvAttnArgs &a, const Schedule &sc, const Seq &s, int t)
     {
-        const Seq s = load_seq(a, b, sc.sb);
-        const int tiles = tiles_of(s, (int)sc.group.d);
-        long long n = 0;
-        for (int t = 0; t < tiles; ++t) {
-            int i0, i1, rows, first, units;
-            span(a, sc, s, t, i0, i1, rows, first, units);
-            n += (long long)a.cache.heads * (kLead + max(units, 1));
-        }
-        return n;
+        if (t >= tiles_of(s, (int)sc.group.d)) return 0;
+        int i0, i1, rows, first, units;
+        span(a, sc, s, t, i0, i1, rows, first, units);
+        return (long long)a.cache.heads * (kLead + max(units, 1));
     }
-    __device__ void start(int b0, long long off0, long long begin, long long end_)
+    __device__ void start(int b0, int tile0, long long off0, long long begin, long long end_)
     {
         b = b0;
+        tile = tile0;
         off = off0;
         at = begin;
         end = end_;
-        tile = 0;
+        if (at < end) {
+            s = load_seq(a, b, sc.sb);
+            loaded = true;
+        }
     }
     // Moves to the next piece with at least one unit (or the one place of an item without units).
     __device__ bool next()
@@ -362,40 +362,52 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     allow_dependents();
     dependent_wait();
 
-    // ---- this CTA's share of the list ----
+    // ---- this CTA's share of the list: a warp takes a run of sequences, its lanes their row tiles ----
     const int batch = a.batch.batch;
-    const int chunk = (batch + kThreads - 1) / kThreads;
-    const int b_first = min(batch, tid * chunk), b_last = min(batch, b_first + chunk);
+    const int chunk = (batch + kWarps - 1) / kWarps;
+    const int b_first = min(batch, warp * chunk), b_last = min(batch, b_first + chunk);
     long long mine = 0;
-    for (int b = b_first; b < b_last; ++b) mine += Walk::length_of(a, sc, b);
-    long long incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
+    for (int b = b_first; b < b_last; ++b) {
+        const Seq s = load_seq(a, b, sc.sb);
+        const int tiles = Walk::tiles_of(s, (int)sc.group.d);
+        for (int t = 0; t < tiles; t += 32) mine += Walk::tile_places(a, sc, s, t + lane);
     }
-    if (lane == 31) ctl->warp_len[warp] = incl;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (lane == 0) ctl->warp_len[warp] = mine;
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = ctl->tmem;
-    long long total = 0;
+    long long total = 0, before = 0;
     for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) incl += ctl->warp_len[w];
+        if (w < warp) before += ctl->warp_len[w];
         total += ctl->warp_len[w];
     }
     const long long per = max(quotient(total + gridDim.x - 1, gridDim.x), 4ll);
     const long long begin = (long long)blockIdx.x * per, end = min(total, begin + per);
-    if (begin < total && begin >= incl - mine && begin < incl) {
-        long long at = incl - mine;
-        for (int b = b_first; b < b_last; ++b) {
-            const long long n = Walk::length_of(a, sc, b);
-            if (begin < at + n) {
-                ctl->found_b = b;
-                ctl->found_off = begin - at;
-                break;
+    if (begin < total && begin >= before && begin < before + mine) {
+        long long at = before;
+        bool found = false;
+        for (int b = b_first; b < b_last && !found; ++b) {
+            const Seq s = load_seq(a, b, sc.sb);
+            const int tiles = Walk::tiles_of(s, (int)sc.group.d);
+            for (int t = 0; t < tiles && !found; t += 32) {
+                const long long n = Walk::tile_places(a, sc, s, t + lane);
+                long long upto = n;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+                    if (lane >= o) upto += v;
+                }
+                if (begin >= at + upto - n && begin < at + upto) {
+                    ctl->found_b = b;
+                    ctl->found_tile = t + lane;
+                    ctl->found_off = begin - (at + upto - n);
+                }
+                at += __shfl_sync(0xffffffffu, upto, 31);
+                found = begin < at;
             }
-            at += n;
         }
     }
     __syncthreads();
@@ -568,6 +580,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             float *part = sc.partials + ((size_t)blockIdx.x * 2 + pc.slot) * (kRows * (D + 2));
             const float inv = l > 0.0f ? __fdiv_rn(-2.0f, l) : 0.0f;
             const size_t out_at = ((size_t)(s.row0 + i) * a.q_heads + head) * D;
+            // place of this thread's first four columns in a part, in quads: [warp][quad of columns][lane]
+            const int quads_at = warp * (D / 4) * 32 + lane;
             auto store8 = [&](int d, const float (&x)[8]) {          // eight elements in their order
                 uint4 o;
 #pragma unroll
@@ -592,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 if (!mine_only) {
 #pragma unroll
                     for (int k = 0; k < 32; k += 4)
-                        __stcg(reinterpret_cast<uint4 *>(part + 2 * kRows + (size_t)r * D + 32 * c + k), make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]));
+                        __stcg(reinterpret_cast<uint4 *>(part + 2 * kRows) + quads_at + (8 * c + k / 4) * 32, make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]));
                 } else if (in) {
 #pragma unroll
                     for (int k = 0; k < 32; k += 8) {        // columns hold the elements 0, 4, 1, 5, 2, 6, 3, 7 of eight
@@ -631,22 +645,35 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 lsum += __ldcg(x + kRows + r) * ex2(__ldcg(x + r) - top);
             }
             const float join_inv = lsum > 0.0f ? __fdiv_rn(-2.0f, lsum) : 0.0f;
-            if (in) {
-                for (int c = 0; c < D; c += 8) {
-                    float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-                    for (int k = 0; k < parts; ++k) {
-                        const float *x = k == 0 ? head_part : rest + (size_t)k * 2 * part_size;
-                        const float f = ex2(__ldcg(x + r) - top);
-                        const float4 y0 = __ldcg(reinterpret_cast<const float4 *>(x + 2 * kRows + (size_t)r * D + c));
-                        const float4 y1 = __ldcg(reinterpret_cast<const float4 *>(x + 2 * kRows + (size_t)r * D + c) + 1);
-                        acc[0] += y0.x * f; acc[4] += y0.y * f; acc[1] += y0.z * f; acc[5] += y0.w * f;
-                        acc[2] += y1.x * f; acc[6] += y1.y * f; acc[3] += y1.z * f; acc[7] += y1.w * f;
-                    }
+            constexpr int kCols = 64;        // columns at a time: their loads are all in flight together
+#pragma unroll 1
+            for (int c = 0; c < D; c += kCols) {
+                float acc[kCols];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) acc[k] *= join_inv;
-                    store8(c, acc);
+                for (int k = 0; k < kCols; ++k) acc[k] = 0.0f;
+#pragma unroll 1
+                for (int k = 0; k < parts; ++k) {
+                    const float *x = k == 0 ? head_part : rest + (size_t)k * 2 * part_size;
+                    const float f = ex2(__ldcg(x + r) - top) * join_inv;
+                    const float4 *from = reinterpret_cast<const float4 *>(x + 2 * kRows) + quads_at + c / 4 * 32;
+#pragma unroll
+                    for (int q = 0; q < kCols / 4; ++q) {
+                        const float4 y = __ldcg(from + q * 32);
+                        acc[4 * q] = fmaf(y.x, f, acc[4 * q]);
+                        acc[4 * q + 1] = fmaf(y.y, f, acc[4 * q + 1]);
+                        acc[4 * q + 2] = fmaf(y.z, f, acc[4 * q + 2]);
+                        acc[4 * q + 3] = fmaf(y.w, f, acc[4 * q + 3]);
+                    }
                 }
+                if (in) {
+#pragma unroll
+                    for (int k = 0; k < kCols; k += 8) {
+                        const float y[8] = {acc[k], acc[k + 2], acc[k + 4], acc[k + 6], acc[k + 1], acc[k + 3], acc[k + 5], acc[k + 7]};
+                        store8(c + k, y);
+                    }
+                }
+            }
+            if (in) {
                 if (a.lse) a.lse[out_at / D] = lsum > 0.0f ? (top + lg2(lsum)) * kLn2 : -INFINITY;
             }
             if (lane == 0) sc.counters[w0 * kSoftmaxWarps + warp] = 0;       // ready for the next call
@@ -749,7 +776,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 const uint32_t buf = unit_no % kRing, use = unit_no / kRing & 1, slot = unit_no % kConstSlots;
                 const bool there = (unit0 + u) * kUnit + tk < len;
                 // ---- keys ----
-                if (unit_no >= kRing && !(ok = wait_warp(bar(L::kKEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 5))) break;
+                if (unit_no >= kRing && !(ok = wait_warp(bar(L::kKEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 5, 200))) break;
                 {
                     const uint32_t off = (kw & 15u) * 0x00400040u + 0x48004800u;
 #pragma unroll
@@ -783,7 +810,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(L::kKFull + buf));
                 // ---- values ----
-                if (unit_no >= kRing && !(ok = wait_warp(bar(L::kVEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 6))) break;
+                if (unit_no >= kRing && !(ok = wait_warp(bar(L::kVEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 6, 200))) break;
                 {
                     const uint32_t off = (value_word & 15u) * 0x00400040u + 0x48004800u;
                     const float vs = step * __uint_as_float((uint32_t)(127 - ev) << 23);
@@ -818,7 +845,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             uint32_t unit_no = 0, item_no = 0;
             bool ok = true;
             auto wait = [&](int i, uint32_t parity, int where) {
-                return try_wait(bar(i), parity) || wait_long(bar(i), parity, ctl, sc.sb, kWaitSite + where);
+                return try_wait(bar(i), parity) || wait_long(bar(i), parity, ctl, sc.sb, kWaitSite + where, 0);
             };
             const uint32_t q_tile = desc_low(base + w * L::kQTile, 16), s_tile = tmem_s + w * 128, o_tile = tmem_o + w * D;
             auto scores = [&](uint32_t n) {                // S of unit number n
@@ -876,11 +903,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         if (warp == kListWarp && lane == 0) {
             // -------------------------------------------------------------- the pieces of this CTA's share
             Walk walk(a, sc);
-            walk.start(ctl->found_b, ctl->found_off, begin, max(begin, end));
+            walk.start(ctl->found_b, ctl->found_tile, ctl->found_off, begin, max(begin, end));
             for (uint32_t piece_no = 0;; ++piece_no) {
                 const bool more = walk.next();
                 if (piece_no >= 2 && !try_wait(bar(L::kPieceEmpty + (piece_no & 1)), (piece_no >> 1 & 1) ^ 1) &&
-                    !wait_long(bar(L::kPieceEmpty + (piece_no & 1)), (piece_no >> 1 & 1) ^ 1, ctl, sc.sb, kWaitSite + 15))
+                    !wait_long(bar(L::kPieceEmpty + (piece_no & 1)), (piece_no >> 1 & 1) ^ 1, ctl, sc.sb, kWaitSite + 15, 1000))
                     break;
                 Piece p = {};
                 p.count = -1;
