@@ -42,25 +42,6 @@ struct KvCache {
     }
 };
 
-// Sequence of a row: the number of entries among cu_rows[1 .. batch] that are <= row (batch for a
-// row behind the last sequence).  All lanes of a warp call it with the same row; every step probes
-// 32 places at once, so a batch of 1024 takes two dependent loads.
-__device__ __forceinline__ int kv_sequence_of(const KvBatch &bt, int row)
-{
-    if (!bt.cu_rows) return row;
-    const int lane = threadIdx.x & 31;
-    int lo = 0, n = bt.batch;                // answer in [lo, lo + n]
-    while (n > 0) {
-        const int step = (n + 31) >> 5;
-        const int at = lo + (lane + 1) * step;              // is cu_rows[at] <= row ?
-        const bool le = at <= lo + n && __ldg(bt.cu_rows + at) <= row;
-        const int k = __popc(__ballot_sync(0xffffffffu, le));
-        lo += k * step;
-        n = min(step - 1, n - k * step);
-    }
-    return lo;
-}
-
 // Position of row `row` of sequence b; `ok` false when the length or the offsets make no sense.
 __device__ __forceinline__ int kv_position_of(const KvBatch &bt, int b, int row, bool &ok)
 {
@@ -111,35 +92,45 @@ __device__ __forceinline__ uint32_t kv_range_word(float lo, float hi, float &r, 
     return bits | (uint32_t)z;
 }
 
-// Rank of x: Eq. 5 with the levels in ascending order.
-__device__ __forceinline__ uint32_t kv_rank(float x, float r, int z)
+// Eight consecutive elements as a code word: Eq. 5, the levels numbered in ascending order.  With u = x r, the place y
+// of a level counted from zero is 0 for |u| <= 1/4, +-1 for |u| <= 3/4 (the specials) and
+// +-(rint|u| + 1) beyond; the rank is y + z + 1.  The clamp of Eq. 5 acts at the upper end only: the least element's u is
+// -z before rounding.  Rounding and conversion are additions of 1.5 * 2^23, which leave the integer in the
+// mantissa's low bits (the constant's own low 16 bits are zero).
+__device__ __forceinline__ uint32_t kv_rank_bits(float x, float r, float top, float bias)
 {
-    const float u = __fmul_rn(x, r), a = fabsf(u);
-    int l = (int)rintf(u);
-    l = min(max(l, -z), 13 - z);
-    l += (l > 0) - (l < 0);
-    if (a > 0.25f && a <= 0.75f) l = u > 0.0f ? 1 : -1;
-    return (uint32_t)(l + z + 1);
+    const float u = __fmul_rn(x, r);
+    float y = __fadd_rn(__fadd_rn(fabsf(u), 12582912.0f), -12582911.0f);
+    y = fabsf(u) > 0.75f ? y : 1.0f;
+    y = fabsf(u) > 0.25f ? y : 0.0f;
+    return __float_as_uint(__fadd_rn(fminf(copysignf(y, u), top), bias));
+}
+__device__ __forceinline__ uint32_t kv_code_word(const float (&x)[8], float r, int z)
+{
+    const float top = (float)(14 - z), bias = 12582913.0f + (float)z;
+    uint32_t k[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k[i] = kv_rank_bits(x[i], r, top, bias);
+    const uint32_t lo = (k[3] * 16u + k[2]) * 256u + (k[1] * 16u + k[0]);
+    const uint32_t hi = (k[7] * 16u + k[6]) * 256u + (k[5] * 16u + k[4]);
+    const uint32_t w = __byte_perm(lo, hi, 0x5410);
+    return ((w << 2) & 0xFFFCFFFCu) | ((w >> 14) & 0x00030003u);         // both halves rotated left by two
 }
 
-// Level of a rank in units of the step.
-__device__ __forceinline__ float kv_level(uint32_t rank, int z)
+// The eight levels of a code word, halved: pair k holds elements k and k + 4.  (x = rank - z - 1;
+// level / 2 = (x + 1) / 2 - sat(x / 4 + 1/2), packed binary16, exact.)
+__device__ __forceinline__ void kv_levels(uint32_t w, int z, __half2 (&o)[4])
 {
-    const float y = (float)((int)rank - z - 1);
-    return y - fminf(fmaxf(0.5f * y, -1.0f), 1.0f);
-}
-
-// The eight ranks of a code word in element order, and back.
-__device__ __forceinline__ uint32_t kv_half(uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3)
-{
-    const uint32_t h = r0 | (r1 << 4) | (r2 << 8) | (r3 << 12);
-    return ((h << 2) | (h >> 14)) & 0xffffu;
-}
-__device__ __forceinline__ uint32_t kv_rank_at(uint32_t w, int e)
-{
-    const uint32_t h = e < 4 ? (w & 0xffffu) : (w >> 16);
-    const uint32_t n = (h >> 2) | (h << 14);
-    return (n >> (4 * (e & 3))) & 15u;
+    const uint32_t off = (uint32_t)z * 0x00400040u + 0x48004800u;        // (16 + z) / 2 twice
+    const uint32_t sw = __byte_perm(w, w, 0x2301);
+    const uint32_t bits[4] = {w << 4, w, sw << 4, sw};
+    const __half2 minus_half = __float2half2_rn(-0.5f), quarter = __float2half2_rn(0.25f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t lin = (bits[k] & 0x03C003C0u) | 0xC800C800u;      // -(16 + rank) / 2
+        const __half2 x = __hadd2(*reinterpret_cast<const __half2 *>(&lin), *reinterpret_cast<const __half2 *>(&off));
+        o[k] = __hsub2(__hneg2(x), __hfma2_sat(x, minus_half, quarter));
+    }
 }
 
 cudaError_t launch_kv_append(const void *K, const void *V, int bf16, long long k_stride,
