@@ -28,8 +28,6 @@
 // workspace and the last of them to finish joins all parts in list order, so the result does not
 // depend on who is last.  Inside a CTA the warps take blocks in turn, each with its own ring of
 // bulk copies.
-#include <atomic>
-
 #include "kv_attention.cuh"
 
 namespace w4a8 {
@@ -650,19 +648,13 @@ bool use_prefill(int rows, int batch, int q_heads, int kv_heads)
     return (long long)(q_heads / kv_heads) * rows >= 96ll * batch;
 }
 
-constexpr int kMaxDevices = 64;
-
 template <int D, int NT, int WARPS>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
 {
     using S = Shape<D, NT, WARPS>;
-    static std::atomic<bool> ready[kMaxDevices];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices || !ready[dev].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(kv_decode_kernel<D, NT, WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-        if (e != cudaSuccess) return e;
-        if (dev >= 0 && dev < kMaxDevices) ready[dev].store(true, std::memory_order_release);
-    }
+    static std::atomic<int> raised[kMaxDevices];
+    const cudaError_t e = raise_smem_limit(kv_decode_kernel<D, NT, WARPS>, S::kSmem, raised);
+    if (e != cudaSuccess) return e;
     return launch_overlapped(kv_decode_kernel<D, NT, WARPS>, dim3(ctas), dim3(WARPS * 32), S::kSmem, st, a, sc);
 }
 template <int D>

@@ -24,7 +24,6 @@
 // Bounds per unit and SM for D = 128: 2048 cycles of MMA (two 128 x 128 x 128 products per row
 // tile), 2048 cycles of exponentials at 16 per cycle, about 1000 cycles of packed binary16 arithmetic to
 // expand 32768 codes: the expansion is shared by 256 rows, which is why the two tiles are one CTA's.
-#include <atomic>
 #include <type_traits>
 
 #include "kv_attention.cuh"
@@ -943,18 +942,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     }
 }
 
-constexpr int kMaxDevices = 64;
-
 template <int D>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
 {
-    static std::atomic<bool> ready[kMaxDevices];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices || !ready[dev].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(kv_prefill_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D>::kSmem);
-        if (e != cudaSuccess) return e;
-        if (dev >= 0 && dev < kMaxDevices) ready[dev].store(true, std::memory_order_release);
-    }
+    static std::atomic<int> raised[kMaxDevices];
+    const cudaError_t e = raise_smem_limit(kv_prefill_kernel<D>, Layout<D>::kSmem, raised);
+    if (e != cudaSuccess) return e;
     return launch_overlapped(kv_prefill_kernel<D>, dim3(ctas), dim3(kThreads), Layout<D>::kSmem, st, a, sc);
 }
 
