@@ -461,8 +461,7 @@ w4a8_status w4a8_kv_read(const void *cache, int num_pages, int page_size, int kv
  *   lse        out [rows][q_heads] FP32, natural logarithm of the softmax's denominator
  *              (-inf for a row that sees no key), or NULL.
  * Precision: scores, maxima and sums in binary32; the weights p enter the value product in
- * binary16, and so do the values where there are many rows per sequence (96 rows x heads per key
- * head and more, on average: the tensor-core kernel with operands in shared memory).  The result does not depend on how the work was scheduled.
+ * binary16.  The result does not depend on how the work was scheduled.
  *   workspace >= w4a8_kv_attention_workspace_bytes(rows, batch, q_heads, kv_heads, D). */
 size_t w4a8_kv_attention_workspace_bytes(int rows, int batch, int q_heads, int kv_heads,
                                          int head_dim);

@@ -48,12 +48,6 @@ __device__ __forceinline__ void copy_block(uint32_t dst, const uint8_t *src, uin
                  : "memory");
 }
 
-__device__ __forceinline__ float rcp(float x)
-{
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ uint32_t transpose8(uint32_t v)
 {
     uint32_t d;

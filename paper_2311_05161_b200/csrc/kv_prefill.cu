@@ -14,12 +14,12 @@
 // softmax warps, twice what the MMAs take); one lists the pieces of work.  Twenty warps in all.
 // Every hand-over is an mbarrier with a bounded wait; a wait that runs out raises a flag that ends all roles.
 //
-// Numbers: key operands are exact levels (times -1/2), the step of a token multiplies its score column.
-// Value operands are level * step, rounded once to binary16, on a power-of-two scale per 32 tokens that
-// the weights' exponents take back.  A thread looks over its row's 128 scores for their maximum first; where a
-// weight would exceed 2^15 against the running reference, it moves the reference and scales the output row
-// in tensor memory.  (One pass that computed the weights at once and again after an overflow was slower:
-// on scores that spread over five bits one unit in eight overflowed in some row of a warp.)
+// Numbers: both operands are exact levels (times -1/2).  A token's key step multiplies its score column; its value
+// step enters the weight's exponent, as in the decode form, so that the weights' rounding to binary16 is the
+// only one.  A thread looks over its row's scores for their maximum first; where a weight would exceed 2^15
+// against the running reference, it moves the reference and scales the output row in tensor memory.  (One
+// pass that computed the weights at once and again after an overflow was slower: on scores that spread
+// over five bits one unit in eight overflowed in some row of a warp.)
 //
 // Bounds per unit and SM for D = 128: 2048 cycles of MMA (two 128 x 128 x 128 products per row
 // tile), 2048 cycles of exponentials at 16 per cycle, about 1000 cycles of packed binary16 arithmetic to
@@ -168,7 +168,7 @@ struct Layout {
     static constexpr int kPartBytes = kUnit * 128, kTile = kHalves * kPartBytes; // a unit's keys or values
     static constexpr int kOffK = 2 * kQTile, kOffV = kOffK + kRing * kTile;
     static constexpr int kOffConst = kOffV + kRing * kTile;
-    static constexpr int kConstBytes = kUnit * 4 + 16;     // step * unit per token; two groups' scale exponents and powers
+    static constexpr int kConstBytes = kUnit * 12;         // per token: key step * unit; log2 of the value step; its inverse
     static constexpr int kOffQmax = kOffConst + kConstSlots * kConstBytes;
     static constexpr int kOffBars = kOffQmax + 2 * kSoftmaxWarps * 4;
     // barriers
@@ -497,7 +497,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     if (!(ok = wait_warp(bar(L::kSFull + 2 * w + (unit_no & 1)), (unit_no >> 1) & 1, ctl, sc.sb, kWaitSite + 2))) break;
                     fence_after();
                     const uint32_t ks_addr = base + L::kOffConst + slot * L::kConstBytes;
-                    const volatile float *scale = reinterpret_cast<const float *>(smem + L::kOffConst + slot * L::kConstBytes) + kUnit;   // exponents of the two groups' value scales, then 2^-exponent
                     const uint32_t s_addr = s_base + (unit_no & 1) * kUnit;
                     const bool edge = j0 < lo_max || j0 + kUnit > hi_min;
                     // exponents of the row's weights.  (Scalar instructions: the packed binary32 ones take as long in the
@@ -505,16 +504,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     float x[kUnit];
                     tmem_load64(s_addr, x);
 #pragma unroll
-                    for (int c = 0; c < kUnit / 32; ++c) {
-                        const float shift = scale[c];
-#pragma unroll
-                        for (int k = 32 * c; k < 32 * c + 32; k += 4) {
-                            const float4 f = load_shared4(ks_addr + 4 * k);
-                            x[k] = fmaf(x[k], f.x, shift);
-                            x[k + 1] = fmaf(x[k + 1], f.y, shift);
-                            x[k + 2] = fmaf(x[k + 2], f.z, shift);
-                            x[k + 3] = fmaf(x[k + 3], f.w, shift);
-                        }
+                    for (int k = 0; k < kUnit; k += 4) {
+                        const float4 f = load_shared4(ks_addr + 4 * k), g = load_shared4(ks_addr + 4 * (kUnit + k));
+                        x[k] = fmaf(x[k], f.x, g.x);
+                        x[k + 1] = fmaf(x[k + 1], f.y, g.y);
+                        x[k + 2] = fmaf(x[k + 2], f.z, g.z);
+                        x[k + 3] = fmaf(x[k + 3], f.w, g.w);
                     }
                     if (edge) {
                         const int lo_off = j0 - row_lo;
@@ -551,18 +546,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     }
                     const float ref = m == kNoReference ? 0.0f : m;
                     uint32_t pk[kUnit / 2];
+                    float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
-                    for (int c = 0; c < kUnit / 32; ++c) {
-                        float sum0 = 0.0f, sum1 = 0.0f;
-#pragma unroll
-                        for (int k = 32 * c; k < 32 * c + 32; k += 2) {
-                            const float x0 = ex2(x[k] - ref), x1 = ex2(x[k + 1] - ref);
-                            sum0 += x0;
-                            sum1 += x1;
-                            pk[k / 2] = pack_half2(x0, x1);
-                        }
-                        l = fmaf(sum0 + sum1, scale[2 + c], l);  // a group's weights are on its values' scale
+                    for (int k = 0; k < kUnit; k += 4) {
+                        const float4 g = load_shared4(ks_addr + 4 * (2 * kUnit + k));
+                        const float x0 = ex2(x[k] - ref), x1 = ex2(x[k + 1] - ref), x2 = ex2(x[k + 2] - ref), x3 = ex2(x[k + 3] - ref);
+                        sum0 = fmaf(x0, g.x, sum0);
+                        sum1 = fmaf(x1, g.y, sum1);
+                        sum0 = fmaf(x2, g.z, sum0);
+                        sum1 = fmaf(x3, g.w, sum1);
+                        pk[k / 2] = pack_half2(x0, x1);
+                        pk[k / 2 + 1] = pack_half2(x2, x3);
                     }
+                    l += sum0 + sum1;
                     tmem_store32(s_addr, pk);
                     tmem_store_wait();
                     fence_before();
@@ -680,7 +676,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     } else if (warp < kMmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // ------------------------------------------------------------------ expansion of the codes
-        const int id = tid - 32 * kSoftmaxWarps, tk = id & (kUnit - 1), quarter = id >> kUnitShift, group32 = (warp - kSoftmaxWarps) & 1;
+        const int id = tid - 32 * kSoftmaxWarps, tk = id & (kUnit - 1), quarter = id >> kUnitShift;
         constexpr int KW = D / 32;                         // words of a quarter of a token's key codes
         constexpr int CB = D / 16;                         // bytes of a value slice
         ExpandConsts ek = {kNibble, kMinusEight};
@@ -787,17 +783,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                                          : "memory");
                         }
                 }
-                // the value steps' largest in these 32 tokens gives their scale: steps below 2^11 after it
-                const float step = there ? __uint_as_float(vw & ~15u) : 0.0f;
-                const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(step));
-                const int ev = top ? (int)(top >> 23) - 127 - 10 : 0;
-                float *ks = reinterpret_cast<float *>(smem + L::kOffConst + slot * L::kConstBytes);
-                if (quarter == 0) {
-                    ks[tk] = there ? __uint_as_float(kw & ~15u) * unit : 0.0f;
-                    if (lane == 0) {
-                        ks[kUnit + group32] = (float)ev;
-                        ks[kUnit + 2 + group32] = __uint_as_float((uint32_t)(127 - ev) << 23);
-                    }
+                if (quarter == 0) {                        // (a token behind the end weighs nothing)
+                    float *ks = reinterpret_cast<float *>(smem + L::kOffConst + slot * L::kConstBytes) + tk;
+                    const float step = __uint_as_float(vw & ~15u);
+                    ks[0] = there ? __uint_as_float(kw & ~15u) * unit : 0.0f;
+                    ks[kUnit] = there ? lg2(step) : -INFINITY;
+                    ks[2 * kUnit] = there ? rcp(step) : 0.0f;
                 }
                 const uint32_t value_word = vw;
                 if (u + 1 < count) {                       // the next unit's keys travel while the values are expanded
@@ -812,18 +803,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 if (unit_no >= kRing && !(ok = wait_warp(bar(L::kVEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 6, 200))) break;
                 {
                     const uint32_t off = (value_word & 15u) * 0x00400040u + 0x48004800u;
-                    const float vs = step * __uint_as_float((uint32_t)(127 - ev) << 23);
-                    const __half hi = __float2half_rn(vs), lo = __float2half_rn(vs - __half2float(hi));
-                    const __half2 hi2 = __half2half2(hi), lo2 = __half2half2(lo);
-                    const uint32_t h = *reinterpret_cast<const uint32_t *>(&hi2), q = *reinterpret_cast<const uint32_t *>(&lo2);
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
 #pragma unroll
                         for (int j = 0; j < CB / 4; ++j) {
                             uint32_t o[4];
                             levels(vc[k][j], off, o);
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) o[x] = hfma2(o[x], h, hfma2(o[x], q, 0u));   // level * step, rounded once
                             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place[k * (CB / 4) + j] + (kRing + buf) * L::kTile),
                                          "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
                                          : "memory");

@@ -127,7 +127,7 @@ def filled_cache(bt, H, D, seed=1, dtype=torch.float16, scale=1.0):
     return cache
 
 
-def attention_reference(Q, cache, bt, H, scale, causal=True, window=0, rounded_values=False):
+def attention_reference(Q, cache, bt, H, scale, causal=True, window=0):
     """Binary64 attention over the cached values.  Returns (o, lse, allowance): the allowance covers
     what the kernel rounds besides its output.
 
@@ -137,9 +137,7 @@ def attention_reference(Q, cache, bt, H, scale, causal=True, window=0, rounded_v
     binary32 roundings of s itself.  A weight p enters the value product as binary16 (2^-11), and its exponential
     is good to 2^-21; so o is off by sum_j p_j |v_j - o| (ds_j) + 2^-11 sum_j p_j |v_j| to first order.  The value
     product carries an offset of up to 30 steps in binary32: 2^-23 of it per addition, n / 16 + 40
-    additions.
-    rounded_values (many rows per sequence): the values enter as binary16 too, 2^-11 of each once more, or, where
-    one is 2^-24 of the largest, 2^-30 of that."""
+    additions."""
     rows, Hq, D = Q.shape
     G, P = Hq // H, bt.P
     K, V, ks, vs = decode_pages(cache, H, D, P)
@@ -169,8 +167,6 @@ def attention_reference(Q, cache, bt, H, scale, causal=True, window=0, rounded_v
                     offset = 30 * vsb[h // G, lo:hi]
                     allow[row, h] = ((p * ds) @ (v - o[row, h]).abs() + (2.0 ** -11 + 2.0 ** -20) * (p @ v.abs())
                                      + 2.0 ** -23 * ((hi - lo) / 16 + 40) * (p @ offset))
-                    if rounded_values:
-                        allow[row, h] += 2.0 ** -11 * (p @ v.abs()) + 2.0 ** -30 * v.abs().max()
             row += 1
     return o, lse, allow
 
