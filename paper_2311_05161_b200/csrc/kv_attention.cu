@@ -636,10 +636,15 @@ Variant pick(const KvAttnArgs &a, int sms)
     return v;
 }
 
-// The prefill kernel's tile is 256 query rows of one key head.
+// Which kernel, by the query rows that share a key head, on average over the sequences.  The prefill kernel's
+// tile is 256 rows and costs about the same from one row on; the decode kernel's cost grows with every 16.
+// Measured in us, decode / prefill, 8 key heads of 128: 4 sequences of 3000 tokens, 32 rows 32 / 37,
+// 64 rows 39 / 37, 96 rows 49 / 37; 16 of 3000, 64 rows 93 / 86, 128 rows 171 / 91; one of 32000,
+// 64 rows 69 / 73, 96 rows 98 / 74.  With little work the decode kernel stays ahead further (one of 4000, 128
+// rows 35 / 35; one of 500, 128 rows 17 / 22), but the lengths are known on the device only.
 bool use_prefill(int rows, int batch, int q_heads, int kv_heads)
 {
-    return (long long)(q_heads / kv_heads) * rows >= 96ll * batch;
+    return (long long)(q_heads / kv_heads) * rows > 64ll * batch;
 }
 
 template <int D, int NT, int WARPS>

@@ -182,11 +182,18 @@ struct Layout {
 
 struct Schedule {
     StatusBlock *sb;
-    int *counters;             // [workers][8]: one per worker and softmax warp
     float *partials;           // [workers][2] parts of 256 * (D + 2) numbers
+    struct Shared *shared;     // [workers]
     Divisor group;
 };
 
+// The item that begins in a CTA's share and ends in a later one's, for the kernel that joins its parts.
+struct Shared {
+    int parts;                                 // 0: there is none
+    int inside;                                // it does not begin with the share
+    int row0, h, tile, rows;
+    int pad[2];
+};
 
 // A piece of an item that falls into a CTA's share, as the scheduling warp hands it to the others.
 struct Piece {
@@ -194,8 +201,7 @@ struct Piece {
     int row0, n, len;                          // of the sequence
     int unit0, count;                          // units to walk; count < 0: no more pieces
     int whole;                                 // the item lies in this share alone
-    int slot, w0, w1, inside;                  // else: where the part goes, the CTAs that share the item, and
-                                               // whether it begins inside the first one's share
+    int slot;                                  // else: where the part goes
 };
 
 struct Control {
@@ -317,6 +323,22 @@ struct Walk {
     }
 };
 
+// Eight elements of the output in their order, from element `at` of O on.
+__device__ __forceinline__ void store_eight(const KvAttnArgs &a, size_t at, const float (&x)[8])
+{
+    uint4 o;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float top = a.o_bf16 ? __uint_as_float(0x7f7f0000u) : 65504.0f;
+        const float y0 = fminf(fmaxf(x[2 * k], -top), top), y1 = fminf(fmaxf(x[2 * k + 1], -top), top);
+        if (a.o_bf16) {
+            const __nv_bfloat162 z = __floats2bfloat162_rn(y0, y1);
+            (&o.x)[k] = *reinterpret_cast<const uint32_t *>(&z);
+        } else (&o.x)[k] = pack_half2(y0, y1);
+    }
+    *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.O) + at) = o;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_constant__ KvAttnArgs a, const __grid_constant__ Schedule sc)
 {
@@ -419,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         const int w = warp >> 2, r = tid;                  // row tile, row of the 256
         const uint32_t quarter = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes of tensor memory
         const uint32_t s_base = tmem_s + w * 128 + quarter, o_addr = tmem_o + w * D + quarter;
-        const uint32_t q_row = base + w * L::kQTile + (r & 127) * 128;
+        const uint32_t q_tile = base + w * L::kQTile;
         uint32_t unit_no = 0, item_no = 0;
         bool ok = true;
         // The output product of unit number n.  Its barrier (one per parity of n) knows one phase: the product of
@@ -442,12 +464,22 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             float m = kNoReference, l = 0.0f;
             if (count > 0) {
                 // ---- queries to the operand tile, scaled by a power of two to the top of binary16's range ----
-                uint4 raw[D / 8];
-                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + (in ? (size_t)(s.row0 + i) * a.q_stride + (size_t)head * D : 0));
+                // (the lanes of a row group take the 16-byte pieces of a row, so that a load touches whole lines)
+                constexpr int kPer = D / 8, kTogether = 32 / kPer;   // lanes per row, rows at a time
+                const int c = lane % kPer;
+                uint4 raw[kPer];
                 float amax = 0.0f;
 #pragma unroll
-                for (int k = 0; k < D / 8; ++k) {
-                    raw[k] = in ? __ldg(p + k) : make_uint4(0u, 0u, 0u, 0u);
+                for (int k = 0; k < kPer; ++k) {
+                    const int at = (r & ~31) + k * kTogether + lane / kPer, q_flat = pc.tile * kRows + at, q_i = sc.group.div(q_flat);
+                    const int q_head = pc.h * (int)sc.group.d + q_flat - q_i * (int)sc.group.d;
+                    raw[k] = make_uint4(0u, 0u, 0u, 0u);
+                    if (at < pc.rows)
+                        raw[k] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + (size_t)(s.row0 + q_i) * a.q_stride +
+                                                                       (size_t)q_head * D) + c);
+                }
+#pragma unroll
+                for (int k = 0; k < kPer; ++k)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const uint32_t v = (&raw[k].x)[e] & 0x7fff7fffu;
@@ -455,7 +487,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                                                   : __half22float2(*reinterpret_cast<const __half2 *>(&v));
                         amax = fmaxf(amax, fmaxf(x.x, x.y));
                     }
-                }
                 amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
                 volatile float *qmax = reinterpret_cast<float *>(smem + L::kOffQmax) + (item_no & 1) * kSoftmaxWarps;
                 if (lane == 0) {
@@ -468,7 +499,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 const int e = min(max((int)((__float_as_uint(amax) >> 23) & 255u) - 127 - 14, -100), 113);
                 const float down = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
-                for (int k = 0; k < D / 8; ++k) {
+                for (int k = 0; k < kPer; ++k) {
+                    const int at = (r & 96) + k * kTogether + lane / kPer;     // row of the tile of 128
                     float f[8];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -478,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                         f[2 * j] = x.x * down;
                         f[2 * j + 1] = x.y * down;
                     }
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_row + (k >> 3) * L::kQPart + (((k & 7) ^ (r & 7)) << 4)),
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_tile + (c >> 3) * L::kQPart + at * 128 + (((c & 7) ^ (at & 7)) << 4)),
                                  "r"(pack_half2(f[0], f[4])), "r"(pack_half2(f[1], f[5])), "r"(pack_half2(f[2], f[6])),
                                  "r"(pack_half2(f[3], f[7]))
                                  : "memory");
@@ -577,19 +609,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             const size_t out_at = ((size_t)(s.row0 + i) * a.q_heads + head) * D;
             // place of this thread's first four columns in a part, in quads: [warp][quad of columns][lane]
             const int quads_at = warp * (D / 4) * 32 + lane;
-            auto store8 = [&](int d, const float (&x)[8]) {          // eight elements in their order
-                uint4 o;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float top = a.o_bf16 ? __uint_as_float(0x7f7f0000u) : 65504.0f;
-                    const float y0 = fminf(fmaxf(x[2 * k], -top), top), y1 = fminf(fmaxf(x[2 * k + 1], -top), top);
-                    if (a.o_bf16) {
-                        const __nv_bfloat162 z = __floats2bfloat162_rn(y0, y1);
-                        (&o.x)[k] = *reinterpret_cast<const uint32_t *>(&z);
-                    } else (&o.x)[k] = pack_half2(y0, y1);
-                }
-                *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.O) + out_at + d) = o;
-            };
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t v[32];
@@ -599,6 +618,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     for (int k = 0; k < 32; ++k) v[k] = 0u;
                 }
                 if (!mine_only) {
+                    if (in)
 #pragma unroll
                     for (int k = 0; k < 32; k += 4)
                         __stcg(reinterpret_cast<uint4 *>(part + 2 * kRows) + quads_at + (8 * c + k / 4) * 32, make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]));
@@ -608,70 +628,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                         const float x[8] = {__uint_as_float(v[k]) * inv, __uint_as_float(v[k + 2]) * inv, __uint_as_float(v[k + 4]) * inv,
                                             __uint_as_float(v[k + 6]) * inv, __uint_as_float(v[k + 1]) * inv, __uint_as_float(v[k + 3]) * inv,
                                             __uint_as_float(v[k + 5]) * inv, __uint_as_float(v[k + 7]) * inv};
-                        store8(32 * c + k, x);
+                        store_eight(a, out_at + 32 * c + k, x);
                     }
                 }
             }
-            const int w0 = pc.w0, w1 = pc.w1, inside = pc.inside;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(L::kPieceEmpty + (piece_no & 1)));
+            if (!in) continue;
             if (mine_only) {
-                if (in && a.lse) a.lse[out_at / D] = l > 0.0f ? (m + lg2(l)) * kLn2 : -INFINITY;
-                continue;
+                if (a.lse) a.lse[out_at / D] = l > 0.0f ? (m + lg2(l)) * kLn2 : -INFINITY;
+            } else {
+                __stcg(part + r, m);
+                __stcg(part + kRows + r, l);
             }
-            __stcg(part + r, m);
-            __stcg(part + kRows + r, l);
-            __threadfence();
-            __syncwarp();
-            int last = 0;
-            if (lane == 0) last = atomicAdd(sc.counters + w0 * kSoftmaxWarps + warp, 1) == w1 - w0;
-            if (!__shfl_sync(0xffffffffu, last, 0)) continue;
-            __threadfence();
-            // the last of this warp's counterparts joins the parts in list order
-            const size_t part_size = kRows * (D + 2);
-            const float *head_part = sc.partials + ((size_t)w0 * 2 + (inside ? 1 : 0)) * part_size;
-            const float *rest = sc.partials + (size_t)w0 * 2 * part_size;
-            const int parts = w1 - w0 + 1;
-            float top = __ldcg(head_part + r);
-            for (int k = 1; k < parts; ++k) top = fmaxf(top, __ldcg(rest + (size_t)k * 2 * part_size + r));
-            float lsum = 0.0f;
-            for (int k = 0; k < parts; ++k) {
-                const float *x = k == 0 ? head_part : rest + (size_t)k * 2 * part_size;
-                lsum += __ldcg(x + kRows + r) * ex2(__ldcg(x + r) - top);
-            }
-            const float join_inv = lsum > 0.0f ? __fdiv_rn(-2.0f, lsum) : 0.0f;
-            constexpr int kCols = 64;        // columns at a time: their loads are all in flight together
-#pragma unroll 1
-            for (int c = 0; c < D; c += kCols) {
-                float acc[kCols];
-#pragma unroll
-                for (int k = 0; k < kCols; ++k) acc[k] = 0.0f;
-#pragma unroll 1
-                for (int k = 0; k < parts; ++k) {
-                    const float *x = k == 0 ? head_part : rest + (size_t)k * 2 * part_size;
-                    const float f = ex2(__ldcg(x + r) - top) * join_inv;
-                    const float4 *from = reinterpret_cast<const float4 *>(x + 2 * kRows) + quads_at + c / 4 * 32;
-#pragma unroll
-                    for (int q = 0; q < kCols / 4; ++q) {
-                        const float4 y = __ldcg(from + q * 32);
-                        acc[4 * q] = fmaf(y.x, f, acc[4 * q]);
-                        acc[4 * q + 1] = fmaf(y.y, f, acc[4 * q + 1]);
-                        acc[4 * q + 2] = fmaf(y.z, f, acc[4 * q + 2]);
-                        acc[4 * q + 3] = fmaf(y.w, f, acc[4 * q + 3]);
-                    }
-                }
-                if (in) {
-#pragma unroll
-                    for (int k = 0; k < kCols; k += 8) {
-                        const float y[8] = {acc[k], acc[k + 2], acc[k + 4], acc[k + 6], acc[k + 1], acc[k + 3], acc[k + 5], acc[k + 7]};
-                        store8(c + k, y);
-                    }
-                }
-            }
-            if (in) {
-                if (a.lse) a.lse[out_at / D] = lsum > 0.0f ? (top + lg2(lsum)) * kLn2 : -INFINITY;
-            }
-            if (lane == 0) sc.counters[w0 * kSoftmaxWarps + warp] = 0;       // ready for the next call
         }
     } else if (warp < kMmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
@@ -888,6 +857,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             // -------------------------------------------------------------- the pieces of this CTA's share
             Walk walk(a, sc);
             walk.start(ctl->found_b, ctl->found_tile, ctl->found_off, begin, max(begin, end));
+            Shared shared = {};
             for (uint32_t piece_no = 0;; ++piece_no) {
                 const bool more = walk.next();
                 if (piece_no >= 2 && !try_wait(bar(L::kPieceEmpty + (piece_no & 1)), (piece_no >> 1 & 1) ^ 1) &&
@@ -908,14 +878,20 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     p.count = walk.count;
                     p.whole = walk.whole;
                     p.slot = walk.first_unit <= begin ? 0 : 1;
-                    p.w0 = (int)quotient(walk.first_unit, per);
-                    p.w1 = (int)quotient(walk.first_unit + body - 1, per);
-                    p.inside = walk.first_unit > (long long)p.w0 * per;
+                    if (!walk.whole && walk.first_unit >= begin) {       // begins here and ends in a later share
+                        shared.parts = (int)(quotient(walk.first_unit + body - 1, per) - (long long)blockIdx.x) + 1;
+                        shared.inside = walk.first_unit > begin;
+                        shared.row0 = walk.s.row0;
+                        shared.h = walk.h;
+                        shared.tile = walk.tile;
+                        shared.rows = walk.rows;
+                    }
                 }
                 ctl->piece[piece_no & 1] = p;
                 mbar_arrive(bar(L::kPieceFull + (piece_no & 1)));
                 if (!more) break;
             }
+            sc.shared[blockIdx.x] = shared;
         }
         __syncwarp();
     }
@@ -927,29 +903,78 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     }
 }
 
+// Joins the parts of the items that several CTAs shared, in list order.  A kernel of its own spreads this over
+// the GPU: left to the CTA that finishes an item last, the parts (131 KB each) pass through one SM, some 1.2 us
+// per part.  Block (x, y): rows 32 x .. 32 x + 31 of the item that begins in share y; a warp takes 32 columns.
+template <int D>
+__global__ void __launch_bounds__(D) kv_prefill_join_kernel(const __grid_constant__ KvAttnArgs a, const __grid_constant__ Schedule sc)
+{
+    allow_dependents();
+    dependent_wait();
+    const Shared item = sc.shared[blockIdx.y];
+    const int lane = threadIdx.x & 31, c = threadIdx.x & ~31, r = blockIdx.x * 32 + lane;
+    if (item.parts == 0 || r >= item.rows) return;
+    constexpr size_t kPart = kRows * (D + 2);
+    const float *rest = sc.partials + (size_t)blockIdx.y * 2 * kPart, *first = rest + (item.inside ? kPart : 0);
+    auto part = [&](int k) { return k == 0 ? first : rest + (size_t)k * 2 * kPart; };
+    float top = kNoReference;
+#pragma unroll 4
+    for (int k = 0; k < item.parts; ++k) top = fmaxf(top, __ldcg(part(k) + r));
+    float acc[32], lsum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) acc[k] = 0.0f;
+#pragma unroll 2
+    for (int k = 0; k < item.parts; ++k) {
+        const float *x = part(k);
+        const float f = ex2(__ldcg(x + r) - top);
+        lsum = fmaf(__ldcg(x + kRows + r), f, lsum);
+        const float4 *from = reinterpret_cast<const float4 *>(x + 2 * kRows) + (blockIdx.x * (D / 4) + c / 4) * 32 + lane;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const float4 y = __ldcg(from + q * 32);
+            acc[4 * q] = fmaf(y.x, f, acc[4 * q]);
+            acc[4 * q + 1] = fmaf(y.y, f, acc[4 * q + 1]);
+            acc[4 * q + 2] = fmaf(y.z, f, acc[4 * q + 2]);
+            acc[4 * q + 3] = fmaf(y.w, f, acc[4 * q + 3]);
+        }
+    }
+    const float inv = lsum > 0.0f ? __fdiv_rn(-2.0f, lsum) : 0.0f;
+    const int flat = item.tile * kRows + r, i = sc.group.div(flat);
+    const size_t row = (size_t)(item.row0 + i) * a.q_heads + item.h * (int)sc.group.d + flat - i * (int)sc.group.d;
+#pragma unroll
+    for (int k = 0; k < 32; k += 8) {
+        const float y[8] = {acc[k] * inv, acc[k + 2] * inv, acc[k + 4] * inv, acc[k + 6] * inv,
+                            acc[k + 1] * inv, acc[k + 3] * inv, acc[k + 5] * inv, acc[k + 7] * inv};
+        store_eight(a, row * D + c + k, y);
+    }
+    if (a.lse && c == 0) a.lse[row] = lsum > 0.0f ? (top + lg2(lsum)) * kLn2 : -INFINITY;
+}
+
 template <int D>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
 {
     static std::atomic<int> raised[kMaxDevices];
-    const cudaError_t e = raise_smem_limit(kv_prefill_kernel<D>, Layout<D>::kSmem, raised);
-    if (e != cudaSuccess) return e;
-    return launch_overlapped(kv_prefill_kernel<D>, dim3(ctas), dim3(kThreads), Layout<D>::kSmem, st, a, sc);
+    cudaError_t e = raise_smem_limit(kv_prefill_kernel<D>, Layout<D>::kSmem, raised);
+    if (e == cudaSuccess) e = launch_overlapped(kv_prefill_kernel<D>, dim3(ctas), dim3(kThreads), Layout<D>::kSmem, st, a, sc);
+    if (e == cudaSuccess) e = launch_overlapped(kv_prefill_join_kernel<D>, dim3(kRows / 32, ctas), dim3(D), 0, st, a, sc);
+    return e;
 }
 
 }  // namespace
 
-// Status block, counters, two parts per CTA.
+// Status block, two parts per CTA, the shared items.  (The counters of the decode form are left alone.)
 size_t kv_prefill_workspace(int D)
 {
     const int sms = device_sms();
-    return sizeof(StatusBlock) + kv_counters_bytes(sms) + (size_t)sms * 2 * kRows * (D + 2) * sizeof(float);
+    return sizeof(StatusBlock) + kv_counters_bytes(sms) + (size_t)sms * (2 * kRows * (D + 2) * sizeof(float) + sizeof(Shared));
 }
 
 cudaError_t launch_kv_prefill(const KvAttnArgs &a, uint8_t *workspace, cudaStream_t st)
 {
     const int sms = device_sms();
-    const Schedule sc = {reinterpret_cast<StatusBlock *>(workspace), reinterpret_cast<int *>(workspace + sizeof(StatusBlock)),
-                         reinterpret_cast<float *>(workspace + sizeof(StatusBlock) + kv_counters_bytes(sms)),
+    float *partials = reinterpret_cast<float *>(workspace + sizeof(StatusBlock) + kv_counters_bytes(sms));
+    const Schedule sc = {reinterpret_cast<StatusBlock *>(workspace), partials,
+                         reinterpret_cast<Shared *>(partials + (size_t)sms * 2 * kRows * (a.cache.D + 2)),
                          Divisor((uint32_t)(a.q_heads / a.cache.heads))};
     return a.cache.D == 64 ? launch<64>(a, sc, sms, st) : launch<128>(a, sc, sms, st);
 }
