@@ -245,6 +245,20 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
             __syncwarp();
             if (lane < 2) copy_block(ring + st * UB + lane * BB, head_base + from, BB, bars + st * 8);
         };
+        // ---- queries, shared by the warps: a lane takes eight elements of a row, scales them by a power of two
+        // to the top of binary16's range and leaves them as the four pairs that expand() gives of a word ----
+        // (Loaded in front of the first copies: 3 units of every warp are 31 MB, and the loads would wait behind them.)
+        constexpr int kPass = WARPS * (32 / LPV), kPasses = (R + kPass - 1) / kPass;
+        uint4 q_raw[kPasses];
+#pragma unroll
+        for (int n = 0; n < kPasses; ++n) {
+            const int r = warp * (32 / LPV) + lane / LPV + n * kPass;
+            const int i = sc.group.div(tile * R + r), head = h * group + tile * R + r - i * group;
+            q_raw[n] = make_uint4(0u, 0u, 0u, 0u);
+            if (r < rows_here)
+                q_raw[n] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + (size_t)(s.row0 + i) * a.q_stride +
+                                                                 (size_t)head * D) + lane % LPV);
+        }
         {
             int st = stage;
             for (int k = 0; k < min(nk, S::kStages); ++k) {
@@ -252,18 +266,14 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 st = st + 1 == S::kStages ? 0 : st + 1;
             }
         }
-        // ---- queries, shared by the warps: a lane takes eight elements of a row, scales them by a power of two
-        // to the top of binary16's range and leaves them as the four pairs that expand() gives of a word ----
-        for (int r = warp * (32 / LPV) + lane / LPV; r < R; r += WARPS * (32 / LPV)) {
-            const int i = sc.group.div(tile * R + r), head = h * group + tile * R + r - i * group;
-            uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-            if (r < rows_here)
-                raw = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + (size_t)(s.row0 + i) * a.q_stride +
-                                                            (size_t)head * D) + lane % LPV);
+#pragma unroll
+        for (int n = 0; n < kPasses; ++n) {
+            const int r = warp * (32 / LPV) + lane / LPV + n * kPass;
+            if (r >= R) break;             // (whole row groups of lanes)
             float f[8], amax = 0.0f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const uint32_t v = (&raw.x)[k];
+                const uint32_t v = (&q_raw[n].x)[k];
                 if (a.q_bf16) {
                     f[2 * k] = __uint_as_float(v << 16);
                     f[2 * k + 1] = __uint_as_float(v & 0xffff0000u);
@@ -578,35 +588,71 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 __stcg(part + tid, tile_m[tid]);
                 __stcg(part + R + tid, tile_l[tid]);
             }
-            __threadfence();
             __syncthreads();
             const int w0 = (int)quotient(first_unit, per), w1 = (int)quotient(first_unit + item_units - 1, per);
-            if (tid == 0) last_part = atomicAdd(sc.counters + w0, 1) == w1 - w0;
+            if (tid == 0) {                // releases what the CTA has stored, acquires the parts of those before it
+                int before;
+                asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(sc.counters + w0) : "memory");
+                last_part = before == w1 - w0;
+            }
             __syncthreads();
             if (last_part) {
-                __threadfence();
-                // part of worker w: its first segment, unless the item begins inside its share
+                // part of worker w: its first segment, unless the item begins inside its share.  A warp takes every
+                // WARPS-th part, all of their loads in flight together; the warps' sums are joined as above.
                 const bool inside = first_unit > (long long)w0 * per;
-                const float *first = sc.partials + ((size_t)w0 * 2 + (inside ? 1 : 0)) * part_size;
                 const float *rest = sc.partials + (size_t)w0 * 2 * part_size;
                 const int parts = w1 - w0 + 1;
+                auto part_of = [&](int p) { return rest + (p > 0 ? (size_t)p * 2 * part_size : inside ? (size_t)part_size : 0); };
+                float m = kNoReference, lsum = 0.0f;         // of row lane % R
+#pragma unroll 8
+                for (int p = warp; p < parts; p += WARPS) m = fmaxf(m, __ldcg(part_of(p) + lane % R));
+                constexpr int kMine = kQuads / 32;           // quad lane + 32 k: row 32 k / (D / 4) + lane / (D / 4)
+                float4 v[kMine];
+#pragma unroll
+                for (int k = 0; k < kMine; ++k) v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
+                for (int p = warp; p < parts; p += WARPS) {
+                    const float *x = part_of(p);
+                    const float keep = ex2(__ldcg(x + lane % R) - m);
+                    lsum = fmaf(__ldcg(x + R + lane % R), keep, lsum);
+#pragma unroll
+                    for (int k = 0; k < kMine; ++k) {
+                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(x + 2 * R) + lane + 32 * k);
+                        const float f = __shfl_sync(0xffffffffu, keep, (lane + 32 * k) / (D / 4));
+                        v[k].x = fmaf(y.x, f, v[k].x);
+                        v[k].y = fmaf(y.y, f, v[k].y);
+                        v[k].z = fmaf(y.z, f, v[k].z);
+                        v[k].w = fmaf(y.w, f, v[k].w);
+                    }
+                }
+                if (lane < R) {
+                    row_m[warp][lane] = m;
+                    row_l[warp][lane] = lsum;
+                }
+#pragma unroll
+                for (int k = 0; k < kMine; ++k) {
+                    const int i = lane + 32 * k;
+                    *reinterpret_cast<float4 *>(join + ((size_t)warp * R + i / (D / 4)) * S::kPad + i % (D / 4) * 4) = v[k];
+                }
+                __syncthreads();
                 for (int i = tid; i < kQuads; i += THREADS) {
                     const int r = i / (D / 4), d = (i % (D / 4)) * 4;
                     if (r >= rows_here) continue;
-                    float m = __ldcg(first + r);
-#pragma unroll 8
-                    for (int p = 1; p < parts; ++p) m = fmaxf(m, __ldcg(rest + (size_t)p * 2 * part_size + r));
-                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    float lsum = 0.0f;
-#pragma unroll 8
-                    for (int p = 0; p < parts; ++p) {
-                        const float *x = p == 0 ? first : rest + (size_t)p * 2 * part_size;
-                        const float keep = ex2(__ldcg(x + r) - m);
-                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(x + 2 * R) + i);
-                        lsum += __ldcg(x + R + r) * keep;
-                        v.x += y.x * keep; v.y += y.y * keep; v.z += y.z * keep; v.w += y.w * keep;
+                    float top = row_m[0][r], den = 0.0f;
+#pragma unroll
+                    for (int w = 1; w < WARPS; ++w) top = fmaxf(top, row_m[w][r]);
+                    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int w = 0; w < WARPS; ++w) {
+                        const float keep = ex2(row_m[w][r] - top);
+                        const float4 x = *reinterpret_cast<const float4 *>(join + ((size_t)w * R + r) * S::kPad + d);
+                        den = fmaf(row_l[w][r], keep, den);
+                        y.x = fmaf(x.x, keep, y.x);
+                        y.y = fmaf(x.y, keep, y.y);
+                        y.z = fmaf(x.z, keep, y.z);
+                        y.w = fmaf(x.w, keep, y.w);
                     }
-                    write_row(r, d, v, m, lsum);
+                    write_row(r, d, y, top, den);
                 }
                 if (tid == 0) sc.counters[w0] = 0;           // ready for the next call
             }
