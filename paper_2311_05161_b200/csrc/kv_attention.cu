@@ -439,7 +439,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                        m = fmaxf(m, ref[n][j]);
+                        m = fmaxf(m - kRoom, ref[n][j]);
                         const float keep = ex2(ref[n][j] - m);
                         ref[n][j] = m;
                         l[n][j] *= keep;

@@ -11,6 +11,9 @@ constexpr uint32_t kSuspendHintNs = 20000;                 // a waiting thread i
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoReference = -1.0e30f;
 constexpr float kSlack = 15.0f;                            // weights stay below 2^15, within binary16
+// A reference that moves is put this far below the largest exponent, so that weights down to 2^-32 of the largest
+// one are more than binary16's zero (many small ones can add up), with 8 bits left above for what comes later.
+constexpr float kRoom = 7.0f;
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p)
 {

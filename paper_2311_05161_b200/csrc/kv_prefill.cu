@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     const bool fresh = m == kNoReference;
                     const bool over = top > (fresh ? kNoReference : m + kSlack);
                     if (__any_sync(0xffffffffu, over)) {     // move the reference and scale what has been summed
-                        const float to = over ? top : m;
+                        const float to = over ? top - kRoom : m;
                         const float keep = fresh ? 0.0f : ex2(m - to);
                         m = to;
                         l *= keep;

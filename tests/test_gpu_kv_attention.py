@@ -164,6 +164,185 @@ def test_strided_queries_other_stream_and_graph():
     w4a8.check_status(ws)
 
 
+@pytest.mark.parametrize("lens,rows,P,Hq,H,D,window", [
+    ([700, 300, 0, 64], [513, 300, 0, 1], 32, 10, 2, 128, 0),       # five heads share a key head: rows straddle row tiles
+    ([700, 300, 9, 64], [90, 300, 9, 64], 16, 7, 1, 64, 100),
+    ([300], [257], 64, 1, 1, 128, 0),                               # one head alone; a second row tile of one row
+    ([129, 65, 63, 64, 1], [129, 65, 63, 64, 1], 128, 24, 1, 64, 0),
+    ([2000, 10], [20, 10], 16, 16, 2, 128, 1900),
+    ([20000], [24], 64, 8, 2, 128, 0),                              # every item is shared by many CTAs
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_rows(lens, rows, P, Hq, H, D, window, causal):
+    run(lens, rows, P, Hq, H, D, BF16, F16, causal=causal, window=window, pad=3)
+
+
+def test_one_distant_token_against_many_light_ones():
+    """One token holds most of the weight and thousands hold 2^-27 of it each: a reference that sat on the
+    largest exponent would round those to binary16's zero."""
+    H, D, P, n = 1, 64, 64, 6000
+    for rows in (1, 96):
+        bt = Batch([n], [rows], P)
+        K = torch.zeros(n, 1, D)
+        K[0, 0, 0] = 1.0
+        V = torch.ones(n, 1, D)
+        V[0] = -1.0
+        cache = w4a8.new_kv_cache(bt.num_pages, P, H, D).fill_(0)
+        ws = w4a8.new_kv_workspace(rows, 1, 1, H, D)
+        w4a8.kv_append(K.half().cuda(), V.half().cuda(), cache, bt.table, bt.kv_lens, ws,
+                       cu_rows=torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+        Q = torch.zeros(rows, 1, D)
+        Q[:, 0, 0] = 27 * math.log(2.0)
+        Q = Q.half().cuda()
+        O = w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, cu_rows=bt.cu, scale=1.0, dtype=BF16)
+        w4a8.check_status(ws)
+        o, _, allow = attention_reference(Q, cache, bt, H, 1.0)
+        check_attention(O, o, allow, BF16)
+
+
+def _problem(lens, rows, P, Hq, H, D, seed):
+    bt = Batch(lens, rows, P, seed=seed)
+    cache = filled_cache(bt, H, D, seed=seed)
+    Q = vectors((bt.rows, Hq, D), seed + 3, F16).cuda()
+    return bt, cache, Q, H
+
+
+def test_calls_of_different_forms_share_a_workspace():
+    """Many-row and few-row calls in turn on one workspace, with other kernels' leavings on the chip between
+    them: every call gives the bits that it gives alone on a fresh workspace."""
+    problems = [_problem([3000], [100], 64, 8, 2, 128, 1), _problem([700, 1, 2500], None, 32, 16, 2, 128, 2),
+                _problem([300, 40], [300, 40], 16, 6, 2, 64, 3), _problem([5000], None, 64, 8, 1, 64, 4),
+                _problem([900, 900], [6, 7], 64, 8, 2, 128, 5)]
+    size, want = 0, []
+    for bt, cache, Q, H in problems:
+        n = w4a8.kv_attention_workspace_bytes(bt.rows, len(bt.lens), Q.shape[1], H, Q.shape[2])
+        size = max(size, n)
+        want.append(w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, w4a8.new_kv_workspace(
+            bt.rows, len(bt.lens), Q.shape[1], H, Q.shape[2]), cu_rows=bt.cu))
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    w4a8.workspace_init(ws)
+    noise = torch.randn(2048, 2048, device="cuda").half()
+    order = [0, 1, 2, 3, 4, 1, 0, 4, 2, 0, 3, 1]
+    got = []
+    for k in order:
+        bt, cache, Q, H = problems[k]
+        got.append(w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, cu_rows=bt.cu))
+        if k % 2 == 0:
+            noise = (noise @ noise).clamp(-1, 1)
+    w4a8.check_status(ws)
+    for k, o in zip(order, got):
+        assert torch.equal(o, want[k]), k
+
+
+def test_streams_and_graphs_with_workspaces_of_their_own():
+    """Calls that overlap on two streams, and two captured graphs, each with its own workspace."""
+    for lens, rows in (([4000, 100, 9], None), ([2000, 500], [200, 100])):
+        bt, cache, Q, H = _problem(lens, rows, 64, 8, 2, 128, 11)
+        spaces = [w4a8.new_kv_workspace(bt.rows, len(lens), 8, H, 128) for _ in range(2)]
+        want = w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, spaces[0], cu_rows=bt.cu)
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        outs = [[torch.empty_like(want) for _ in range(6)] for _ in range(2)]
+        torch.cuda.synchronize()
+        for k in range(6):
+            for st, ws, out in zip(streams, spaces, outs):
+                with torch.cuda.stream(st):
+                    w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, cu_rows=bt.cu, out=out[k])
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want) for out in outs for o in out)
+        graphs, held = [], []
+        for ws in spaces:
+            graph, out = torch.cuda.CUDAGraph(), torch.empty_like(want)
+            with torch.cuda.graph(graph):
+                w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, cu_rows=bt.cu, out=out)
+            graphs.append(graph)
+            held.append(out)
+        for _ in range(3):
+            for graph, st, out in zip(graphs, streams, held):
+                with torch.cuda.stream(st):
+                    out.zero_()
+                    graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, want) for out in held)
+        for ws in spaces:
+            w4a8.check_status(ws)
+
+
+def test_captured_call_of_many_rows_follows_its_inputs():
+    """Replays with other lengths, row counts and queries in the captured tensors."""
+    bt, cache, Q, H = _problem([400, 300], [60, 40], 32, 8, 2, 128, 21)
+    ws = w4a8.new_kv_workspace(bt.rows, 2, 8, H, 128)
+    out = torch.zeros(bt.rows, 8, 128, dtype=F16, device="cuda")
+    w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, cu_rows=bt.cu, out=out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, cu_rows=bt.cu, out=out)
+    for k, (lens, counts) in enumerate([([400, 300], [60, 40]), ([100, 1], [99, 1]), ([33, 300], [0, 100]), ([0, 0], [50, 50]),
+                                        ([400, 17], [1, 1])]):
+        bt.lens, bt.counts = lens, counts
+        bt.kv_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        bt.cu.copy_(torch.tensor([0, counts[0], sum(counts)], dtype=torch.int32))
+        Q.copy_(vectors(Q.shape, 30 + k, F16))
+        out.fill_(5.0)
+        graph.replay()
+        o, _, allow = attention_reference(Q, cache, bt, H, 128 ** -0.5)
+        n = sum(counts)
+        check_attention(out[:n].clone(), o[:n], allow[:n], F16)
+        assert bool((out[n:] == 5.0).all())
+    w4a8.check_status(ws)
+
+
+def test_pages_beyond_32_bit_offsets():
+    """The same pages at the far end of a cache of more than 4 GiB."""
+    H, D, P = 8, 128, 64
+    if torch.cuda.mem_get_info()[0] < 8 << 30:
+        pytest.skip("not enough device memory")
+    for lens, rows in (([200, 65], None), ([200, 65], [100, 65])):
+        bt = Batch(lens, rows, P)
+        small = filled_cache(bt, H, D)
+        big = w4a8.new_kv_cache((1 << 32) // small.shape[1] + 2 * bt.num_pages, P, H, D)
+        shift = big.shape[0] - bt.num_pages
+        big[shift:] = small
+        Q = vectors((bt.rows, 16, D), 3, F16).cuda()
+        ws = w4a8.new_kv_workspace(bt.rows, 2, 16, H, D)
+        want = w4a8.kv_attention(Q, small, bt.table, bt.kv_lens, H, ws, cu_rows=bt.cu)
+        got = w4a8.kv_attention(Q, big, torch.where(bt.table < 0, bt.table, bt.table + shift), bt.kv_lens, H, ws, cu_rows=bt.cu)
+        w4a8.check_status(ws)
+        assert torch.equal(got, want)
+
+
+def test_refusals():
+    H, D, P = 2, 64, 16
+    bt = Batch([20, 5], None, P)
+    cache = filled_cache(bt, H, D)
+    ws = w4a8.new_kv_workspace(2, 2, 4, H, D)
+    Q = vectors((2, 4, D), 1, F16).cuda()
+    K = vectors((2, H, D), 1, F16).cuda()
+
+    def attend(q=Q, c=cache, table=bt.table, lens=bt.kv_lens, heads=H, space=ws, **kw):
+        return w4a8.kv_attention(q, c, table, lens, heads, space, **kw)
+
+    for error, call in (
+            (TypeError, lambda: attend(q=Q.float())), (TypeError, lambda: attend(q=Q.cpu())), (TypeError, lambda: attend(q=Q.view(2, -1))),
+            (TypeError, lambda: attend(table=bt.table.long())), (TypeError, lambda: attend(lens=bt.kv_lens.long())),
+            (TypeError, lambda: attend(c=cache.view(torch.int32))), (ValueError, lambda: attend(lens=bt.kv_lens[:1])),
+            (ValueError, lambda: attend(heads=3)), (ValueError, lambda: attend(c=cache[:, :-8].contiguous())),
+            (ValueError, lambda: attend(out=torch.empty(2, 4, 32, dtype=F16, device="cuda"))),
+            (TypeError, lambda: attend(out=torch.empty(2, 4, D, device="cuda"))),
+            (ValueError, lambda: attend(lse=torch.empty(2, 2, device="cuda"))), (w4a8.W4A8Error, lambda: attend(scale=0.0)),
+            (w4a8.W4A8Error, lambda: attend(scale=float("nan"))), (w4a8.W4A8Error, lambda: attend(window=-1)),
+            (w4a8.W4A8Error, lambda: attend(q=Q[:, :3].contiguous())), (w4a8.W4A8Error, lambda: attend(space=ws[:256])),
+            (w4a8.W4A8Error, lambda: attend(q=torch.cat([Q, Q]))),
+            (ValueError, lambda: attend(cu_rows=torch.zeros(2, dtype=torch.int32, device="cuda"))),
+            (TypeError, lambda: w4a8.kv_append(K, K.bfloat16(), cache, bt.table, bt.kv_lens, ws)),
+            (ValueError, lambda: w4a8.kv_append(K, K[:1], cache, bt.table, bt.kv_lens, ws)),
+            (w4a8.W4A8Error, lambda: w4a8.kv_append(K[:1], K[:1], cache, bt.table, bt.kv_lens, ws)),
+            (TypeError, lambda: w4a8.kv_read(cache, bt.table, bt.kv_lens, 2, H, D, ws, dtype=torch.float32))):
+        with pytest.raises(error):
+            call()
+    attend()
+    w4a8.check_status(ws)
+
+
 def test_bad_tables_are_reported():
     H, D, P = 2, 64, 16
     cache = w4a8.new_kv_cache(4, P, H, D).fill_(0)
