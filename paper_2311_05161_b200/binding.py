@@ -1,4 +1,5 @@
-"""ctypes binding of libw4a8.so: argument marshalling only.
+"""Binding of libw4a8.so by ctypes: argument marshalling only.  (The calls that a decoder makes per layer and token
+are marshalled by the extension module _calls, csrc/calls.cpp: 12 to 14 us of Python took longer than their kernels.)
 
 Every function here has the name of the C entry point it calls (include/w4a8.h) minus the
 `w4a8_` prefix.  torch supplies device memory and the current stream; all arithmetic of
@@ -146,6 +147,10 @@ def _load() -> ctypes.CDLL:
 
 lib = _load()
 
+from . import _calls  # noqa: E402  (links to the library that was loaded above)
+
+_calls.set_errors(W4A8Error, torch.OutOfMemoryError)
+
 
 def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
@@ -256,65 +261,14 @@ def norm_quantize_act(X, norm_weight, norm_bias=None, kind: int = NORM_RMS, eps:
     return Xq, tok
 
 
-_DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
-_DTYPES16 = (torch.float16, torch.bfloat16)
-
-
-def _here(what, *tensors):
-    """The stream of the current device, on which all the tensors live: the library launches there."""
-    at = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != at:
-            raise ValueError(f"{what}: tensor on {t.device}, current device is cuda:{at}")
-    return _raw_stream(at)
-
-
-def _is(t, shape, what):
-    if t is not None and t.shape != shape:
-        raise ValueError(f"{what}: expected shape {shape}, got {tuple(t.shape)}")
-    return t
-
-
-def _dev16(t, what, contiguous=True):
-    if not t.is_cuda or t.dtype not in _DTYPES16 or (contiguous and not t.is_contiguous()):
-        raise TypeError(f"{what}: expected a CUDA tensor of float16 or bfloat16{', contiguous' if contiguous else ''}")
-    return t
-
-
-def _at(t):
-    return None if t is None else t.data_ptr()
-
-
 def add_norm_quantize_act(X, residual, norm_weight, norm_bias=None, kind: int = NORM_RMS, eps: float = 1e-5,
                           residual_out=None, out=None):
     """residual + X, then RMSNorm / LayerNorm and the token-wise INT8 quantizer of the sum, in one pass:
     X [M, K] float16 / bfloat16, residual [M, K] float16 / bfloat16 / float32 ->
     (Xq [M, K] int8, tok_scale [M] float32, residual_out [M, K] of residual's type).  In place with
     `residual_out=residual`."""
-    X = _dev16(X, "X")
-    if residual.dtype not in _DTYPES:
-        raise TypeError("residual: expected float16, bfloat16 or float32")
-    residual = _dev(residual, residual.dtype, "residual")
-    norm_weight = _dev(norm_weight, torch.float32, "norm_weight")
-    norm_bias = _dev(norm_bias, torch.float32, "norm_bias")
-    M, K = X.shape
-    _is(residual, X.shape, "residual")
-    _is(norm_weight, (K,), "norm_weight")
-    _is(norm_bias, (K,), "norm_bias")
-    if residual_out is None:
-        residual_out = torch.empty_like(residual)
-    else:
-        _is(_dev(residual_out, residual.dtype, "residual_out"), X.shape, "residual_out")
-    if out is None:
-        Xq, tok = torch.empty_like(X, dtype=torch.int8), X.new_empty(M, dtype=torch.float32)
-    else:
-        Xq, tok = _is(_dev(out[0], torch.int8, "Xq"), X.shape, "Xq"), _is(_dev(out[1], torch.float32, "tok_scale"), (M,), "tok_scale")
-    stream = _here("add_norm_quantize_act", X, residual, norm_weight, norm_bias, residual_out, Xq, tok)
-    _check(lib.w4a8_add_norm_quantize_act(
-        X.data_ptr(), _DTYPES[X.dtype], residual.data_ptr(), _DTYPES[residual.dtype], residual_out.data_ptr(),
-        norm_weight.data_ptr(), _at(norm_bias), kind, eps, M, K, Xq.data_ptr(), tok.data_ptr(), stream),
-        "w4a8_add_norm_quantize_act")
-    return Xq, tok, residual_out
+    Xq, tok = (None, None) if out is None else out
+    return _calls.add_norm_quantize_act(X, residual, norm_weight, norm_bias, kind, eps, residual_out, Xq, tok)
 
 
 def linear_workspace_bytes(M: int, N: int, K: int, group: int = 0, opts: Opts | None = None) -> int:
@@ -552,63 +506,19 @@ def new_kv_workspace(rows: int, batch: int, q_heads: int, kv_heads: int, head_di
     return ws
 
 
-def _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, head_dim, workspace, what, *tensors):
-    """Checks of the arguments that the cache calls share, and those arguments in the library's order:
-    (cache .. kv_heads, D, page table .. batch), workspace and stream."""
-    _dev(cache, torch.uint8, "cache")
-    _dev(page_table, torch.int32, "page_table")
-    _dev(kv_lens, torch.int32, "kv_lens")
-    _dev(workspace, torch.uint8, "workspace")
-    batch, max_pages = page_table.shape
-    _is(kv_lens, (batch,), "kv_lens")
-    if cu_rows is not None:
-        _is(_dev(cu_rows, torch.int32, "cu_rows"), (batch + 1,), "cu_rows")
-    num_pages, nbytes = cache.shape
-    slot = kv_heads * (head_dim + 8)                   # bytes of a token, all heads
-    if slot <= 0 or nbytes % slot or nbytes != lib.w4a8_kv_page_bytes(nbytes // slot, kv_heads, head_dim):
-        raise ValueError(f"{what}: pages of {nbytes} bytes do not hold {kv_heads} heads of {head_dim}")
-    stream = _here(what, cache, page_table, kv_lens, cu_rows, workspace, *tensors)
-    return ((cache.data_ptr(), num_pages, nbytes // slot, kv_heads, head_dim, page_table.data_ptr(), max_pages, kv_lens.data_ptr(),
-             _at(cu_rows), batch), (workspace.data_ptr(), workspace.numel(), stream))
-
-
-def _rows_of(t, what):
-    """[rows, heads, D] whose rows may be slices of wider ones: the row stride in elements."""
-    _dev16(t, what, contiguous=False)
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise TypeError(f"{what}: expected [rows, heads, D] with contiguous heads")
-    # torch leaves the stride of a dimension of one row without meaning
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
-
-
 def kv_append(K, V, cache, page_table, kv_lens, workspace, cu_rows=None):
     """Quantizes the rows' keys and values (K, V [rows, kv_heads, D] float16 / bfloat16; rows may be strided)
     into the cache.  Rows cu_rows[b] .. cu_rows[b + 1] - 1 are the last positions of sequence b, whose
     length kv_lens[b] counts them already; without cu_rows, one row per sequence."""
-    ks, vs = _rows_of(K, "K"), _rows_of(V, "V")
-    rows, kv_heads, D = K.shape
-    if V.dtype != K.dtype:
-        raise TypeError("V: expected the type of K")
-    _is(V, K.shape, "V")
-    batch, tail = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, D, workspace, "kv_append", K, V)
-    _check(lib.w4a8_kv_append(K.data_ptr(), V.data_ptr(), _DTYPES[K.dtype], ks, vs, *batch, rows, *tail), "w4a8_kv_append")
+    _calls.kv_append(K, V, cache, page_table, kv_lens, workspace, cu_rows)
 
 
 def kv_read(cache, page_table, kv_lens, rows: int, kv_heads: int, head_dim: int, workspace, cu_rows=None,
             dtype=torch.float16, out=None):
     """Reads the keys and values of `rows` rows (numbered as in kv_append) back:
     (K, V) [rows, kv_heads, D] of `dtype`."""
-    if out is None:
-        K = torch.empty((rows, kv_heads, head_dim), dtype=dtype, device=cache.device)
-        V = torch.empty_like(K)
-    else:
-        K, V = (_is(t, (rows, kv_heads, head_dim), "out") for t in out)
-    _dev16(K, "K")
-    if _dev16(V, "V").dtype != K.dtype:
-        raise TypeError("out: expected two tensors of one type")
-    batch, tail = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, head_dim, workspace, "kv_read", K, V)
-    _check(lib.w4a8_kv_read(*batch, rows, K.data_ptr(), V.data_ptr(), _DTYPES[K.dtype], *tail), "w4a8_kv_read")
-    return K, V
+    K, V = (None, None) if out is None else out
+    return _calls.kv_read(cache, page_table, kv_lens, rows, kv_heads, head_dim, workspace, cu_rows, dtype, K, V)
 
 
 def kv_attention(Q, cache, page_table, kv_lens, kv_heads: int, workspace, cu_rows=None, scale=None,
@@ -616,19 +526,7 @@ def kv_attention(Q, cache, page_table, kv_lens, kv_heads: int, workspace, cu_row
     """Attention of Q [rows, q_heads, D] (float16 / bfloat16; rows may be strided) over the cache:
     O [rows, q_heads, D] of `dtype`.  scale: 1 / sqrt(D) by default; lse: a [rows, q_heads] float32
     tensor that receives the logarithms of the softmax denominators."""
-    qs = _rows_of(Q, "Q")
-    rows, q_heads, D = Q.shape
-    if out is None:
-        out = torch.empty((rows, q_heads, D), dtype=dtype, device=Q.device)
-    else:
-        _is(out, Q.shape, "out")
-    _dev16(out, "out")
-    if lse is not None:
-        _is(_dev(lse, torch.float32, "lse"), (rows, q_heads), "lse")
-    batch, tail = _kv_batch(cache, page_table, kv_lens, cu_rows, kv_heads, D, workspace, "kv_attention", Q, out, lse)
-    _check(lib.w4a8_kv_attention(Q.data_ptr(), _DTYPES[Q.dtype], qs, *batch, rows, q_heads, D ** -0.5 if scale is None else scale,
-                                 int(causal), window, out.data_ptr(), _DTYPES[out.dtype], _at(lse), *tail), "w4a8_kv_attention")
-    return out
+    return _calls.kv_attention(Q, cache, page_table, kv_lens, kv_heads, workspace, cu_rows, scale, causal, window, dtype, out, lse)
 
 
 def linear_static(Xq, tok_scale, packed, bias, N: int, group: int, out):
