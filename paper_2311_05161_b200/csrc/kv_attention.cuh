@@ -11,9 +11,10 @@ constexpr uint32_t kSuspendHintNs = 20000;                 // a waiting thread i
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoReference = -1.0e30f;
 constexpr float kSlack = 15.0f;                            // weights stay below 2^15, within binary16
-// A reference that moves is put this far below the largest exponent, so that weights down to 2^-32 of the largest
-// one are more than binary16's zero (many small ones can add up), with 8 bits left above for what comes later.
-constexpr float kRoom = 7.0f;
+// A reference that moves is put this far below the largest exponent, so that weights down to 2^-29 of the largest
+// one are more than binary16's zero: a hundred thousand of those add up to 2^-12 of it, half a step of a weight.
+// (Every bit of it is one less above, for what comes later; 7 bits cost the many-row form 4 % in moved references.)
+constexpr float kRoom = 4.0f;
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p)
 {
