@@ -452,7 +452,8 @@ w4a8_status w4a8_kv_read(const void *cache, int num_pages, int page_size, int kv
 /* Attention of the rows' queries over the cached keys and values of their sequences, without
  * expanding the cache in memory:  o = sum_j p_j v_j,  p = softmax_j(scale * q . k_j).
  *   Q          [rows][q_heads][D] W4A8_F16 or W4A8_BF16 (q_type); q_heads a multiple of kv_heads,
- *              query head h reads key head h / (q_heads / kv_heads).
+ *              query head h reads key head h / (q_heads / kv_heads).  A row and head whose queries
+ *              are not all finite gets an undefined result; no other does.
  *   scale      > 0 (1 / sqrt(D) as a rule).
  *   causal     non-zero: a row sees positions up to its own; zero: the whole sequence.
  *   window     > 0: a row sees only positions above its own minus window; 0: no limit.

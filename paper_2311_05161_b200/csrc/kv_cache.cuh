@@ -11,7 +11,7 @@
 //    thread load its slice of a token pair with one 16-byte access, without bank conflicts.
 //  - A code is a rank i = y + z + 1, where y is the level x for |x| < 1 doubled and moved out by one
 //    for |x| >= 1: the level is y - clamp(y / 2, -1, 1), three packed binary16 operations
-//    (expand in kv_attention.cu) where a table lookup would need a table per token.
+//    (expand in kv_attention.cuh) where a table lookup would need a table per token.
 //  - The ranks of a 16-bit half are rotated left by two bits: two of them then lie at bits 2-5 and
 //    6-9, inside the mantissa of a binary16 number, and swapping the half's bytes brings the
 //    other two there.

@@ -6,7 +6,7 @@
 // from tensor memory, where it takes the place of its scores.  Tensor memory is full: two score buffers of 64
 // columns and an output tile of 128 per row tile.  Two buffers, so that the scores of the next unit are
 // computed while the softmax of this one runs (units of 128 tokens with one buffer left every row tile with
-// a chain of softmax and MMAs: 173 us on the 1024-row chunk below).
+// a chain of softmax and MMAs: 173 against 159 us on the 1024-row chunk below).
 //
 // Roles: eight softmax warps, a thread per row; eight expanding warps, four threads per token, which turn a unit's
 // codes into binary16 operand tiles in shared memory (four units of keys and values); two
@@ -21,9 +21,13 @@
 // pass that computed the weights at once and again after an overflow was slower: on scores that spread
 // over five bits one unit in eight overflowed in some row of a warp.)
 //
-// Bounds per unit and SM for D = 128: 2048 cycles of MMA (two 128 x 128 x 128 products per row
-// tile), 2048 cycles of exponentials at 16 per cycle, about 1000 cycles of packed binary16 arithmetic to
-// expand 32768 codes: the expansion is shared by 256 rows, which is why the two tiles are one CTA's.
+// Bounds per unit and SM for D = 128: 1024 cycles of MMA (a 128 x 64 x 128 and a 128 x 128 x 64 product per row
+// tile), 1024 cycles of exponentials at 16 per cycle, about 500 cycles of packed binary16 arithmetic to
+// expand 16384 codes: the expansion is shared by 256 rows, which is why the two tiles are one CTA's.
+// Measured: a chunk of 1024 tokens behind 3072 others (8 key heads, 32 query heads of 128) 106 us, 565 TFLOP/s, tensor
+// pipe 28 %, issue slots 56 % busy; some 2300 cycles per unit, the softmax's chain of wait, load, maximum,
+// exponentials and store being the longest.  4 prompts of 2048: 276 us.  (Sixteen softmax warps, two threads per row, were
+// slower for their exchange of maxima: 120 us.)
 #include <type_traits>
 
 #include "kv_attention.cuh"
@@ -39,6 +43,7 @@ constexpr int kRing = 4;                                   // units of expanded 
 constexpr int kConstSlots = 8;                             // more than kRing: a slot is rewritten after its unit's softmax
 constexpr int kLead = 6;                                   // an item's fixed cost, in units
 constexpr int kWaitSite = 950;
+constexpr int kApart = 16;                                 // a row at most 2^16 below its tile's largest is good to 2^-23 of its own largest element
 
 // -------------------------------------------------------------------- tensor core wrappers
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
@@ -170,7 +175,8 @@ struct Layout {
     static constexpr int kOffConst = kOffV + kRing * kTile;
     static constexpr int kConstBytes = kUnit * 12;         // per token: key step * unit; log2 of the value step; its inverse
     static constexpr int kOffQmax = kOffConst + kConstSlots * kConstBytes;
-    static constexpr int kOffBars = kOffQmax + 2 * kSoftmaxWarps * 4;
+    static constexpr int kOffRowScale = kOffQmax + 2 * kSoftmaxWarps * 4;        // per row, see the queries
+    static constexpr int kOffBars = kOffRowScale + kRows * 4;
     // barriers
     static constexpr int kKFull = 0, kKEmpty = kKFull + kRing, kVFull = kKEmpty + kRing, kVEmpty = kVFull + kRing,
                          kSFull = kVEmpty + kRing, kPReady = kSFull + 4, kODone = kPReady + 4,
@@ -323,6 +329,14 @@ struct Walk {
     }
 };
 
+// e such that x 2^-e is in [2^14, 2^15), the top of binary16's range; both powers normal in binary32.
+__device__ __forceinline__ int query_exponent(float x) { return min(max((int)((__float_as_uint(x) >> 23) & 255u) - 127 - 14, -100), 113); }
+
+__device__ __forceinline__ float power_of_two(int e)
+{
+    return __uint_as_float(e >= -126 ? (uint32_t)(127 + e) << 23 : e >= -149 ? 1u << (149 + e) : 0u);
+}
+
 // Eight elements of the output in their order, from element `at` of O on.
 __device__ __forceinline__ void store_eight(const KvAttnArgs &a, size_t at, const float (&x)[8])
 {
@@ -468,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 constexpr int kPer = D / 8, kTogether = 32 / kPer;   // lanes per row, rows at a time
                 const int c = lane % kPer;
                 uint4 raw[kPer];
-                float amax = 0.0f;
+                uint32_t row_max[kPer];                    // magnitudes, as their 15 bits
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) {
                     const int at = (r & ~31) + k * kTogether + lane / kPer, q_flat = pc.tile * kRows + at, q_i = sc.group.div(q_flat);
@@ -479,14 +493,22 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                                                                        (size_t)q_head * D) + c);
                 }
 #pragma unroll
-                for (int k = 0; k < kPer; ++k)
+                for (int k = 0; k < kPer; ++k) {
+                    uint32_t v = 0u;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t v = (&raw[k].x)[e] & 0x7fff7fffu;
-                        const float2 x = a.q_bf16 ? make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u))
-                                                  : __half22float2(*reinterpret_cast<const __half2 *>(&v));
-                        amax = fmaxf(amax, fmaxf(x.x, x.y));
+                    for (int e = 0; e < 4; ++e) v = __vmaxu2(v, (&raw[k].x)[e] & 0x7fff7fffu);
+                    row_max[k] = max(v & 0xffffu, v >> 16);
+                }
+                // the lanes of a row group reduce their rows together: lane c is left with the maximum of its c-th
+#pragma unroll
+                for (int o = kPer / 2; o > 0; o >>= 1)
+#pragma unroll
+                    for (int k = 0; k < o; ++k) {
+                        const uint32_t send = (lane & o) ? row_max[k] : row_max[k + o], keep = (lane & o) ? row_max[k + o] : row_max[k];
+                        row_max[k] = max(keep, __shfl_xor_sync(0xffffffffu, send, o));
                     }
+                const float row_top = a.q_bf16 ? __uint_as_float(row_max[0] << 16) : __half2float(__ushort_as_half((unsigned short)row_max[0]));
+                float amax = row_top < INFINITY ? row_top : 0.0f;
                 amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
                 volatile float *qmax = reinterpret_cast<float *>(smem + L::kOffQmax) + (item_no & 1) * kSoftmaxWarps;
                 if (lane == 0) {
@@ -496,11 +518,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 if (!(ok = wait_warp(bar(L::kQmax), item_no & 1, ctl, sc.sb, kWaitSite))) break;
 #pragma unroll
                 for (int k = 0; k < kSoftmaxWarps; ++k) amax = fmaxf(amax, qmax[k]);
-                const int e = min(max((int)((__float_as_uint(amax) >> 23) & 255u) - 127 - 14, -100), 113);
-                const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+                // One power of two for the tile's 256 rows, so that a token's constants serve them all.  A row so much smaller
+                // that binary16 would lose it has a power of its own; its scores are scaled back one by one.
+                const int e_tile = query_exponent(amax), e_row = query_exponent(row_top);
+                const bool apart = row_top > 0.0f && e_row < e_tile - kApart;
+                const bool some_apart = __any_sync(0xffffffffu, apart);
+                float *row_scale = reinterpret_cast<float *>(smem + L::kOffRowScale) + (r & ~31);
+                row_scale[c * kTogether + lane / kPer] = apart ? power_of_two(e_row - e_tile) : 1.0f;
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) {
                     const int at = (r & 96) + k * kTogether + lane / kPer;     // row of the tile of 128
+                    float down = power_of_two(-e_tile);
+                    if (some_apart) down = power_of_two(-__shfl_sync(0xffffffffu, apart ? e_row : e_tile, (lane & ~(kPer - 1)) + k));
                     float f[8];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -518,6 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 fence_async();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(L::kQFull + w));
+                const float scale_back = row_scale[lane];
                 // rows of this warp's tile: what all of them see
                 const int t_first = sc.group.div(pc.tile * kRows + w * 128);
                 const int t_last = sc.group.div(pc.tile * kRows + max(w * 128, min(pc.rows, w * 128 + 128) - 1));
@@ -535,6 +565,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     // pipe, and the register moves that align their operands cost more than they saved.)
                     float x[kUnit];
                     tmem_load64(s_addr, x);
+                    if (some_apart) {
+#pragma unroll
+                        for (int k = 0; k < kUnit; ++k) x[k] *= scale_back;
+                    }
 #pragma unroll
                     for (int k = 0; k < kUnit; k += 4) {
                         const float4 f = load_shared4(ks_addr + 4 * k), g = load_shared4(ks_addr + 4 * (kUnit + k));
@@ -720,8 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             float amax = 0.0f;
 #pragma unroll
             for (int k = 0; k < kSoftmaxWarps; ++k) amax = fmaxf(amax, qmax[k]);
-            const int e = min(max((int)((__float_as_uint(amax) >> 23) & 255u) - 127 - 14, -100), 113);
-            const float unit = -2.0f * (a.scale * kLog2e) * __uint_as_float((uint32_t)(127 + e) << 23);
+            const float unit = -2.0f * (a.scale * kLog2e) * __uint_as_float((uint32_t)(127 + query_exponent(amax)) << 23);
             ++item_no;
             // Eight levels (times -1/2) of a code word; off = (16 + z) / 2 twice.
             auto levels = [&](uint32_t w, uint32_t off, uint32_t (&o)[4]) {

@@ -200,6 +200,29 @@ def test_one_distant_token_against_many_light_ones():
         check_attention(O, o, allow, BF16)
 
 
+@pytest.mark.parametrize("rows", [None, 100])
+@pytest.mark.parametrize("extreme", ["large", "inf", "nan"])
+def test_a_row_of_extreme_queries_leaves_the_others_alone(rows, extreme):
+    """One query head of one row holds values 2^90 above the others', or ones that are not finite: the other
+    rows and heads of its tile are what they are without it."""
+    H, D, n = 2, 128, 300
+    bt = Batch([n], None if rows is None else [rows], 64)
+    cache = filled_cache(bt, H, D)
+    Q = vectors((bt.rows, 8, D), 3, BF16)
+    row, head = bt.rows // 2, 1
+    Q[row, head] = {"large": Q[row, head] * 2.0 ** 90, "inf": math.inf, "nan": math.nan}[extreme]
+    Q[row, 7] *= 2.0 ** -20                                # and a small one, apart from its tile without the large one
+    Q = Q.cuda()
+    ws = w4a8.new_kv_workspace(bt.rows, 1, 8, H, D)
+    O = w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, H, ws, cu_rows=bt.cu, scale=0.1)
+    w4a8.check_status(ws)
+    Q[row, head] = 0
+    o, _, allow = attention_reference(Q, cache, bt, H, 0.1)
+    O[row, head] = 0
+    o[row, head] = 0
+    check_attention(O, o, allow, F16)
+
+
 def _problem(lens, rows, P, Hq, H, D, seed):
     bt = Batch(lens, rows, P, seed=seed)
     cache = filled_cache(bt, H, D, seed=seed)
