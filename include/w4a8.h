@@ -459,6 +459,7 @@ w4a8_status w4a8_kv_read(const void *cache, int num_pages, int page_size, int kv
  *   window     > 0: a row sees only positions above its own minus window; 0: no limit.
  *   O          out [rows][q_heads][D] W4A8_F16 (what w4a8_quantize_act takes next) or W4A8_BF16
  *              (o_type).  A row that sees no key gets zeros.
+ *              O and lse may not overlap Q or the cache.
  *   lse        out [rows][q_heads] FP32, natural logarithm of the softmax's denominator
  *              (-inf for a row that sees no key), or NULL.
  * Precision: scores, maxima and sums in binary32; the weights p enter the value product in

@@ -172,7 +172,7 @@ struct Sight {
     bool causal;
     __device__ Sight(const KvAttnArgs &a, const Seq &s) : pos0(s.len - s.n), len(s.len), window(a.window), causal(a.causal != 0) {}
     __device__ int hi(int i) const { return pos0 + i < 0 ? 0 : causal ? pos0 + i + 1 : len; }
-    __device__ int lo(int i) const { return window > 0 ? max(0, pos0 + i + 1 - window) : 0; }
+    __device__ int lo(int i) const { return window > 0 ? (int)max(0ll, (long long)pos0 + i + 1 - window) : 0; }
 };
 
 // Counters of shared items in the workspace, behind the status block.  Both kernels use this region and

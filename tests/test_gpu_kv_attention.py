@@ -82,6 +82,8 @@ def test_rows_that_see_nothing():
     """More rows than tokens: the rows in front of position 0 get zeros; an empty sequence too."""
     O = run([2, 0, 5], [6, 3, 1], 16, 4, 2, 64)
     assert bool((O[:4] == 0).all()) and bool((O[6:9] == 0).all()) and bool((O[4:6] != 0).any())
+    for rows in ([6, 3, 1], [150, 3, 70]):                 # a window beyond any position hides nothing
+        assert torch.equal(run([2, 0, 5], rows, 16, 4, 2, 64), run([2, 0, 5], rows, 16, 4, 2, 64, window=2 ** 31 - 1))
 
 
 @pytest.mark.parametrize("window", [1, 7, 16, 100, 5000])
@@ -375,11 +377,12 @@ def test_bad_tables_are_reported():
         return torch.tensor(v, dtype=torch.int32, device="cuda")
 
     good = i32(0, 1).view(2, 1)
-    for rows in (2, 8):
+    for rows in (2, 8, 100):                               # one row each, a few, many
         Q = vectors((rows, 4, D), 1, F16).cuda()
-        ok = None if rows == 2 else i32(0, 4, 8)
+        ws = w4a8.new_kv_workspace(rows, 2, 4, H, D)
+        ok = None if rows == 2 else i32(0, rows // 2, rows)
         for table, lens, cu in ((i32(4, 1).view(2, 1), i32(3, 3), ok), (i32(0, -1).view(2, 1), i32(9, 9), ok),
-                                (good, i32(3, 17), ok), (good, i32(-1, 3), ok), (good, i32(3, 3), i32(0, 1, 50)),
+                                (good, i32(3, 17), ok), (good, i32(-1, 3), ok), (good, i32(3, 3), i32(0, 1, rows + 1)),
                                 (good, i32(3, 3), i32(0, -4, 2))):
             w4a8.kv_attention(Q, cache, table, lens, H, ws, cu_rows=cu)
             assert w4a8.poll_status(ws) == 9, (rows, table, lens, cu)

@@ -102,3 +102,19 @@ def test_add_norm_refusals(w4a8):
     for k in ("X", "res", "out", "w", "b", "Xq"):
         assert f(*args(**{k: P(GOOD + 8)})) == 3, k
     assert f(*args(tok=P(GOOD + 2))) == 3
+
+
+def test_python_calls_refuse_before_they_touch_a_device(w4a8):
+    """Tensors of the host, wrong types and numbers raise in the marshalling; nothing is launched."""
+    import torch
+    w = w4a8
+    half, page = torch.zeros(1, 4, 64, dtype=torch.float16), torch.zeros(1, 16 * 72, dtype=torch.uint8)
+    one = torch.ones(1, 1, dtype=torch.int32)
+    for call in (lambda: w.kv_attention(half, page, one, one[0], 1, page), lambda: w.kv_append(half, half, page, one, one[0], page),
+                 lambda: w.kv_read(page, one, one[0], 1, 1, 64, page), lambda: w.kv_attention(None, page, one, one[0], 1, page),
+                 lambda: w.kv_attention(half, page, one, one[0], "1", page), lambda: w.add_norm_quantize_act(half, half, half),
+                 lambda: w.add_norm_quantize_act(1, 2, 3)):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(ValueError):
+        w.kv_read(page, one, one[0], 1, 2 ** 40, 64, page)
