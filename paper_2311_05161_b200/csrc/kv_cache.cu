@@ -128,11 +128,11 @@ kv_append_kernel(const T *__restrict__ K, const T *__restrict__ V, long long k_s
                     x[2 * k] = f.x;
                     x[2 * k + 1] = f.y;
                 }
-                float lo = fminf(x[0], 0.0f), hi = fmaxf(x[0], 0.0f);
+                float lo = 0.0f, hi = 0.0f;
 #pragma unroll
-                for (int k = 1; k < 8; ++k) {
-                    lo = fminf(lo, x[k]);
-                    hi = fmaxf(hi, x[k]);
+                for (int k = 0; k < 8; k += 2) {
+                    lo = min3(lo, x[k], x[k + 1]);
+                    hi = max3(hi, x[k], x[k + 1]);
                 }
 #pragma unroll
                 for (int o = LPV / 2; o > 0; o >>= 1) {

@@ -61,6 +61,19 @@ __device__ __forceinline__ int kv_page_of(const KvCache &c, const KvBatch &bt, i
     return (unsigned)p < (unsigned)c.num_pages ? p : -1;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float d;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // Address of the block that holds token slot `slot` of head h of a page.
 __device__ __forceinline__ uint8_t *kv_block_at(const KvCache &c, int page, int h, int slot)
 {
@@ -95,14 +108,13 @@ __device__ __forceinline__ uint32_t kv_range_word(float lo, float hi, float &r, 
 // Eight consecutive elements as a code word: Eq. 5, the levels numbered in ascending order.  With u = x r, the place y
 // of a level counted from zero is 0 for |u| <= 1/4, +-1 for |u| <= 3/4 (the specials) and
 // +-(rint|u| + 1) beyond; the rank is y + z + 1.  The clamp of Eq. 5 acts at the upper end only: the least element's u is
-// -z before rounding.  Rounding and conversion are additions of 1.5 * 2^23, which leave the integer in the
-// mantissa's low bits (the constant's own low 16 bits are zero).
+// -z before rounding.  y is the smaller of rint(f |u|) and rint|u| + 1, where f is the binary32 number in front of 2 (with 2
+// itself, 3/4 would be a tie): equal to the definition for every binary32 |u| below 16.  Rounding and conversion are additions of 1.5 * 2^23 (minus one), which leave the integer in the mantissa's low bits (the
+// constant's own low 16 bits are zero).
 __device__ __forceinline__ uint32_t kv_rank_bits(float x, float r, float top, float bias)
 {
     const float u = __fmul_rn(x, r);
-    float y = __fadd_rn(__fadd_rn(fabsf(u), 12582912.0f), -12582911.0f);
-    y = fabsf(u) > 0.75f ? y : 1.0f;
-    y = fabsf(u) > 0.25f ? y : 0.0f;
+    const float y = __fadd_rn(fminf(__fmaf_rn(fabsf(u), 0x1.fffffep0f, 12582911.0f), __fadd_rn(fabsf(u), 12582912.0f)), -12582911.0f);
     return __float_as_uint(__fadd_rn(fminf(copysignf(y, u), top), bias));
 }
 __device__ __forceinline__ uint32_t kv_code_word(const float (&x)[8], float r, int z)

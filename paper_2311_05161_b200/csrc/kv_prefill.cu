@@ -131,12 +131,6 @@ __device__ __forceinline__ void tmem_load64(uint32_t addr, float (&r)[64])
         : "r"(addr)
         : "memory");
 }
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
 __device__ __forceinline__ float4 load_shared4(uint32_t addr)
 {
     float4 v;
