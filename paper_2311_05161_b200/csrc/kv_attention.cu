@@ -30,9 +30,9 @@
 // bulk copies.
 //
 // Measured (8 key heads of 128 unless said): 64 ragged sequences of 1000 to 6000 tokens, 8 query heads per key
-// head, 248 MB: 79.6 us, 3.1 TB/s, issue slots 66 %, binary16 pipe 53 %, logic pipe 48 % busy.  One sequence of
-// 131001 tokens 52.5 us; 32 ragged sequences with 32 heads of their own 55.9 us; 513 tokens 9.2 us.  Beside the main
-// loop (some 36 us of the 52.5 us, at 1200 cycles per 32 tokens and scheduler) stand 8 us until the first
+// head, 248 MB: 80 us, 3.1 TB/s, issue slots 66 %, binary16 pipe 53 %, logic pipe 48 % busy.  One sequence of
+// 131001 tokens 52.8 us; 32 ragged sequences with 32 heads of their own 56.1 us; 513 tokens 9.2 us.  Beside the main
+// loop (some 36 us of the 52.8 us, at 1200 cycles per 32 tokens and scheduler) stand 8 us until the first
 // unit is there (place on the list, page numbers, queries, copies, each waiting for the one before) and 4 us for the joins.
 #include "kv_attention.cuh"
 

@@ -24,9 +24,9 @@
 // Bounds per unit and SM for D = 128: 1024 cycles of MMA (a 128 x 64 x 128 and a 128 x 128 x 64 product per row
 // tile), 1024 cycles of exponentials at 16 per cycle, about 500 cycles of packed binary16 arithmetic to
 // expand 16384 codes: the expansion is shared by 256 rows, which is why the two tiles are one CTA's.
-// Measured: the last 1024 of 4096 tokens (8 key heads, 32 query heads of 128) 106 us, 565 TFLOP/s, tensor
+// Measured: the last 1024 of 4096 tokens (8 key heads, 32 query heads of 128) 108 us, 558 TFLOP/s, tensor
 // pipe 28 %, issue slots 56 % busy; some 2300 cycles per unit, the softmax's chain of wait, load, maximum,
-// exponentials and store being the longest.  4 prompts of 2048: 276 us.  (Sixteen softmax warps, two threads per row, were
+// exponentials and store being the longest.  4 prompts of 2048: 286 us.  (Sixteen softmax warps, two threads per row, were
 // slower for their exchange of maxima: 120 us.)
 #include <type_traits>
 
