@@ -464,7 +464,9 @@ w4a8_status w4a8_kv_read(const void *cache, int num_pages, int page_size, int kv
  *              (-inf for a row that sees no key), or NULL.
  * Precision: scores, maxima and sums in binary32; the weights p enter the value product in
  * binary16.  The result does not depend on how the work was scheduled.
- *   workspace >= w4a8_kv_attention_workspace_bytes(rows, batch, q_heads, kv_heads, D). */
+ *   workspace >= w4a8_kv_attention_workspace_bytes(rows, batch, q_heads, kv_heads, D).  (Fewer rows of
+ *              as many sequences need no more; as many rows of fewer sequences may: calls that share a
+ *              workspace take the largest of their sizes.) */
 size_t w4a8_kv_attention_workspace_bytes(int rows, int batch, int q_heads, int kv_heads,
                                          int head_dim);
 w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, const void *cache,

@@ -497,7 +497,8 @@ def kv_attention_workspace_bytes(rows: int, batch: int, q_heads: int, kv_heads: 
 
 
 def new_kv_workspace(rows: int, batch: int, q_heads: int, kv_heads: int, head_dim: int, device="cuda"):
-    """Workspace of the three cache calls for up to `rows` rows of `batch` sequences."""
+    """Workspace of the three cache calls for up to `rows` rows of `batch` sequences (as many rows of fewer
+    sequences may need a larger one)."""
     nbytes = kv_attention_workspace_bytes(rows, batch, q_heads, kv_heads, head_dim)
     if nbytes == 0:
         raise W4A8Error(2, "w4a8_kv_attention_workspace_bytes")
