@@ -229,12 +229,12 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         const uint8_t *head_base = a.cache.pages + ((size_t)h << a.cache.page_shift) * (D + 8);
         const int page_bits = a.cache.page_shift - 4, in_page = (1 << page_bits) - 1;   // in blocks
         const size_t page_bytes = a.cache.page_bytes();
-        // byte offsets of the blocks of this warp's next 16 units: lane 2 i + j has block j of the i-th (a
-        // block behind the sequence's end: the one in front of it again)
+        // byte offsets of the blocks of this warp's next 16 units: lane 2 i + j has block j of the i-th (a block behind
+        // the sequence's end, or in front of what the tile sees: its neighbour again; its page may be gone)
         size_t where = 0;
         int requested = 0;                 // units of this item whose copies were started
         auto look_up = [&](int k) {
-            const int blk = min(2 * (k0 + warp + (k + (lane >> 1)) * WARPS) + (lane & 1), last_block);
+            const int blk = max(min(2 * (k0 + warp + (k + (lane >> 1)) * WARPS) + (lane & 1), last_block), lo_min >> 4);
             int page = __ldg(table + (blk >> page_bits));
             if ((unsigned)page >= (unsigned)a.cache.num_pages) {
                 report_failure(sc.sb, W4A8_ERR_BAD_TABLE, b);

@@ -200,6 +200,7 @@ struct Piece {
     int b, h, tile, rows;                      // sequence, key head, row tile, its rows
     int row0, n, len;                          // of the sequence
     int unit0, count;                          // units to walk; count < 0: no more pieces
+    int lo;                                    // first token that a row of the tile sees
     int whole;                                 // the item lies in this share alone
     int slot;                                  // else: where the part goes
 };
@@ -247,7 +248,7 @@ struct Walk {
     Seq s;
     bool loaded;
     // the current piece
-    int h, rows, i_first, first, units, from, count;
+    int h, rows, i_first, lo, first, units, from, count;
     long long first_unit;                      // the item's first unit on the list
     bool whole;
 
@@ -255,21 +256,22 @@ struct Walk {
 
     __device__ static int tiles_of(const Seq &s, int group) { return (int)(((long long)s.n * group + kRows - 1) / kRows); }
     __device__ static void span(const KvAttnArgs &a, const Schedule &sc, const Seq &s, int tile, int &i_first, int &i_last, int &rows,
-                                int &first, int &units)
+                                int &lo, int &first, int &units)
     {
         rows = (int)min((long long)kRows, (long long)s.n * sc.group.d - (long long)tile * kRows);
         i_first = sc.group.div(tile * kRows);
         i_last = sc.group.div(tile * kRows + rows - 1);
         const Sight sight(a, s);
-        first = sight.lo(i_first) >> kUnitShift;
+        lo = sight.lo(i_first);
+        first = lo >> kUnitShift;
         units = max(0, ((sight.hi(i_last) + kUnit - 1) >> kUnitShift) - first);
     }
     // Places of the row tiles first_tile + lane of a sequence (0 behind the last).
     __device__ static long long tile_places(const KvAttnArgs &a, const Schedule &sc, const Seq &s, int t)
     {
         if (t >= tiles_of(s, (int)sc.group.d)) return 0;
-        int i0, i1, rows, first, units;
-        span(a, sc, s, t, i0, i1, rows, first, units);
+        int i0, i1, rows, lo, first, units;
+        span(a, sc, s, t, i0, i1, rows, lo, first, units);
         return (long long)a.cache.heads * (kLead + max(units, 1));
     }
     __device__ void start(int b0, int tile0, long long off0, long long begin, long long end_)
@@ -299,7 +301,7 @@ struct Walk {
                 continue;
             }
             int i_last;
-            span(a, sc, s, tile, i_first, i_last, rows, first, units);
+            span(a, sc, s, tile, i_first, i_last, rows, lo, first, units);
             const int body = max(units, 1), length = kLead + body;
             if (off >= (long long)a.cache.heads * length) {
                 off -= (long long)a.cache.heads * length;
@@ -692,16 +694,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         for (uint32_t piece_no = 0;; ++piece_no) {
             if (!(ok = wait_warp(bar(L::kPieceFull + (piece_no & 1)), (piece_no >> 1) & 1, ctl, sc.sb, kWaitSite + 13))) break;
             const volatile Piece &pc = ctl->piece[piece_no & 1];
-            const int count = pc.count, unit0 = pc.unit0, len = pc.len, seq = pc.b;
+            const int count = pc.count, unit0 = pc.unit0, lo = pc.lo, len = pc.len, seq = pc.b;
             const uint8_t *head_base = a.cache.pages + ((size_t)pc.h << a.cache.page_shift) * (D + 8);
             __syncwarp();
             if (count >= 0 && lane == 0) mbar_arrive(bar(L::kPieceEmpty + (piece_no & 1)));
             if (count < 0) break;
             if (count == 0) continue;
-            const int last_block = (len - 1) >> 4;
+            const int first_block = lo >> 4, last_block = (len - 1) >> 4;
             const int32_t *table = a.batch.page_table + (size_t)seq * a.batch.max_pages;
-            auto page_of = [&](int u) {                    // page of this thread's token of unit u of the piece
-                const int blk = min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block);
+            // block of this thread's token of unit u of the piece (behind the end, or in front of what the tile sees:
+            // the nearest that it sees; the page of the other may be gone)
+            auto block_no = [&](int u) { return max(min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block), first_block); };
+            auto page_of = [&](int u) {
+                const int blk = block_no(u);
                 int page = __ldg(table + (blk >> page_bits));
                 if ((unsigned)page >= (unsigned)a.cache.num_pages) {
                     report_failure(sc.sb, W4A8_ERR_BAD_TABLE, seq);
@@ -712,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             uint32_t kc[KW];
             uint32_t vc[2][CB / 4], kw = 0, vw = 0;
             auto block_of = [&](int u, int page) {         // this thread's block of unit u
-                const int blk = min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block);
+                const int blk = block_no(u);
                 return head_base + (size_t)page * page_bytes + (size_t)(blk & in_page) * (16 * (D + 8));
             };
             const int t = tk & 15;
@@ -903,6 +908,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     p.len = walk.s.len;
                     p.unit0 = walk.first + walk.from;
                     p.count = walk.count;
+                    p.lo = walk.lo;
                     p.whole = walk.whole;
                     p.slot = walk.first_unit <= begin ? 0 : 1;
                     if (!walk.whole && walk.first_unit >= begin) {       // begins here and ends in a later share
