@@ -423,9 +423,12 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                             const int r = n * 8 + 2 * t + (i & 1), at = j0 + 16 * j + g + (i >> 1) * 8;
                             if (at < row_lo[r] || at >= row_hi[r]) wt[j][n][i] = -INFINITY;
                         }
-                    // behind the sequence's end the words are anything
-                    if (j0 + 16 * j + g >= s.len) inv[j][0] = 0.0f;
-                    if (j0 + 16 * j + g + 8 >= s.len) inv[j][1] = 0.0f;
+                    // the words of a token that no row sees are anything (behind the end, in front of the window)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int at = j0 + 16 * j + g + 8 * i;
+                        if (at < lo_min || at >= s.len) inv[j][i] = 0.0f;
+                    }
                 }
             }
             // ---- weights ----

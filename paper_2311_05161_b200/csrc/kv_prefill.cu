@@ -770,7 +770,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             };
             for (int u = 0; u < count; ++u, ++unit_no) {
                 const uint32_t buf = unit_no % kRing, use = unit_no / kRing & 1, slot = unit_no % kConstSlots;
-                const bool there = (unit0 + u) * kUnit + tk < len;
+                const int at = (unit0 + u) * kUnit + tk;
+                const bool there = at >= lo && at < len;     // else its words are anything
                 // ---- keys ----
                 if (unit_no >= kRing && !(ok = wait_warp(bar(L::kKEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 5, 200))) break;
                 {
@@ -784,7 +785,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                                          : "memory");
                         }
                 }
-                if (quarter == 0) {                        // (a token behind the end weighs nothing)
+                if (quarter == 0) {                        // (a token behind the end or in front of the window weighs nothing)
                     float *ks = reinterpret_cast<float *>(smem + L::kOffConst + slot * L::kConstBytes) + tk;
                     const float step = __uint_as_float(vw & ~15u);
                     ks[0] = there ? __uint_as_float(kw & ~15u) * unit : 0.0f;
