@@ -8,8 +8,7 @@
 #include <stdint.h>
 #include <string.h>
 
-#include <atomic>
-
+#include "smem_limit.cuh"
 #include "w4a8.h"
 
 namespace w4a8 {
@@ -228,24 +227,7 @@ __device__ __forceinline__ void dependent_wait()
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-constexpr int kMaxDevices = 64;
-
 #ifdef __CUDACC__
-// Raises a kernel's dynamic shared-memory limit to `bytes` unless an earlier call on this device
-// already set it at least that high (`raised`: one slot per device, an array per kernel instance).
-template <typename Kernel>
-inline cudaError_t raise_smem_limit(Kernel kernel, int bytes, std::atomic<int> (&raised)[kMaxDevices])
-{
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    const bool slot = dev >= 0 && dev < kMaxDevices;
-    if (slot && raised[dev].load(std::memory_order_acquire) >= bytes) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess && slot) raised[dev].store(bytes, std::memory_order_release);
-    return e;
-}
-
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_overlapped_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block,
                                              size_t smem, cudaStream_t st, int cluster,

@@ -30,7 +30,6 @@ constexpr int kGemvMaxSteps = 8;    // steps per CTA: a K slice is at most 16 k-
 constexpr int kGemvDepth = 2;       // steps of codes in flight per thread (asynchronous copies)
 constexpr int kGemvRingBytes = kGemvDepth * kGemvKb * 4 * 128 * 16;   // 32 KiB per CTA
 constexpr int kGemvMaxTokens = 4;
-constexpr int kMaxGemvDevices = 64;
 
 // One k-block (128 input features) of one output row against MT tokens: w = the row's 64 bytes
 // of codes, xk = the tokens' INT8 values of this k-block (token stride in bytes).
@@ -605,25 +604,12 @@ linear_gemv_rows_kernel(const GemvParams P)
     }
 }
 
-// Raise a kernel's dynamic shared-memory limit to `bytes` unless an earlier call on this device
-// already set it at least that high (one slot per kernel instance and device).
-template <typename Kernel>
-void ensure_dynamic_smem(Kernel kern, int bytes, std::atomic<int> (&set_bytes)[kMaxGemvDevices])
-{
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxGemvDevices) dev = -1;
-    if (dev >= 0 && set_bytes[dev].load(std::memory_order_acquire) >= bytes) return;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess &&
-        dev >= 0)
-        set_bytes[dev].store(bytes, std::memory_order_release);
-}
-
 template <int MT, bool GROUPED, int W, int BITS = 4>
 void launch_rows(const GemvParams &P, cudaStream_t st)
 {
     const int smem = MT * P.L.K + W * MT * 32 * 4 + MT * P.L.k_blocks * 4;
-    static std::atomic<int> set_bytes[kMaxGemvDevices] = {};
-    ensure_dynamic_smem(linear_gemv_rows_kernel<MT, GROUPED, W, BITS>, smem, set_bytes);
+    static std::atomic<int> raised[kMaxDevices];
+    raise_smem_limit(linear_gemv_rows_kernel<MT, GROUPED, W, BITS>, smem, raised);     // (a failure shows at the launch)
     launch_overlapped(linear_gemv_rows_kernel<MT, GROUPED, W, BITS>, dim3(P.L.n_tiles * 4), dim3(32 * W),
                       (size_t)smem, st, P);
 }
@@ -673,8 +659,8 @@ template <int MT, bool GROUPED>
 void launch_gemv(dim3 grid, const GemvParams &P, cudaStream_t st)
 {
     constexpr int smem = kGemvRingBytes + MT * kGemvMaxSteps * kGemvKb * kTileK;
-    static std::atomic<int> set_bytes[kMaxGemvDevices] = {};
-    ensure_dynamic_smem(linear_gemv_kernel<MT, GROUPED>, smem, set_bytes);
+    static std::atomic<int> raised[kMaxDevices];
+    raise_smem_limit(linear_gemv_kernel<MT, GROUPED>, smem, raised);
     launch_overlapped(linear_gemv_kernel<MT, GROUPED>, grid, dim3(128), smem, st, P);
 }
 
