@@ -395,7 +395,7 @@ w4a8_status w4a8_attn_pv(const int8_t *Pq, const float *p_scale, const void *pac
  * by a token at a time has only the token to take a range from: here every key and value vector
  * (one token, one head, D elements) is quantized by itself with the dINT4 quantizer of Eq. 5,
  *   lo = min(0, min x), hi = max(0, max x), step = (hi/2 - lo/2) / 6.5 rounded to 20 significant
- *   bits (1 when the quotient is below 2^-100: such a vector is stored as zeros), r = 1 / step,
+ *   bits (2^-64 when the quotient is below 2^-100: such a vector is stored as zeros), r = 1 / step,
  *   z = clamp(rint(-lo * r), 0, 13), and per element u = x * r: +-1/2 when 1/4 < |u| <= 3/4, else
  *   clamp(rint(u) + z, 0, 13) - z; the stored value is that level times step
  * (binary32, one rounding per operation, round half to even).

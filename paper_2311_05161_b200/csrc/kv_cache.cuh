@@ -98,7 +98,11 @@ __device__ __forceinline__ int kv_word_offset(int D, int is_value, int s)
 __device__ __forceinline__ uint32_t kv_range_word(float lo, float hi, float &r, int &z)
 {
     const float raw = __fdiv_rn(__fsub_rn(__fmul_rn(hi, 0.5f), __fmul_rn(lo, 0.5f)), 6.5f);
-    uint32_t bits = 0x3f800000u;             // 1.0f
+    // A vector of zeros gets a step far below any that matters: attention takes a value's step for the size of what the
+    // token adds to the output (with a step of 1, a token of high score and zero value pushed the weights of values of
+    // 2^-14 below binary16).  Not smaller still, so that the token's part of the denominator, a weight times 1 / step,
+    // keeps 60 bits below the weights of values as large as binary16 holds.
+    uint32_t bits = 0x1f800000u;             // 2^-64
     if (raw >= 0x1p-100f) bits = (__float_as_uint(raw) + 8u) & ~15u;
     r = __fdiv_rn(1.0f, __uint_as_float(bits));
     z = (int)fminf(rintf(__fmul_rn(-lo, r)), 13.0f);
