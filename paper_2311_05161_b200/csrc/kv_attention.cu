@@ -337,6 +337,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         ExpandConsts ek = {kNibble, kMinusEight};
         asm volatile("" : "+r"(ek.nibble), "+r"(ek.minus_eight));
         const uint32_t only_g0 = g == 0 ? 0xffffffffu : 0u;
+        bool full = false;                 // a row's denominator has passed kFull
 
         for (int k = 0; k < nk; ++k) {
             const uint32_t bar = bars + stage * 8;
@@ -432,7 +433,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 }
             }
             // ---- weights ----
-            bool over = false;
+            bool over = full;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const float a0 = fmaxf(fmaxf(wt[0][n][0], wt[0][n][2]), fmaxf(wt[1][n][0], wt[1][n][2]));
@@ -440,11 +441,13 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 over |= a0 > ref[n][0] + kSlack || a1 > ref[n][1] + kSlack;
             }
             if (__any_sync(0xffffffffu, over)) {
+                full = false;
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         float m = fmaxf(fmaxf(wt[0][n][j], wt[0][n][2 + j]), fmaxf(wt[1][n][j], wt[1][n][2 + j]));
+                        if (l[n][j] > kFull) m = fmaxf(m, ref[n][j] + (kShift + kRoom));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -509,7 +512,12 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                     }
             }
             __syncwarp();                  // every lane is done with the slot
-            if (k + S::kStages < nk) request(k + S::kStages, stage);
+            if (k + S::kStages < nk) {
+                request(k + S::kStages, stage);
+                if ((k + S::kStages & 15) == 0)              // (every 16 units will do)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) full |= l[n][0] > kFull || l[n][1] > kFull;
+            }
             if (++stage == S::kStages) {
                 stage = 0;
                 parity ^= 1u;
@@ -525,9 +533,10 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                 v += __shfl_xor_sync(0xffffffffu, v, 4);
                 v += __shfl_xor_sync(0xffffffffu, v, 8);
                 v += __shfl_xor_sync(0xffffffffu, v, 16);
-                if (g == 0) {
-                    row_m[warp][n * 8 + 2 * t + j] = ref[n][j];
-                    row_l[warp][n * 8 + 2 * t + j] = v;
+                if (g == 0) {              // (the same sum with a higher reference where it is large)
+                    const bool large = v > kFull;
+                    row_m[warp][n * 8 + 2 * t + j] = large ? ref[n][j] + kLift : ref[n][j];
+                    row_l[warp][n * 8 + 2 * t + j] = large ? v * 0x1p-20f : v;
                 }
             }
         __syncthreads();                   // also: no warp still reads its ring

@@ -15,6 +15,10 @@ constexpr float kSlack = 15.0f;                            // weights stay below
 // one are more than binary16's zero: a hundred thousand of those add up to 2^-12 of it, half a step of a weight.
 // (Every bit of it is one less above, for what comes later; 7 bits cost the many-row form 4 % in moved references.)
 constexpr float kRoom = 4.0f;
+// The denominator sums weight / step, up to 2^(15 + 100) each.  A reference also moves, by kShift, where a sum has passed
+// kFull: a hundred more stay below 2^122.  Where sums are joined, large ones are taken against a
+// reference kLift higher first.
+constexpr float kFull = 0x1p100f, kShift = 16.0f, kLift = 20.0f;
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p)
 {

@@ -587,9 +587,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     }
                     const float top = fmaxf(top0, top1);
                     const bool fresh = m == kNoReference;
-                    const bool over = top > (fresh ? kNoReference : m + kSlack);
+                    const bool full = l > kFull, over = full || top > (fresh ? kNoReference : m + kSlack);
                     if (__any_sync(0xffffffffu, over)) {     // move the reference and scale what has been summed
-                        const float to = over ? top - kRoom : m;
+                        const float to = over ? fmaxf(top - kRoom, full ? m + kShift : kNoReference) : m;
                         const float keep = fresh ? 0.0f : ex2(m - to);
                         m = to;
                         l *= keep;
@@ -951,9 +951,13 @@ __global__ void __launch_bounds__(D) kv_prefill_join_kernel(const __grid_constan
     constexpr size_t kPart = kRows * (D + 2);
     const float *rest = sc.partials + (size_t)blockIdx.y * 2 * kPart, *first = rest + (item.inside ? kPart : 0);
     auto part = [&](int k) { return k == 0 ? first : rest + (size_t)k * 2 * kPart; };
-    float top = kNoReference;
+    float top = kNoReference, most = 0.0f;
 #pragma unroll 4
-    for (int k = 0; k < item.parts; ++k) top = fmaxf(top, __ldcg(part(k) + r));
+    for (int k = 0; k < item.parts; ++k) {
+        top = fmaxf(top, __ldcg(part(k) + r));
+        most = fmaxf(most, __ldcg(part(k) + kRows + r));
+    }
+    if (most > kFull) top += kLift;            // the sums below fit whatever the parts hold
     float acc[32], lsum = 0.0f;
 #pragma unroll
     for (int k = 0; k < 32; ++k) acc[k] = 0.0f;
