@@ -9,7 +9,7 @@ namespace w4a8 {
 constexpr unsigned long long kWaitNs = 2000000000ull;      // limit of every bounded wait
 constexpr uint32_t kSuspendHintNs = 20000;                 // a waiting thread is woken when the phase completes; until then it stays out of the issue slots
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kNoReference = -1.0e30f;
+constexpr float kNoReference = -3.402823466e38f;           // below every score: of a row that has seen no key
 constexpr float kSlack = 15.0f;                            // weights stay below 2^15, within binary16
 // A reference that moves is put this far below the largest exponent, so that weights down to 2^-29 of the largest
 // one are more than binary16's zero: a hundred thousand of those add up to 2^-12 of it, half a step of a weight.
