@@ -463,8 +463,14 @@ w4a8_status w4a8_kv_read(const void *cache, int num_pages, int page_size, int kv
  *              O and lse may not overlap Q or the cache.
  *   lse        out [rows][q_heads] FP32, natural logarithm of the softmax's denominator
  *              (-inf for a row that sees no key), or NULL.
- * Precision: scores, maxima and sums in binary32; the weights p enter the value product in
- * binary16.  The result does not depend on how the work was scheduled.
+ * Precision: scores, maxima and sums in binary32 (a score beyond its range makes the row undefined).
+ * The weights p, each times the step of its value, enter the value product in binary16: to 11
+ * significant bits, or to 2^-29 of the row's largest where that is more.  2^17 tokens that all lie
+ * below that take 2^-12 of the largest off the output, longer rows of such tokens more; the
+ * denominator (and lse) counts them.  It leaves out tokens whose p * step is below 2^-126 of the
+ * largest: with steps that differ by less than 2^96, as all of binary16's values' do, less than 2^-30
+ * of the sum each.
+ * The result does not depend on how the work was scheduled.
  *   workspace >= w4a8_kv_attention_workspace_bytes(rows, batch, q_heads, kv_heads, D).  (Fewer rows of
  *              as many sequences need no more; as many rows of fewer sequences may: calls that share a
  *              workspace take the largest of their sizes.) */
