@@ -159,8 +159,8 @@ add_norm_quant_kernel(const TX *__restrict__ X, const TR *residual, TR *residual
         for (int i = 0; i < EV; ++i) {
             const int v = tid + i * T;
             if (v < nvec) {
-                wa[i] = __ldg(reinterpret_cast<const float4 *>(weight) + 2 * v);
-                wb[i] = __ldg(reinterpret_cast<const float4 *>(weight) + 2 * v + 1);
+                wa[i] = __ldca(reinterpret_cast<const float4 *>(weight) + 2 * v);
+                wb[i] = __ldca(reinterpret_cast<const float4 *>(weight) + 2 * v + 1);
             }
         }
     }
@@ -229,15 +229,15 @@ add_norm_quant_kernel(const TX *__restrict__ X, const TR *residual, TR *residual
             const int v = tid + i * T;
             if (v < nvec) {
                 if (EV != 2) {
-                    wa[i] = __ldg(reinterpret_cast<const float4 *>(weight) + 2 * v);
-                    wb[i] = __ldg(reinterpret_cast<const float4 *>(weight) + 2 * v + 1);
+                    wa[i] = __ldca(reinterpret_cast<const float4 *>(weight) + 2 * v);
+                    wb[i] = __ldca(reinterpret_cast<const float4 *>(weight) + 2 * v + 1);
                 }
                 const float w[8] = {wa[i].x, wa[i].y, wa[i].z, wa[i].w, wb[i].x, wb[i].y, wb[i].z, wb[i].w};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[i][e] = __fmul_rn(__fmul_rn(x[i][e], r), w[e]);
                 if (bias) {
-                    const float4 ba = __ldg(reinterpret_cast<const float4 *>(bias) + 2 * v);
-                    const float4 bb = __ldg(reinterpret_cast<const float4 *>(bias) + 2 * v + 1);
+                    const float4 ba = __ldca(reinterpret_cast<const float4 *>(bias) + 2 * v);
+                    const float4 bb = __ldca(reinterpret_cast<const float4 *>(bias) + 2 * v + 1);
                     const float b[8] = {ba.x, ba.y, ba.z, ba.w, bb.x, bb.y, bb.z, bb.w};
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[i][e] = __fadd_rn(x[i][e], b[e]);

@@ -216,7 +216,10 @@ __device__ inline float add_bias(float t, const float *bias, int n)
 // start while the kernel before it in the stream is still draining: launch latency, CTA
 // scheduling and each kernel's set-up then overlap the predecessor's tail.  The rule every
 // such kernel keeps: before dependent_wait() it touches no global memory except prefetch
-// hints; dependent_wait() returns once all earlier work in the stream is complete and visible.
+// hints; dependent_wait() returns once all earlier work in the stream is complete and visible.  What
+// earlier work may have written is read by coherent loads (__ldca, __ldcs, __ldcg or asynchronous
+// copies): the read-only path (__ldg) is defined only for memory that nobody writes during the
+// kernel's whole life, which begins before that wait.
 // Kernels launched the ordinary way (packing, the reference kernel) order as always.
 __device__ __forceinline__ void allow_dependents()
 {

@@ -235,7 +235,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         int requested = 0;                 // units of this item whose copies were started
         auto look_up = [&](int k) {
             const int blk = max(min(2 * (k0 + warp + (k + (lane >> 1)) * WARPS) + (lane & 1), last_block), lo_min >> 4);
-            int page = __ldg(table + (blk >> page_bits));
+            int page = __ldca(table + (blk >> page_bits));
             if ((unsigned)page >= (unsigned)a.cache.num_pages) {
                 report_failure(sc.sb, W4A8_ERR_BAD_TABLE, b);
                 page = 0;
@@ -262,7 +262,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
             const int i = sc.group.div(tile * R + r), head = h * group + tile * R + r - i * group;
             q_raw[n] = make_uint4(0u, 0u, 0u, 0u);
             if (r < rows_here)
-                q_raw[n] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + (size_t)(s.row0 + i) * a.q_stride +
+                q_raw[n] = __ldca(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + (size_t)(s.row0 + i) * a.q_stride +
                                                                  (size_t)head * D) + lane % LPV);
         }
         {

@@ -156,9 +156,9 @@ __device__ __forceinline__ Seq load_seq(const KvAttnArgs &a, int b, StatusBlock 
 {
     const KvBatch &bt = a.batch;
     Seq s;
-    s.len = __ldg(bt.kv_lens + b);
-    s.row0 = bt.cu_rows ? __ldg(bt.cu_rows + b) : b;
-    const int row1 = bt.cu_rows ? __ldg(bt.cu_rows + b + 1) : b + 1;
+    s.len = __ldca(bt.kv_lens + b);
+    s.row0 = bt.cu_rows ? __ldca(bt.cu_rows + b) : b;
+    const int row1 = bt.cu_rows ? __ldca(bt.cu_rows + b + 1) : b + 1;
     s.n = row1 - s.row0;
     const int most = bt.max_pages << a.cache.page_shift;
     if (s.len < 0 || s.len > most || s.row0 < 0 || row1 > bt.rows || row1 < s.row0) {

@@ -56,7 +56,7 @@ __device__ RowPlace place_of(const KvCache &c, const KvBatch &bt, int row, Statu
         int lo = 0, hi = bt.batch;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (__ldg(bt.cu_rows + mid) <= row) lo = mid;
+            if (__ldca(bt.cu_rows + mid) <= row) lo = mid;
             else hi = mid - 1;
         }
         b = lo;
@@ -182,8 +182,8 @@ kv_read_kernel(KvCache c, KvBatch bt, T *__restrict__ K, T *__restrict__ V, int 
             for (int j = 0; j < kUnroll; ++j) {
                 codes[j] = word[j] = 0u;     // an absent vector: step 0
                 if (p.at >= 0 && h + j < h1) {
-                    codes[j] = __ldg(reinterpret_cast<const uint32_t *>(from + j * head_bytes + code_at));
-                    word[j] = __ldg(reinterpret_cast<const uint32_t *>(from + j * head_bytes + word_at));
+                    codes[j] = __ldca(reinterpret_cast<const uint32_t *>(from + j * head_bytes + code_at));
+                    word[j] = __ldca(reinterpret_cast<const uint32_t *>(from + j * head_bytes + word_at));
                 }
             }
 #pragma unroll

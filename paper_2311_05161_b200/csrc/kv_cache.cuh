@@ -45,9 +45,9 @@ struct KvCache {
 // Position of row `row` of sequence b; `ok` false when the length or the offsets make no sense.
 __device__ __forceinline__ int kv_position_of(const KvBatch &bt, int b, int row, bool &ok)
 {
-    const int len = __ldg(bt.kv_lens + b);
-    const int begin = bt.cu_rows ? __ldg(bt.cu_rows + b) : b;
-    const int end = bt.cu_rows ? __ldg(bt.cu_rows + b + 1) : b + 1;
+    const int len = __ldca(bt.kv_lens + b);
+    const int begin = bt.cu_rows ? __ldca(bt.cu_rows + b) : b;
+    const int end = bt.cu_rows ? __ldca(bt.cu_rows + b + 1) : b + 1;
     ok = len >= 0 && begin >= 0 && begin <= row && end > row && end <= bt.rows;
     return ok ? len - (end - row) : -1;
 }
@@ -57,7 +57,7 @@ __device__ __forceinline__ int kv_page_of(const KvCache &c, const KvBatch &bt, i
 {
     const int i = pos >> c.page_shift;
     if (i >= bt.max_pages) return -1;
-    const int p = __ldg(bt.page_table + (size_t)b * bt.max_pages + i);
+    const int p = __ldca(bt.page_table + (size_t)b * bt.max_pages + i);
     return (unsigned)p < (unsigned)c.num_pages ? p : -1;
 }
 

@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     const int q_head = pc.h * (int)sc.group.d + q_flat - q_i * (int)sc.group.d;
                     raw[k] = make_uint4(0u, 0u, 0u, 0u);
                     if (at < pc.rows)
-                        raw[k] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + (size_t)(s.row0 + q_i) * a.q_stride +
+                        raw[k] = __ldca(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.Q) + (size_t)(s.row0 + q_i) * a.q_stride +
                                                                        (size_t)q_head * D) + c);
                 }
 #pragma unroll
@@ -707,7 +707,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             auto block_no = [&](int u) { return max(min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block), first_block); };
             auto page_of = [&](int u) {
                 const int blk = block_no(u);
-                int page = __ldg(table + (blk >> page_bits));
+                int page = __ldca(table + (blk >> page_bits));
                 if ((unsigned)page >= (unsigned)a.cache.num_pages) {
                     report_failure(sc.sb, W4A8_ERR_BAD_TABLE, seq);
                     page = 0;
@@ -724,24 +724,24 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             auto fetch_keys = [&](const uint8_t *p) {
                 const uint8_t *q = p + t * (D / 2) + quarter * (D / 8);
                 if constexpr (KW == 4) {
-                    const uint4 x = __ldg(reinterpret_cast<const uint4 *>(q));
+                    const uint4 x = __ldca(reinterpret_cast<const uint4 *>(q));
                     kc[0] = x.x; kc[1] = x.y; kc[2] = x.z; kc[3] = x.w;
                 } else {
-                    const uint2 x = __ldg(reinterpret_cast<const uint2 *>(q));
+                    const uint2 x = __ldca(reinterpret_cast<const uint2 *>(q));
                     kc[0] = x.x; kc[1] = x.y;
                 }
-                kw = __ldg(reinterpret_cast<const uint32_t *>(p + 16 * D + 4 * t));
-                vw = __ldg(reinterpret_cast<const uint32_t *>(p + 16 * D + 64 + 4 * t));
+                kw = __ldca(reinterpret_cast<const uint32_t *>(p + 16 * D + 4 * t));
+                vw = __ldca(reinterpret_cast<const uint32_t *>(p + 16 * D + 64 + 4 * t));
             };
             auto fetch_values = [&](const uint8_t *p) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const uint8_t *q = p + 8 * D + (((t >> 3) * 8 + quarter * 2 + k) * 8 + (t & 7)) * CB;
                     if constexpr (CB == 8) {
-                        const uint2 x = __ldg(reinterpret_cast<const uint2 *>(q));
+                        const uint2 x = __ldca(reinterpret_cast<const uint2 *>(q));
                         vc[k][0] = x.x;
                         vc[k][1] = x.y;
-                    } else vc[k][0] = __ldg(reinterpret_cast<const uint32_t *>(q));
+                    } else vc[k][0] = __ldca(reinterpret_cast<const uint32_t *>(q));
                 }
             };
             const uint8_t *block = block_of(0, page_of(0));
