@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 
 import torch
 
@@ -147,19 +148,43 @@ def _load() -> ctypes.CDLL:
 
 lib = _load()
 
-from . import _calls  # noqa: E402  (links to the library that was loaded above)
 
-_calls.set_errors(W4A8Error, torch.OutOfMemoryError)
+class _Absent:
+    """Stands for the extension module where it cannot be loaded: the calls that need it raise, the others work."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError("%s needs the extension module _calls (built by __graft_entry__.build()): %s" % (name, self._why))
+
+
+def _load_calls():
+    try:
+        from . import _calls  # links to the library that was loaded above
+    except ImportError as e:
+        return _Absent(e)
+    here = "torch %s, %s" % (torch.__version__, sys.implementation.cache_tag)
+    if _calls.built_for != here:
+        return _Absent("built for %s, this is %s" % (_calls.built_for, here))
+    _calls.set_errors(W4A8Error, torch.OutOfMemoryError)
+    return _calls
+
+
+_calls = _load_calls()
 
 
 def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream      # current_stream().cuda_stream at a thirtieth of its cost
+# current_stream().cuda_stream at a thirtieth of its cost; torch does not promise the name
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _stream():
+    if _raw_stream is None:
+        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
     return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
 
 

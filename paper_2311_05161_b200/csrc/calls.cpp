@@ -335,4 +335,9 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__calls() { return PyModule_Create(&module_def); }
+PyMODINIT_FUNC PyInit__calls()
+{
+    PyObject *m = PyModule_Create(&module_def);
+    if (m && PyModule_AddStringConstant(m, "built_for", W4A8_BUILT_FOR) != 0) Py_CLEAR(m);
+    return m;
+}
