@@ -63,7 +63,7 @@ act_quant_kernel(const __half *__restrict__ X, const float *__restrict__ inv_s, 
     } else {
         for (int idx = tid; idx < nvec; idx += kActThreads) {
             float x[8];
-            scaled8(__ldg(row + idx), inv_s, idx * 8, x);
+            scaled8(__ldca(row + idx), inv_s, idx * 8, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
         }
@@ -89,7 +89,7 @@ act_quant_kernel(const __half *__restrict__ X, const float *__restrict__ inv_s, 
     } else {
         for (int idx = tid; idx < nvec; idx += kActThreads) {
             float x[8];
-            scaled8(__ldg(row + idx), inv_s, idx * 8, x);
+            scaled8(__ldca(row + idx), inv_s, idx * 8, x);
             out[idx] = quantize8(x, r);
         }
     }
@@ -379,7 +379,7 @@ act_quant_asym_kernel(const __half *__restrict__ X, const float *__restrict__ in
     } else {
         for (int idx = tid; idx < nvec; idx += kActThreads) {
             float x[8];
-            scaled8(__ldg(row + idx), inv_s, idx * 8, x);
+            scaled8(__ldca(row + idx), inv_s, idx * 8, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) { lo = fminf(lo, x[e]); hi = fmaxf(hi, x[e]); }
         }
@@ -409,7 +409,7 @@ act_quant_asym_kernel(const __half *__restrict__ X, const float *__restrict__ in
     } else {
         for (int idx = tid; idx < nvec; idx += kActThreads) {
             float x[8];
-            scaled8(__ldg(row + idx), inv_s, idx * 8, x);
+            scaled8(__ldca(row + idx), inv_s, idx * 8, x);
             out[idx] = quantize8_asym(x, r, shift);
         }
     }

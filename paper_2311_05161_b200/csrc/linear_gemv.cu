@@ -115,7 +115,7 @@ __device__ __forceinline__ void cta_token_absmax(const __half *X, const float *i
         for (int m = 0; m < MT; ++m)
             if (m < M) {
                 float x[8];
-                scaled8(__ldg(reinterpret_cast<const uint4 *>(X + (size_t)m * K) + c), inv_s, c * 8, x);
+                scaled8(__ldca(reinterpret_cast<const uint4 *>(X + (size_t)m * K) + c), inv_s, c * 8, x);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) amax[m] = fmaxf(amax[m], fabsf(x[e]));
             }
@@ -141,7 +141,7 @@ __device__ __forceinline__ uint2 quantize_vec8(const __half *X, const float *inv
                                                int c, float r)
 {
     float x[8];
-    scaled8(__ldg(reinterpret_cast<const uint4 *>(X + (size_t)m * K) + c), inv_s, c * 8, x);
+    scaled8(__ldca(reinterpret_cast<const uint4 *>(X + (size_t)m * K) + c), inv_s, c * 8, x);
     return quantize8(x, r);
 }
 
@@ -236,7 +236,7 @@ linear_gemv_kernel(const GemvParams P)
             const int m = i / kRowChunks, c = i % kRowChunks;
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
             if (m < P.M && c < kb_count * (kTileK / 16))
-                v = __ldg(reinterpret_cast<const uint4 *>(P.Xq + (size_t)m * P.L.K + kb_first * kTileK) + c);
+                v = __ldca(reinterpret_cast<const uint4 *>(P.Xq + (size_t)m * P.L.K + kb_first * kTileK) + c);
             reinterpret_cast<uint4 *>(&s_x[m][0])[c] = v;
         }
     }
@@ -467,7 +467,7 @@ linear_gemv_rows_kernel(const GemvParams P)
         for (int i = threadIdx.x; i < MT * chunks; i += 32 * W) {
             const int m = i / chunks, c = i - m * chunks;
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (m < P.M) v = __ldg(reinterpret_cast<const uint4 *>(P.Xq + (size_t)m * P.L.K) + c);
+            if (m < P.M) v = __ldca(reinterpret_cast<const uint4 *>(P.Xq + (size_t)m * P.L.K) + c);
             reinterpret_cast<uint4 *>(s_x + (size_t)m * P.L.K)[c] = v;
         }
     }

@@ -606,7 +606,7 @@ token_offsum_kernel(const int8_t *__restrict__ Xq, int K, int offset, int32_t *_
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int i = i0 + j * 256;
-            v[j] = i < n16 ? __ldg(row + i) : make_int4(0, 0, 0, 0);
+            v[j] = i < n16 ? __ldca(row + i) : make_int4(0, 0, 0, 0);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -1157,8 +1157,8 @@ linear_tcgen05_kernel(const __grid_constant__ CUtensorMap tok_map,
                 named_bar_sync(1, kEpiThreads);
                 for (int i = et; i < TOK; i += kEpiThreads) {
                     const bool in = tt * TOK + i < P.M;
-                    s_tok[i] = (in && P.tok_scale) ? __ldg(P.tok_scale + nt * P.batch_rows + tt * TOK + i) : 0.0f;
-                    s_tz[i] = (in && P.zp.tok_zero) ? __ldg(P.zp.tok_zero + tt * TOK + i) : 0;
+                    s_tok[i] = (in && P.tok_scale) ? __ldca(P.tok_scale + nt * P.batch_rows + tt * TOK + i) : 0.0f;
+                    s_tz[i] = (in && P.zp.tok_zero) ? __ldca(P.zp.tok_zero + tt * TOK + i) : 0;
                     s_off[i] = (in && P.offset) ? __ldcg(P.tok_offsum + nt * P.batch_rows + tt * TOK + i) : 0;
                 }
                 named_bar_sync(1, kEpiThreads);
