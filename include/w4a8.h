@@ -414,6 +414,7 @@ w4a8_status w4a8_attn_pv(const int8_t *Pq, const float *p_scale, const void *pac
  *   page_table  [batch][max_pages] INT32: page of tokens i * page_size .. of each sequence.  Entries
  *               of pages without a token that the call writes, reads or that a row sees (behind a
  *               sequence's end, in front of its oldest row's window) are not read.
+ *               max_pages * page_size <= 2^31 - 1024.
  *   kv_lens     [batch] INT32, tokens of each sequence INCLUDING this call's rows.
  *   cu_rows     [batch + 1] INT32, ascending from 0: rows cu_rows[b] .. cu_rows[b+1] - 1 of the call
  *               belong to sequence b and are its last positions, kv_lens[b] - n_b + i.  NULL: one

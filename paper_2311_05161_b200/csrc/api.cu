@@ -149,8 +149,8 @@ w4a8_status kv_common(const void *cache, int num_pages, int page_size, int heads
     if (!cache || !page_table || !kv_lens || !workspace) return W4A8_ERR_NULL;
     if (!kv_shape_ok(page_size, heads, D) || num_pages < 1 || max_pages < 1 || batch < 1 || rows < 1)
         return W4A8_ERR_SHAPE;
-    // positions are 32-bit; one launch's rows x heads stay within a grid
-    if ((long long)max_pages * page_size >= (1ll << 31) || (long long)rows * heads >= (1ll << 31))
+    // positions, and the group of up to 64 tokens behind the last, are 32-bit; one launch's rows x heads stay within a grid
+    if ((long long)max_pages * page_size > (1ll << 31) - 1024 || (long long)rows * heads >= (1ll << 31))
         return W4A8_ERR_SHAPE;
     if (!cu_rows && rows != batch) return W4A8_ERR_SHAPE;
     if (!aligned(cache, 16) || !aligned(page_table, 4) || !aligned(kv_lens, 4) || !aligned(cu_rows, 4) ||
