@@ -74,13 +74,6 @@ __device__ __forceinline__ float min3(float a, float b, float c)
     return d;
 }
 
-// Address of the block that holds token slot `slot` of head h of a page.
-__device__ __forceinline__ uint8_t *kv_block_at(const KvCache &c, int page, int h, int slot)
-{
-    return c.pages + (size_t)page * c.page_bytes() +
-           ((size_t)h << c.page_shift) * (c.D + 8) + (size_t)(slot >> 4) * kv_block_bytes(c.D);
-}
-
 // Byte offset, inside a block, of the word with the codes of elements 8 w .. 8 w + 7 of token s.
 __device__ __forceinline__ int kv_code_offset(int D, int is_value, int s, int w)
 {
