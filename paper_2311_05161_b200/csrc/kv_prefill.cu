@@ -700,13 +700,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             if (count >= 0 && lane == 0) mbar_arrive(bar(L::kPieceEmpty + (piece_no & 1)));
             if (count < 0) break;
             if (count == 0) continue;
-            const int first_block = lo >> 4, last_block = (len - 1) >> 4;
+            const int last_block = (len - 1) >> 4;
             const int32_t *table = a.batch.page_table + (size_t)seq * a.batch.max_pages;
-            // block of this thread's token of unit u of the piece (behind the end, or in front of what the tile sees:
-            // the nearest that it sees; the page of the other may be gone)
-            auto block_no = [&](int u) { return max(min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block), first_block); };
-            auto page_of = [&](int u) {
-                const int blk = block_no(u);
+            // Block of this thread's token of unit u of the piece; behind the end the last one.  In front of what the tile
+            // sees, in the first unit only, the first one that it sees: the page of the other may be gone.
+            auto block_no = [&](int u) { return min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block); };
+            auto page_of = [&](int blk) {
                 int page = __ldca(table + (blk >> page_bits));
                 if ((unsigned)page >= (unsigned)a.cache.num_pages) {
                     report_failure(sc.sb, W4A8_ERR_BAD_TABLE, seq);
@@ -716,8 +715,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             };
             uint32_t kc[KW];
             uint32_t vc[2][CB / 4], kw = 0, vw = 0;
-            auto block_of = [&](int u, int page) {         // this thread's block of unit u
-                const int blk = block_no(u);
+            auto block_of = [&](int blk, int page) {
                 return head_base + (size_t)page * page_bytes + (size_t)(blk & in_page) * (16 * (D + 8));
             };
             const int t = tk & 15;
@@ -744,10 +742,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     } else vc[k][0] = __ldca(reinterpret_cast<const uint32_t *>(q));
                 }
             };
-            const uint8_t *block = block_of(0, page_of(0));
+            const int blk0 = max(block_no(0), lo >> 4);
+            const uint8_t *block = block_of(blk0, page_of(blk0));
             fetch_keys(block);
             fetch_values(block);
-            int page = count > 1 ? page_of(1) : 0;
+            int page = count > 1 ? page_of(block_no(1)) : 0;
+            const int from_lo = unit0 * kUnit + tk - lo;     // place of this thread's first token behind the first that the tile sees
+            const uint32_t seen = (uint32_t)(len - lo);
             if (!(ok = wait_warp(bar(L::kQmax), item_no & 1, ctl, sc.sb, kWaitSite + 4))) break;
             const volatile float *qmax = reinterpret_cast<const float *>(smem + L::kOffQmax) + (item_no & 1) * kSoftmaxWarps;
             float amax = 0.0f;
@@ -770,8 +771,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             };
             for (int u = 0; u < count; ++u, ++unit_no) {
                 const uint32_t buf = unit_no % kRing, use = unit_no / kRing & 1, slot = unit_no % kConstSlots;
-                const int at = (unit0 + u) * kUnit + tk;
-                const bool there = at >= lo && at < len;     // else its words are anything
+                const bool there = (uint32_t)(from_lo + u * kUnit) < seen;       // else its words are anything
                 // ---- keys ----
                 if (unit_no >= kRing && !(ok = wait_warp(bar(L::kKEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 5, 200))) break;
                 {
@@ -794,9 +794,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 }
                 const uint32_t value_word = vw;
                 if (u + 1 < count) {                       // the next unit's keys travel while the values are expanded
-                    block = block_of(u + 1, page);
+                    block = block_of(block_no(u + 1), page);
                     fetch_keys(block);
-                    if (u + 2 < count) page = page_of(u + 2);
+                    if (u + 2 < count) page = page_of(block_no(u + 2));
                 }
                 fence_async();
                 __syncwarp();
