@@ -4,10 +4,10 @@
 // codes and one word: 2 D + D/2 + 4 bytes, so the kernel is bound by memory for prompts and by
 // latency for decode steps.  A group of D/8 lanes owns a vector: a lane has eight elements in one
 // 16-byte load and writes one code word; the range is reduced over the group by shuffles.  The places
-// of a CTA's rows are found once, by a thread each.  Arithmetic is close to being the bound (some 80 instructions per
+// of a CTA's rows are found once, by a thread each.  Arithmetic is close to being the bound (182 instructions executed per
 // 8 elements of a lane), hence the group that keeps one row and advances by constants.  Four prompts (611 to 4097 tokens, 8
-// heads of 128, 54 MB): 24 us under the profiler, logic pipe 52 % and issue slots 71 % busy; 31.6 us with their read.
-// Read is the same walk the other way: 16 sequences (231 MB, 8 heads of 128) 45 us, 5.1 TB/s, issue slots
+// heads of 128, 54 MB): 24 us under the profiler, logic pipe 52 % and issue slots 71 % busy; 31.9 us with their read.
+// Read is the same walk the other way: 16 sequences (231 MB, 8 heads of 128) 46 us, 5.0 TB/s, issue slots
 // 69 % busy.  (A thread per eight elements that found its row by itself took 77 us there.)
 #include "kv_cache.cuh"
 

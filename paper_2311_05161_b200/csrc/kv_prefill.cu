@@ -24,10 +24,13 @@
 // Bounds per unit and SM for D = 128: 1024 cycles of MMA (a 128 x 64 x 128 and a 128 x 128 x 64 product per row
 // tile), 1024 cycles of exponentials at 16 per cycle, about 500 cycles of packed binary16 arithmetic to
 // expand 16384 codes: the expansion is shared by 256 rows, which is why the two tiles are one CTA's.
-// Measured: the last 1024 of 4096 tokens (8 key heads, 32 query heads of 128) 108 us, 558 TFLOP/s, tensor
-// pipe 28 %, issue slots 56 % busy; some 2300 cycles per unit, the softmax's chain of wait, load, maximum,
-// exponentials and store being the longest.  4 prompts of 2048: 286 us.  (Sixteen softmax warps, two threads per row, were
-// slower for their exchange of maxima: 120 us.)
+// Measured: the last 1024 of 4096 tokens (8 key heads, 32 query heads of 128) 109 us, 553 TFLOP/s, tensor
+// pipe 28 %, issue slots 56 % busy; 4 prompts of 2048: 285 us.  From runs of several lengths (items of 256 rows, one or
+// more per CTA): 1.47 us per unit (2890 cycles at 1965 MHz; D = 64: 1.34 us), 17 us for the launch and a CTA's first
+// piece, 10 to 13 us for each further piece.  A unit's time is the softmax's chain of wait, load, maximum, exponentials and
+// store.  A piece's is what does not overlap between pieces: queries, first keys, output or parts.  The chunk is 49 units
+// and 1.9 pieces per CTA, the prompts 114 units and 7.9 pieces: a quarter and two fifths of the time lie
+// outside the units.  (Sixteen softmax warps, two threads per row, were slower for their exchange of maxima: 120 us.)
 #include <type_traits>
 
 #include "kv_attention.cuh"
