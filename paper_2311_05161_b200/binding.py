@@ -165,8 +165,9 @@ def _load_calls():
     except ImportError as e:
         return _Absent(e)
     here = "torch %s, %s" % (torch.__version__, sys.implementation.cache_tag)
-    if _calls.built_for != here:
-        return _Absent("built for %s, this is %s" % (_calls.built_for, here))
+    built_for = getattr(_calls, "built_for", "something unknown")
+    if built_for != here:
+        return _Absent("built for %s, this is %s" % (built_for, here))
     _calls.set_errors(W4A8Error, torch.OutOfMemoryError)
     return _calls
 

@@ -10,12 +10,13 @@ import __graft_entry__ as entry
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
-# what stands in for the module: none, one built for another torch, the one that is there under a torch
+# what stands in for the module: none, one built for another torch, one that does not say for what, the one that is there under a torch
 # that lacks the private name of the raw stream
 STANDINS = {
     "absent": "sys.modules['paper_2311_05161_b200._calls'] = None",
     "stale": "m = types.ModuleType('x'); m.built_for = 'torch 1.0, cpython-30'; m.set_errors = None; "
              "sys.modules['paper_2311_05161_b200._calls'] = m",
+    "unmarked": "sys.modules['paper_2311_05161_b200._calls'] = types.ModuleType('x')",
     "no raw stream": "import torch; del torch._C._cuda_getCurrentRawStream",
 }
 PROGRAM = """
