@@ -47,8 +47,9 @@ typedef enum {
     W4A8_ERR_CUDA = 6,              /* a CUDA runtime or driver call failed */
     W4A8_ERR_TIMEOUT = 7,           /* a bounded wait inside a kernel ran out */
     W4A8_ERR_BAD_BLOB = 8,          /* `packed` does not hold a blob of this N, K, group */
-    W4A8_ERR_BAD_TABLE = 9          /* a page number, sequence length or row offset that a kernel
-                                       met lies outside the cache, the page table or the call */
+    W4A8_ERR_BAD_TABLE = 9,         /* a page number, sequence length, row offset, slot or path that a
+                                       kernel met lies outside the cache, the page table or the call */
+    W4A8_ERR_NO_PAGES = 10          /* w4a8_kv_plan: the free list holds fewer pages than the step needs */
 } w4a8_status;
 
 /* Which kernel w4a8_linear_ex runs.  AUTO picks by shape. */
@@ -484,6 +485,110 @@ w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, con
                               int causal, int window, void *O, int o_type, float *lse,
                               void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- a serving step around the cache: plan, rotary positions, sinks, drafted trees ----
+ * The batch arguments are those of the cache calls above.  None of these calls makes the host wait, so that a whole step can be
+ * captured once and replayed with other lengths.
+ *
+ * w4a8_kv_plan: what a step needs to know about its batch, from the requests' lengths on the device.
+ *   held        [batch] INT32, tokens that the sequence's pages were taken for (kv_lens_out of the plan
+ *               before), or NULL: kv_lens.  held >= kv_lens.
+ *   kv_lens     [batch] INT32, tokens that the sequence keeps (fewer than held when drafted tokens were not
+ *               accepted; 0 ends the sequence).
+ *   add         [batch] INT32 >= 0, rows that this step adds to it.
+ *   page_table  [batch][max_pages] INT32, in and out: with P = page_size, entries
+ *               ceil(held / P) .. ceil((kv_lens + add) / P) - 1 are taken from the free list; where there are fewer pages
+ *               than before, the surplus ones are given back (their entries stay as they are and count no longer).
+ *   free_pages  [num_pages] INT32, in and out: a stack, its first *free_count numbers are the free pages.
+ *               The pages given back lie on top of it in the order of sequences and pages, then pages are
+ *               taken from the top in that order.
+ *   free_count  [1] INT32;  free_count_out [1] INT32, may be free_count itself.
+ *   kv_lens_out [batch] INT32: kv_lens + add, what append and attention take as kv_lens.  May be `held` (or
+ *               kv_lens where held is NULL).
+ *   cu_rows     out [batch + 1] INT32, row offsets.
+ *   positions   out [rows] INT32, position of every row, or NULL.
+ *   slots       out [rows] INT64, page * page_size + place of every row, or NULL.
+ *   rows        size of positions and slots; rows from cu_rows[batch] on get position 0 and slot -1.
+ * A step whose rows do not fit, whose lengths are out of range or whose free list is damaged (W4A8_ERR_BAD_TABLE), or
+ * that needs more pages than are free (W4A8_ERR_NO_PAGES), is refused as a whole: cu_rows are 0, slots -1, kv_lens_out is held,
+ * free_count_out is free_count, the table and the list are left alone; the status block reports it.
+ * batch <= 16384.  workspace: 512 bytes, zero-filled once; one that the cache calls use will do. */
+w4a8_status w4a8_kv_plan(const int32_t *held, const int32_t *kv_lens, const int32_t *add, int batch,
+                         int32_t *page_table, int max_pages, int page_size, int32_t *free_pages,
+                         int num_pages, const int32_t *free_count, int32_t *free_count_out,
+                         int32_t *kv_lens_out, int32_t *cu_rows, int32_t *positions, int64_t *slots,
+                         int rows, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Rotary positions on the rows' queries and keys; the keys and values are quantized into their slots (as in
+ * w4a8_kv_append, the keys from the binary32 rotation without a rounding to 16 bits in between).
+ * Pair i of a vector's first `rotary_dim` elements is (x[i], x[i + rotary_dim / 2]), or (x[2i], x[2i + 1]) with
+ * `interleaved`; it is turned by the angle positions[pair_axis[i]][row] * inv_freq[i]:
+ *   a' = a cos - b sin,  b' = b cos + a sin      (binary32, one rounding per operation),
+ * sine and cosine rounded once to binary32 from binary64, also for far positions.  Other elements pass.
+ *   Q, K, V     [rows][heads][D] W4A8_F16 or W4A8_BF16 (dtype), row strides as above.
+ *   positions   [axes][rows] INT32: one axis for text; time, height and width for images and video.
+ *   axes        1 .. 16.
+ *   pair_axis   [rotary_dim / 2] INT32, axis of each pair, or NULL: axis 0.
+ *   inv_freq    [rotary_dim / 2] FP32.
+ *   rotary_dim  a multiple of 16, at most head_dim.
+ *   Q_out       [rows][q_heads][D], row stride q_out_stride: the turned queries, rounded once (values beyond the
+ *               type's range become the largest finite ones).  May be Q itself with its stride; any other overlap with an
+ *               input is not allowed.
+ *   slots       [rows] INT64 as written by w4a8_kv_plan; a row with a negative one is skipped (Q_out too).  One
+ *               that names no page of the cache is reported (W4A8_ERR_BAD_TABLE) and skipped, an axis outside
+ *               0 .. axes - 1 is reported and taken for axis 0.  No two rows may name the same slot.
+ *   workspace   its first 256 bytes, for the reports. */
+w4a8_status w4a8_rope_kv_append(const void *Q, const void *K, const void *V, int dtype, long long q_stride,
+                                long long k_stride, long long v_stride, const int32_t *positions, int axes,
+                                const int32_t *pair_axis, const float *inv_freq, int rotary_dim,
+                                int interleaved, void *Q_out, long long q_out_stride, void *cache,
+                                int num_pages, int page_size, int kv_heads, int head_dim,
+                                const int64_t *slots, int rows, int q_heads, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/* w4a8_kv_attention with a window and first tokens that stay visible: a row at position p sees the keys j (j <= p if
+ * causal) with j > p - window or j < sinks.  window 0: no limit.  Pages without a token that a row sees, those between
+ * the sinks and the oldest row's window among them, are not read, and their table entries neither. */
+w4a8_status w4a8_kv_attention_sinks(const void *Q, int q_type, long long q_stride, const void *cache,
+                                    int num_pages, int page_size, int kv_heads, int head_dim,
+                                    const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                                    const int32_t *cu_rows, int batch, int rows, int q_heads, float scale,
+                                    int causal, int window, int sinks, void *O, int o_type, float *lse,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+
+/* Attention of drafted rows: the rows of a sequence are the nodes of a tree (or several) behind its tokens.  Row i of
+ * sequence b, whose rows begin at position base = kv_lens[b] - n_b, sees
+ *   - the tokens in front of base, all of them or, with a window, those j with j > p - window or j < sinks, where
+ *     p = base + (bits of its mask) - 1 (its mask names its ancestors and itself);
+ *   - the drafted rows j (at position base + j) of its mask: bit j % 32 of tree_mask[row][j / 32].
+ * Bits of rows that the sequence does not have are ignored; any mask is allowed, an empty one too.
+ *   tree_mask   [rows][mask_words] UINT32; a sequence may have up to 32 * mask_words rows (more are reported as
+ *               W4A8_ERR_BAD_TABLE, and the rows behind are seen by none).
+ * All else as in w4a8_kv_attention.  The drafted rows' keys and values are in the cache, at their places in the
+ * order of rows (rotary positions are the tree's, p above as a rule); their pages are read whether a mask names
+ * them or not. */
+w4a8_status w4a8_kv_attention_tree(const void *Q, int q_type, long long q_stride, const void *cache,
+                                   int num_pages, int page_size, int kv_heads, int head_dim,
+                                   const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                                   const int32_t *cu_rows, int batch, int rows, int q_heads, float scale,
+                                   const uint32_t *tree_mask, int mask_words, int window, int sinks, void *O,
+                                   int o_type, float *lse, void *workspace, size_t workspace_bytes,
+                                   void *stream);
+
+/* The accepted path of each tree moves to the front of the drafted rows: slot base + i takes the keys and values of
+ * slot base + accepted[b][i] for i < accept_lens[b] (base = kv_lens[b] - n_b; codes are copied as they are).  Call
+ * it once per layer's cache, then plan the next step with kv_lens_out (and held = the lengths of this one).
+ *   accepted    [batch][max_accept] INT32, places among the sequence's rows, ascending.
+ *   accept_lens [batch] INT32, at most max_accept and the sequence's rows.
+ *   kv_lens_out out [batch] INT32: base + accept_lens[b], or NULL.  Not kv_lens itself.
+ * A sequence with lengths or offsets out of range, or with more accepted rows than it has, keeps its slots
+ * as they are; a place that does not ascend or names no row is left out; both are reported (W4A8_ERR_BAD_TABLE).
+ *   workspace   its first 256 bytes, for the reports. */
+w4a8_status w4a8_kv_accept(void *cache, int num_pages, int page_size, int kv_heads, int head_dim,
+                           const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                           const int32_t *cu_rows, int batch, int rows, const int32_t *accepted, int max_accept,
+                           const int32_t *accept_lens, int32_t *kv_lens_out, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
 /* w4a8_linear_asym for any group_size: with group_size 128 the token's zero-point leaves every
  * group's integer sum before that sum is scaled,
  *   acc_g[m][n] = sum_{k in g} Xq[m][k] * t2(code[n][k]) - tok_zero[m] * rowsum[g][n],
@@ -514,8 +619,8 @@ w4a8_status w4a8_unpack_codes_bits(const void *packed, int N, int K, int group_s
                                    uint8_t *codes, float *scales, uint8_t *zeros, void *stream);
 
 /* Synchronizes `stream`, then reads and clears the status block of `workspace`:
- * W4A8_OK, W4A8_ERR_TIMEOUT, W4A8_ERR_BAD_BLOB or W4A8_ERR_BAD_TABLE (first failure since the
- * last poll).
+ * W4A8_OK, W4A8_ERR_TIMEOUT, W4A8_ERR_BAD_BLOB, W4A8_ERR_BAD_TABLE or W4A8_ERR_NO_PAGES (first
+ * failure since the last poll).
  * A kernel that gave up (W4A8_ERR_TIMEOUT) may leave split-K tile counters behind in the
  * workspace: run w4a8_workspace_init on it before the next call, else a later split-K call can
  * reduce partial tiles too early.  The output of a call that reported a failure is undefined. */

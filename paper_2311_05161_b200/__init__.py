@@ -16,4 +16,5 @@ from .binding import (  # noqa: F401
     interleave_gate_up, linear_swiglu, new_linear_swiglu_workspace, linear_asym_group,
     add_norm_quantize_act, new_kv_cache, kv_page_bytes, new_kv_workspace, kv_attention_workspace_bytes,
     kv_append, kv_read, kv_attention,
+    kv_plan, rope_kv_append, kv_attention_sinks, kv_attention_tree, kv_accept,
 )

@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libw4a8.so")
 STATUS_NAMES = {
     0: "W4A8_OK", 1: "W4A8_ERR_NULL", 2: "W4A8_ERR_SHAPE", 3: "W4A8_ERR_ALIGN",
     4: "W4A8_ERR_BUFFER_TOO_SMALL", 5: "W4A8_ERR_UNSUPPORTED_ARCH", 6: "W4A8_ERR_CUDA",
-    7: "W4A8_ERR_TIMEOUT", 8: "W4A8_ERR_BAD_BLOB", 9: "W4A8_ERR_BAD_TABLE",
+    7: "W4A8_ERR_TIMEOUT", 8: "W4A8_ERR_BAD_BLOB", 9: "W4A8_ERR_BAD_TABLE", 10: "W4A8_ERR_NO_PAGES",
 }
 PATH_AUTO, PATH_SIMPLE, PATH_TCGEN05, PATH_GEMV = 0, 1, 2, 3
 
@@ -38,6 +38,7 @@ EXPORTS = (
     "w4a8_linear_swiglu", "w4a8_linear_swiglu_workspace_bytes", "w4a8_linear_asym_group",
     "w4a8_add_norm_quantize_act", "w4a8_kv_page_bytes", "w4a8_kv_append", "w4a8_kv_read",
     "w4a8_kv_attention", "w4a8_kv_attention_workspace_bytes",
+    "w4a8_kv_plan", "w4a8_rope_kv_append", "w4a8_kv_attention_sinks", "w4a8_kv_attention_tree", "w4a8_kv_accept",
 )
 
 
@@ -133,6 +134,19 @@ def _load() -> ctypes.CDLL:
     lib.w4a8_kv_attention.restype = ci
     lib.w4a8_kv_attention.argtypes = [vp, ci, ll, vp, ci, ci, ci, ci, vp, ci, vp, vp, ci, ci, ci, cf, ci, ci,
                                       vp, ci, vp, vp, sz, vp]
+    lib.w4a8_kv_attention_sinks.restype = ci
+    lib.w4a8_kv_attention_sinks.argtypes = [vp, ci, ll, vp, ci, ci, ci, ci, vp, ci, vp, vp, ci, ci, ci, cf, ci, ci, ci,
+                                            vp, ci, vp, vp, sz, vp]
+    lib.w4a8_kv_attention_tree.restype = ci
+    lib.w4a8_kv_attention_tree.argtypes = [vp, ci, ll, vp, ci, ci, ci, ci, vp, ci, vp, vp, ci, ci, ci, cf, vp, ci, ci, ci,
+                                           vp, ci, vp, vp, sz, vp]
+    lib.w4a8_kv_plan.restype = ci
+    lib.w4a8_kv_plan.argtypes = [vp, vp, vp, ci, vp, ci, ci, vp, ci, vp, vp, vp, vp, vp, vp, ci, vp, sz, vp]
+    lib.w4a8_rope_kv_append.restype = ci
+    lib.w4a8_rope_kv_append.argtypes = [vp, vp, vp, ci, ll, ll, ll, vp, ci, vp, vp, ci, ci, vp, ll, vp, ci, ci, ci, ci,
+                                        vp, ci, ci, vp, sz, vp]
+    lib.w4a8_kv_accept.restype = ci
+    lib.w4a8_kv_accept.argtypes = [vp, ci, ci, ci, ci, vp, ci, vp, vp, ci, ci, vp, ci, vp, vp, vp, sz, vp]
     lib.w4a8_linear_acc_i32.restype = ci
     lib.w4a8_linear_acc_i32.argtypes = [vp, vp, ci, ci, ci, ci, vp, vp, sz, vp, op]
     lib.w4a8_unpack_codes.restype = ci
@@ -554,6 +568,43 @@ def kv_attention(Q, cache, page_table, kv_lens, kv_heads: int, workspace, cu_row
     O [rows, q_heads, D] of `dtype`.  scale: 1 / sqrt(D) by default; lse: a [rows, q_heads] float32
     tensor that receives the logarithms of the softmax denominators."""
     return _calls.kv_attention(Q, cache, page_table, kv_lens, kv_heads, workspace, cu_rows, scale, causal, window, dtype, out, lse)
+
+
+def kv_plan(held, kv_lens, add, page_table, free_pages, free_count, page_size: int, rows: int, workspace, out=None):
+    """A step's plan on the device (int32 tensors).  Sequences keep kv_lens tokens of the `held` ones that their pages were
+    taken for (None: kv_lens) and get `add` rows; page_table [batch, max_pages] and free_pages [num_pages], a stack of
+    free_count [1] pages, are updated in place.  Returns (kv_lens_out [batch], cu_rows [batch + 1], positions [rows],
+    slots [rows] int64, free_count_out [1]); `out` gives any of these tensors (None: allocated).  A plan that does not fit
+    changes nothing, has no rows and is reported by check_status(workspace)."""
+    lens, cu, positions, slots, count = (None,) * 5 if out is None else out
+    return _calls.kv_plan(held, kv_lens, add, page_table, free_pages, free_count, page_size, rows, workspace, lens, cu, positions, slots, count)
+
+
+def rope_kv_append(Q, K, V, positions, inv_freq, cache, slots, workspace, pair_axis=None, interleaved: bool = False, out=None):
+    """Rotary positions on Q [rows, q_heads, D] and K [rows, kv_heads, D], K and V quantized into their slots of the cache: returns
+    the turned queries (in place with `out=Q`).  positions [rows] or [axes, rows] int32, inv_freq [rotary_dim / 2] float32,
+    pair_axis [rotary_dim / 2] int32 (which axis turns a pair), slots [rows] int64 (kv_plan; negative: skipped).
+    Pairs are elements i and i + rotary_dim / 2, or 2 i and 2 i + 1 with `interleaved`."""
+    return _calls.rope_kv_append(Q, K, V, positions, inv_freq, cache, slots, workspace, pair_axis, interleaved, out)
+
+
+def kv_attention_sinks(Q, cache, page_table, kv_lens, kv_heads: int, workspace, window: int, sinks: int, cu_rows=None, scale=None,
+                       causal: bool = True, dtype=torch.float16, out=None, lse=None):
+    """kv_attention with a window of `window` tokens (0: no limit) and the first `sinks` tokens visible beside it."""
+    return _calls.kv_attention_sinks(Q, cache, page_table, kv_lens, kv_heads, workspace, window, sinks, cu_rows, scale, causal, dtype, out, lse)
+
+
+def kv_attention_tree(Q, cache, page_table, kv_lens, kv_heads: int, workspace, tree_mask, cu_rows=None, scale=None, window: int = 0,
+                      sinks: int = 0, dtype=torch.float16, out=None, lse=None):
+    """Attention of drafted rows: a row sees the tokens in front of its sequence's rows (with a window and sinks, if given) and
+    those of the sequence's rows whose bits are set in its mask, tree_mask [rows, words] int32 (bit j % 32 of word j / 32)."""
+    return _calls.kv_attention_tree(Q, cache, page_table, kv_lens, kv_heads, workspace, tree_mask, cu_rows, scale, window, sinks, dtype, out, lse)
+
+
+def kv_accept(cache, page_table, kv_lens, accepted, accept_lens, kv_heads: int, head_dim: int, workspace, cu_rows=None, out=None):
+    """Moves the accepted drafted rows, places accepted [batch, max_accept] int32 among the sequence's rows in ascending order, to
+    the front of the sequence's drafted slots, accept_lens [batch] int32 of them.  Returns the sequences' new lengths."""
+    return _calls.kv_accept(cache, page_table, kv_lens, accepted, accept_lens, kv_heads, head_dim, workspace, cu_rows, out)
 
 
 def linear_static(Xq, tok_scale, packed, bias, N: int, group: int, out):

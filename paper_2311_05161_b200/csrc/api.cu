@@ -1,4 +1,6 @@
 // extern "C" entry points: argument validation and dispatch.  See include/w4a8.h.
+#include <initializer_list>
+
 #include "common.cuh"
 #include "kv_cache.cuh"
 
@@ -563,12 +565,16 @@ size_t w4a8_kv_attention_workspace_bytes(int rows, int batch, int q_heads, int k
     return kv_attention_workspace(rows, batch, q_heads, kv_heads, head_dim);
 }
 
-w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, const void *cache,
-                              int num_pages, int page_size, int kv_heads, int head_dim,
-                              const int32_t *page_table, int max_pages, const int32_t *kv_lens,
-                              const int32_t *cu_rows, int batch, int rows, int q_heads, float scale,
-                              int causal, int window, void *O, int o_type, float *lse,
-                              void *workspace, size_t workspace_bytes, void *stream)
+}  // extern "C"
+
+// What the three attention calls check alike.
+static w4a8_status kv_attention_common(const void *Q, int q_type, long long q_stride, const void *cache,
+                                       int num_pages, int page_size, int kv_heads, int head_dim,
+                                       const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                                       const int32_t *cu_rows, int batch, int rows, int q_heads, float scale,
+                                       int causal, int window, int sinks, const uint32_t *tree, int tree_words,
+                                       void *O, int o_type, float *lse, void *workspace, size_t workspace_bytes,
+                                       void *stream)
 {
     if (!Q || !O) return W4A8_ERR_NULL;
     KvAttnArgs a;
@@ -579,8 +585,8 @@ w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, con
     if (!kv_attention_shape_ok(rows, batch, q_heads, kv_heads, head_dim)) return W4A8_ERR_SHAPE;
     if (!is_16bit(q_type) || !is_16bit(o_type) || q_stride < (long long)q_heads * head_dim || q_stride % 8 != 0)
         return W4A8_ERR_SHAPE;
-    if (!(scale > 0.0f) || scale > 3.0e38f || window < 0) return W4A8_ERR_SHAPE;
-    if (!aligned(Q, 16) || !aligned(O, 16) || !aligned(lse, 4)) return W4A8_ERR_ALIGN;
+    if (!(scale > 0.0f) || scale > 3.0e38f || window < 0 || sinks < 0) return W4A8_ERR_SHAPE;
+    if (!aligned(Q, 16) || !aligned(O, 16) || !aligned(lse, 4) || !aligned(tree, 4)) return W4A8_ERR_ALIGN;
     if (workspace_bytes < kv_attention_workspace(rows, batch, q_heads, kv_heads, head_dim))
         return W4A8_ERR_BUFFER_TOO_SMALL;
     const w4a8_status arch = check_arch();
@@ -592,11 +598,137 @@ w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, con
     a.scale = scale;
     a.causal = causal != 0;
     a.window = window;
+    a.sinks = sinks;
+    a.tree = tree;
+    a.tree_words = tree_words;
     a.O = O;
     a.o_bf16 = o_type == W4A8_BF16;
     a.lse = lse;
     const cudaError_t e = launch_kv_attention(a, static_cast<uint8_t *>(workspace),
                                               static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
+}
+
+extern "C" {
+
+w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, const void *cache,
+                              int num_pages, int page_size, int kv_heads, int head_dim,
+                              const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                              const int32_t *cu_rows, int batch, int rows, int q_heads, float scale,
+                              int causal, int window, void *O, int o_type, float *lse,
+                              void *workspace, size_t workspace_bytes, void *stream)
+{
+    return kv_attention_common(Q, q_type, q_stride, cache, num_pages, page_size, kv_heads, head_dim, page_table,
+                               max_pages, kv_lens, cu_rows, batch, rows, q_heads, scale, causal, window, 0, nullptr, 0,
+                               O, o_type, lse, workspace, workspace_bytes, stream);
+}
+
+w4a8_status w4a8_kv_attention_sinks(const void *Q, int q_type, long long q_stride, const void *cache,
+                                    int num_pages, int page_size, int kv_heads, int head_dim,
+                                    const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                                    const int32_t *cu_rows, int batch, int rows, int q_heads, float scale,
+                                    int causal, int window, int sinks, void *O, int o_type, float *lse,
+                                    void *workspace, size_t workspace_bytes, void *stream)
+{
+    return kv_attention_common(Q, q_type, q_stride, cache, num_pages, page_size, kv_heads, head_dim, page_table,
+                               max_pages, kv_lens, cu_rows, batch, rows, q_heads, scale, causal, window, sinks, nullptr, 0,
+                               O, o_type, lse, workspace, workspace_bytes, stream);
+}
+
+w4a8_status w4a8_kv_attention_tree(const void *Q, int q_type, long long q_stride, const void *cache,
+                                   int num_pages, int page_size, int kv_heads, int head_dim,
+                                   const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                                   const int32_t *cu_rows, int batch, int rows, int q_heads, float scale,
+                                   const uint32_t *tree_mask, int mask_words, int window, int sinks, void *O,
+                                   int o_type, float *lse, void *workspace, size_t workspace_bytes,
+                                   void *stream)
+{
+    if (!tree_mask) return W4A8_ERR_NULL;
+    if (mask_words < 1 || mask_words > (1 << 20)) return W4A8_ERR_SHAPE;
+    return kv_attention_common(Q, q_type, q_stride, cache, num_pages, page_size, kv_heads, head_dim, page_table,
+                               max_pages, kv_lens, cu_rows, batch, rows, q_heads, scale, 1, window, sinks, tree_mask,
+                               mask_words, O, o_type, lse, workspace, workspace_bytes, stream);
+}
+
+w4a8_status w4a8_kv_plan(const int32_t *held, const int32_t *kv_lens, const int32_t *add, int batch,
+                         int32_t *page_table, int max_pages, int page_size, int32_t *free_pages,
+                         int num_pages, const int32_t *free_count, int32_t *free_count_out,
+                         int32_t *kv_lens_out, int32_t *cu_rows, int32_t *positions, int64_t *slots,
+                         int rows, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!kv_lens || !add || !page_table || !free_pages || !free_count || !free_count_out || !kv_lens_out || !cu_rows || !workspace)
+        return W4A8_ERR_NULL;
+    if (batch < 1 || batch > kPlanMaxBatch || max_pages < 1 || num_pages < 1 || rows < 1 || !kv_shape_ok(page_size, 1, 64) ||
+        (long long)max_pages * page_size > (1ll << 31) - 1024 || (held && kv_lens_out == kv_lens))
+        return W4A8_ERR_SHAPE;
+    for (const void *p : {(const void *)held, (const void *)kv_lens, (const void *)add, (const void *)page_table, (const void *)free_pages,
+                          (const void *)free_count, (const void *)free_count_out, (const void *)kv_lens_out, (const void *)cu_rows,
+                          (const void *)positions})
+        if (!aligned(p, 4)) return W4A8_ERR_ALIGN;
+    if (!aligned(slots, 8) || !aligned(workspace, 256)) return W4A8_ERR_ALIGN;
+    if (workspace_bytes < sizeof(StatusBlock) + 256) return W4A8_ERR_BUFFER_TOO_SMALL;
+    const w4a8_status arch = check_arch();
+    if (arch != W4A8_OK) return arch;
+    KvPlanArgs a = {held, kv_lens, add, page_table, free_pages, free_count, free_count_out, kv_lens_out, cu_rows, positions, slots,
+                    batch, max_pages, 0, num_pages, rows};
+    while ((1 << a.page_shift) < page_size) ++a.page_shift;
+    const cudaError_t e = launch_kv_plan(a, static_cast<StatusBlock *>(workspace),
+                                         reinterpret_cast<int *>(static_cast<uint8_t *>(workspace) + sizeof(StatusBlock)),
+                                         static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
+}
+
+w4a8_status w4a8_rope_kv_append(const void *Q, const void *K, const void *V, int dtype, long long q_stride,
+                                long long k_stride, long long v_stride, const int32_t *positions, int axes,
+                                const int32_t *pair_axis, const float *inv_freq, int rotary_dim,
+                                int interleaved, void *Q_out, long long q_out_stride, void *cache,
+                                int num_pages, int page_size, int kv_heads, int head_dim,
+                                const int64_t *slots, int rows, int q_heads, void *workspace,
+                                size_t workspace_bytes, void *stream)
+{
+    if (!Q || !K || !V || !positions || !inv_freq || !Q_out || !cache || !slots || !workspace) return W4A8_ERR_NULL;
+    if (!kv_shape_ok(page_size, kv_heads, head_dim) || num_pages < 1 || rows < 1 || q_heads < 1 || q_heads > 65535 ||
+        (long long)rows * (q_heads + 2ll * kv_heads) >= (1ll << 31))
+        return W4A8_ERR_SHAPE;
+    if (!is_16bit(dtype) || axes < 1 || axes > 16 || rotary_dim < 16 || rotary_dim > head_dim || rotary_dim % 16 != 0)
+        return W4A8_ERR_SHAPE;
+    const long long q_least = (long long)q_heads * head_dim, k_least = (long long)kv_heads * head_dim;
+    if (q_stride < q_least || q_out_stride < q_least || k_stride < k_least || v_stride < k_least || q_stride % 8 != 0 ||
+        q_out_stride % 8 != 0 || k_stride % 8 != 0 || v_stride % 8 != 0 || (Q_out == Q && q_out_stride != q_stride))
+        return W4A8_ERR_SHAPE;
+    if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(Q_out, 16) || !aligned(cache, 16) ||
+        !aligned(positions, 4) || !aligned(pair_axis, 4) || !aligned(inv_freq, 4) || !aligned(slots, 8) || !aligned(workspace, 256))
+        return W4A8_ERR_ALIGN;
+    if (workspace_bytes < sizeof(StatusBlock)) return W4A8_ERR_BUFFER_TOO_SMALL;
+    const w4a8_status arch = check_arch();
+    if (arch != W4A8_OK) return arch;
+    KvCache c = {static_cast<uint8_t *>(cache), num_pages, 0, kv_heads, head_dim};
+    while ((1 << c.page_shift) < page_size) ++c.page_shift;
+    const RopeArgs a = {Q, K, V, q_stride, k_stride, v_stride, positions, pair_axis, inv_freq, Q_out, q_out_stride, slots, axes,
+                        rotary_dim, rows, q_heads};
+    const cudaError_t e = launch_rope_kv_append(a, dtype == W4A8_BF16, interleaved != 0, c, static_cast<StatusBlock *>(workspace),
+                                                static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
+}
+
+w4a8_status w4a8_kv_accept(void *cache, int num_pages, int page_size, int kv_heads, int head_dim,
+                           const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                           const int32_t *cu_rows, int batch, int rows, const int32_t *accepted, int max_accept,
+                           const int32_t *accept_lens, int32_t *kv_lens_out, void *workspace,
+                           size_t workspace_bytes, void *stream)
+{
+    if (!accepted || !accept_lens) return W4A8_ERR_NULL;
+    KvCache c;
+    KvBatch bt;
+    const w4a8_status s = kv_common(cache, num_pages, page_size, kv_heads, head_dim, page_table, max_pages,
+                                    kv_lens, cu_rows, batch, rows, workspace, workspace_bytes, &c, &bt);
+    if (s != W4A8_OK) return s;
+    if (max_accept < 1 || kv_lens_out == kv_lens) return W4A8_ERR_SHAPE;
+    if (!aligned(accepted, 4) || !aligned(accept_lens, 4) || !aligned(kv_lens_out, 4)) return W4A8_ERR_ALIGN;
+    const w4a8_status arch = check_arch();
+    if (arch != W4A8_OK) return arch;
+    const cudaError_t e = launch_kv_accept(c, bt, {accepted, accept_lens, kv_lens_out, max_accept}, static_cast<StatusBlock *>(workspace),
+                                           static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
 }
 
@@ -699,6 +831,7 @@ w4a8_status w4a8_poll_status(void *workspace, void *stream)
     if (host[0] == 0) return W4A8_OK;
     if (cudaMemset(workspace, 0, sizeof(StatusBlock)) != cudaSuccess) return W4A8_ERR_CUDA;
     if (host[0] == W4A8_ERR_BAD_BLOB) return W4A8_ERR_BAD_BLOB;
+    if (host[0] == W4A8_ERR_NO_PAGES) return W4A8_ERR_NO_PAGES;
     return host[0] == W4A8_ERR_BAD_TABLE ? W4A8_ERR_BAD_TABLE : W4A8_ERR_TIMEOUT;
 }
 

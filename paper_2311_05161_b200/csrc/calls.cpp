@@ -1,5 +1,5 @@
 // Argument marshalling of the calls that a decoder makes per layer and token (residual + norm + quantizer, cache
-// append, read, attention): the functions of the same names in binding.py pass their arguments here.  The work
+// append, read, attention, rotary positions, accepted paths) and of a step's plan: the functions of the same names in binding.py pass their arguments here.  The work
 // of such a call takes the device 3 us or so, and the checks, allocations and the foreign call took 12 to 14 us in Python
 // (one token of 4096: 12.1 us there, 5.6 us here).  Nothing is computed or kept here.
 #include <Python.h>
@@ -283,34 +283,207 @@ PyObject *kv_read(PyObject *, PyObject *const *v, Py_ssize_t n)
     });
 }
 
+// What the three attention calls share: their arguments in the places of `v` that they name.
+struct Attention {
+    const at::Tensor &Q;
+    const int64_t stride, D;
+    const int heads;
+    const Batch b;
+    const float scale;
+    at::Tensor O;
+    const at::Tensor *lse;
+    void *st;
+    int rows, q_heads;
+    Attention(const char *call, PyObject *Q_, PyObject *cache, PyObject *table, PyObject *lens, PyObject *heads_, PyObject *space, PyObject *cu,
+              PyObject *scale_, PyObject *dtype, PyObject *out, PyObject *lse_, const at::Tensor *mask = nullptr)
+        : Q(of_16_bits(Q_, "Q", false)), stride(row_stride(Q, "Q")), D(Q.size(2)), heads(integer(heads_, "kv_heads")),
+          b(call, cache, table, lens, cu, space, heads, D), scale(scale_ == Py_None ? (float)std::pow((double)D, -0.5) : real(scale_))
+    {
+        const at::ScalarType type = scalar_type(dtype, "dtype");
+        if (out == Py_None && type != at::kHalf && type != at::kBFloat16) wrong_type("dtype: expected float16 or bfloat16");
+        if (out != Py_None) shaped(tensor(out, "out"), Q.sizes(), "out");
+        O = out == Py_None ? fresh(Q.sizes(), type, Q) : of_16_bits(out, "out");
+        lse = maybe(lse_, at::kFloat, "lse");
+        if (lse) shaped(*lse, {Q.size(0), Q.size(1)}, "lse");
+        st = stream_of(call, {&b.cache, &b.table, &b.lens, b.cu, &b.space, &Q, &O, lse, mask});
+        rows = number(Q.size(0), "Q");
+        q_heads = number(Q.size(1), "Q");
+    }
+    float *lse_at() const { return static_cast<float *>(at_or_null(lse)); }
+};
+
+// Q, cache, page_table, kv_lens, kv_heads, workspace, window, sinks, cu_rows, scale, causal, dtype, out, lse
+PyObject *kv_attention_sinks(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (!counted("kv_attention_sinks", n, 14)) return nullptr;
+    return guarded([&] {
+        const int window = integer(v[6], "window"), sinks = integer(v[7], "sinks"), causal = PyObject_IsTrue(v[10]);
+        if (causal < 0) throw Raised();
+        const Attention a("kv_attention_sinks", v[0], v[1], v[2], v[3], v[4], v[5], v[8], v[9], v[11], v[12], v[13]);
+        const Batch &b = a.b;
+        w4a8_status status;
+        Py_BEGIN_ALLOW_THREADS
+        status = w4a8_kv_attention_sinks(a.Q.data_ptr(), dtype_of(a.Q), a.stride, b.cache.data_ptr(), b.num_pages, b.page_size, a.heads, (int)a.D,
+                                         b.table_at(), b.max_pages, b.lens_at(), b.cu_at(), b.batch, a.rows, a.q_heads, a.scale, causal, window,
+                                         sinks, a.O.data_ptr(), dtype_of(a.O), a.lse_at(), b.space.data_ptr(), b.space.numel(), a.st);
+        Py_END_ALLOW_THREADS
+        check(status, "w4a8_kv_attention_sinks");
+        return own(v[12], a.O);
+    });
+}
+
+// Q, cache, page_table, kv_lens, kv_heads, workspace, tree_mask, cu_rows, scale, window, sinks, dtype, out, lse
+PyObject *kv_attention_tree(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (!counted("kv_attention_tree", n, 14)) return nullptr;
+    return guarded([&] {
+        const at::Tensor &mask = of_type(v[6], at::kInt, "tree_mask");
+        if (mask.dim() != 2) wrong_value("tree_mask: expected [rows, words]");
+        const int window = integer(v[9], "window"), sinks = integer(v[10], "sinks"), words = number(mask.size(1), "tree_mask");
+        const Attention a("kv_attention_tree", v[0], v[1], v[2], v[3], v[4], v[5], v[7], v[8], v[11], v[12], v[13], &mask);
+        shaped(mask, {a.Q.size(0), mask.size(1)}, "tree_mask");
+        const Batch &b = a.b;
+        w4a8_status status;
+        Py_BEGIN_ALLOW_THREADS
+        status = w4a8_kv_attention_tree(a.Q.data_ptr(), dtype_of(a.Q), a.stride, b.cache.data_ptr(), b.num_pages, b.page_size, a.heads, (int)a.D,
+                                        b.table_at(), b.max_pages, b.lens_at(), b.cu_at(), b.batch, a.rows, a.q_heads, a.scale,
+                                        static_cast<const uint32_t *>(mask.data_ptr()), words, window, sinks, a.O.data_ptr(), dtype_of(a.O),
+                                        a.lse_at(), b.space.data_ptr(), b.space.numel(), a.st);
+        Py_END_ALLOW_THREADS
+        check(status, "w4a8_kv_attention_tree");
+        return own(v[12], a.O);
+    });
+}
+
+// cache, page_table, kv_lens, accepted, accept_lens, kv_heads, head_dim, workspace, cu_rows, out
+PyObject *kv_accept(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (!counted("kv_accept", n, 10)) return nullptr;
+    return guarded([&] {
+        const int heads = integer(v[5], "kv_heads"), D = integer(v[6], "head_dim");
+        const Batch b("kv_accept", v[0], v[1], v[2], v[8], v[7], heads, D);
+        const at::Tensor &accepted = of_type(v[3], at::kInt, "accepted"), &lens = of_type(v[4], at::kInt, "accept_lens");
+        if (accepted.dim() != 2 || accepted.size(0) != b.batch) wrong_value("accepted: expected [batch, max_accept]");
+        shaped(lens, {b.batch}, "accept_lens");
+        const at::Tensor out = v[9] == Py_None ? fresh({b.batch}, at::kInt, b.lens) : of_type(v[9], at::kInt, "out");
+        shaped(out, {b.batch}, "out");
+        void *st = stream_of("kv_accept", {&b.cache, &b.table, &b.lens, b.cu, &b.space, &accepted, &lens, &out});
+        // (no row of the call is read here: with cu_rows any number of them will do)
+        const int most = number(accepted.size(1), "accepted"), rows = b.cu ? INT_MAX / heads : b.batch;
+        w4a8_status status;
+        Py_BEGIN_ALLOW_THREADS
+        status = w4a8_kv_accept(b.cache.data_ptr(), b.num_pages, b.page_size, heads, D, b.table_at(), b.max_pages, b.lens_at(), b.cu_at(), b.batch, rows,
+                                static_cast<const int32_t *>(accepted.data_ptr()), most, static_cast<const int32_t *>(lens.data_ptr()),
+                                static_cast<int32_t *>(out.data_ptr()), b.space.data_ptr(), b.space.numel(), st);
+        Py_END_ALLOW_THREADS
+        check(status, "w4a8_kv_accept");
+        return own(v[9], out);
+    });
+}
+
+// Q, K, V, positions, inv_freq, cache, slots, workspace, pair_axis, interleaved, out
+PyObject *rope_kv_append(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (!counted("rope_kv_append", n, 11)) return nullptr;
+    return guarded([&] {
+        const at::Tensor &Q = of_16_bits(v[0], "Q", false), &K = of_16_bits(v[1], "K", false), &V = of_16_bits(v[2], "V", false);
+        const int64_t qs = row_stride(Q, "Q"), ks = row_stride(K, "K"), vs = row_stride(V, "V"), rows = Q.size(0), D = Q.size(2), heads = K.size(1);
+        if (K.scalar_type() != Q.scalar_type() || V.scalar_type() != Q.scalar_type()) wrong_type("Q, K, V: expected one type");
+        shaped(K, {rows, heads, D}, "K");
+        shaped(V, K.sizes(), "V");
+        const at::Tensor &positions = of_type(v[3], at::kInt, "positions"), &freq = of_type(v[4], at::kFloat, "inv_freq");
+        if (positions.dim() != 1 && positions.dim() != 2) wrong_value("positions: expected [rows] or [axes, rows]");
+        const int64_t axes = positions.dim() == 2 ? positions.size(0) : 1;
+        if (positions.size(-1) != rows) wrong_value("positions: expected [rows] or [axes, rows]");
+        if (freq.dim() != 1) wrong_value("inv_freq: expected [rotary_dim / 2]");
+        const at::Tensor &cache = of_type(v[5], at::kByte, "cache"), &slots = of_type(v[6], at::kLong, "slots"), &space = of_type(v[7], at::kByte, "workspace");
+        const at::Tensor *axis = maybe(v[8], at::kInt, "pair_axis");
+        const int interleaved = PyObject_IsTrue(v[9]);
+        if (interleaved < 0) throw Raised();
+        if (axis) shaped(*axis, freq.sizes(), "pair_axis");
+        shaped(slots, {rows}, "slots");
+        if (cache.dim() != 2) wrong_value("cache: expected [num_pages, page_bytes]");
+        const int64_t bytes = cache.size(1), token = heads * (D + 8);
+        if (token <= 0 || bytes % token || bytes / token > INT_MAX || heads > INT_MAX || D > INT_MAX ||
+            (size_t)bytes != w4a8_kv_page_bytes((int)(bytes / token), (int)heads, (int)D))
+            wrong_value("rope_kv_append: pages of " + std::to_string(bytes) + " bytes do not hold " + std::to_string(heads) + " heads of " + std::to_string(D));
+        if (v[10] != Py_None) shaped(tensor(v[10], "out"), Q.sizes(), "out");
+        const at::Tensor out = v[10] == Py_None ? fresh(Q.sizes(), Q.scalar_type(), Q) : of_16_bits(v[10], "out", false);
+        if (out.scalar_type() != Q.scalar_type()) wrong_type("out: expected the type of Q");
+        const int64_t os = row_stride(out, "out");
+        void *st = stream_of("rope_kv_append", {&Q, &K, &V, &positions, &freq, &cache, &slots, &space, axis, &out});
+        const int r = number(rows, "Q"), q_heads = number(Q.size(1), "Q"), rotary = number(2 * freq.size(0), "inv_freq"), pages = number(cache.size(0), "cache"),
+                  n_axes = number(axes, "positions");
+        w4a8_status status;
+        Py_BEGIN_ALLOW_THREADS
+        status = w4a8_rope_kv_append(Q.data_ptr(), K.data_ptr(), V.data_ptr(), dtype_of(Q), qs, ks, vs, static_cast<const int32_t *>(positions.data_ptr()), n_axes,
+                                     static_cast<const int32_t *>(at_or_null(axis)), static_cast<const float *>(freq.data_ptr()), rotary, interleaved,
+                                     out.data_ptr(), os, cache.data_ptr(), pages, (int)(bytes / token), (int)heads, (int)D,
+                                     static_cast<const int64_t *>(slots.data_ptr()), r, q_heads, space.data_ptr(), space.numel(), st);
+        Py_END_ALLOW_THREADS
+        check(status, "w4a8_rope_kv_append");
+        return own(v[10], out);
+    });
+}
+
+// held, kv_lens, add, page_table, free_pages, free_count, page_size, rows, workspace, kv_lens_out, cu_rows, positions, slots, free_count_out
+PyObject *kv_plan(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (!counted("kv_plan", n, 14)) return nullptr;
+    return guarded([&] {
+        const at::Tensor *held = maybe(v[0], at::kInt, "held");
+        const at::Tensor &lens = of_type(v[1], at::kInt, "kv_lens"), &add = of_type(v[2], at::kInt, "add"), &table = of_type(v[3], at::kInt, "page_table"),
+                         &pages = of_type(v[4], at::kInt, "free_pages"), &count = of_type(v[5], at::kInt, "free_count"),
+                         &space = of_type(v[8], at::kByte, "workspace");
+        const int page_size = integer(v[6], "page_size"), rows = integer(v[7], "rows");
+        if (rows < 0) wrong_value("rows: negative");
+        if (table.dim() != 2) wrong_value("page_table: expected [batch, max_pages]");
+        const int batch = number(table.size(0), "page_table"), max_pages = number(table.size(1), "page_table");
+        shaped(lens, {batch}, "kv_lens");
+        shaped(add, {batch}, "add");
+        if (held) shaped(*held, {batch}, "held");
+        if (pages.dim() != 1) wrong_value("free_pages: expected [num_pages]");
+        const int num_pages = number(pages.size(0), "free_pages");
+        shaped(count, {1}, "free_count");
+        auto space_of = [&](PyObject *given, int64_t size, at::ScalarType type, const char *what) {
+            const at::Tensor t = given == Py_None ? fresh({size}, type, lens) : of_type(given, type, what);
+            shaped(t, {size}, what);
+            return t;
+        };
+        const at::Tensor new_lens = space_of(v[9], batch, at::kInt, "kv_lens_out"), cu = space_of(v[10], (int64_t)batch + 1, at::kInt, "cu_rows"),
+                         pos = space_of(v[11], rows, at::kInt, "positions"), slots = space_of(v[12], rows, at::kLong, "slots"),
+                         left = space_of(v[13], 1, at::kInt, "free_count_out");
+        void *st = stream_of("kv_plan", {held, &lens, &add, &table, &pages, &count, &space, &new_lens, &cu, &pos, &slots, &left});
+        auto ints = [](const at::Tensor &t) { return static_cast<int32_t *>(t.data_ptr()); };
+        w4a8_status status;
+        Py_BEGIN_ALLOW_THREADS
+        status = w4a8_kv_plan(held ? ints(*held) : nullptr, ints(lens), ints(add), batch, ints(table), max_pages, page_size, ints(pages), num_pages,
+                              ints(count), ints(left), ints(new_lens), ints(cu), ints(pos), static_cast<int64_t *>(slots.data_ptr()), rows,
+                              space.data_ptr(), space.numel(), st);
+        Py_END_ALLOW_THREADS
+        check(status, "w4a8_kv_plan");
+        PyObject *out[5] = {own(v[9], new_lens), own(v[10], cu), own(v[11], pos), own(v[12], slots), own(v[13], left)};
+        return tuple(out);
+    });
+}
+
 // Q, cache, page_table, kv_lens, kv_heads, workspace, cu_rows, scale, causal, window, dtype, out, lse
 PyObject *kv_attention(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     if (!counted("kv_attention", n, 13)) return nullptr;
     return guarded([&] {
-        const at::Tensor &Q = of_16_bits(v[0], "Q", false);
-        const int64_t stride = row_stride(Q, "Q"), D = Q.size(2);
-        const int heads = integer(v[4], "kv_heads");
-        const Batch b("kv_attention", v[1], v[2], v[3], v[6], v[5], heads, D);
-        const float scale = v[7] == Py_None ? (float)std::pow((double)D, -0.5) : real(v[7]);
         const int causal = PyObject_IsTrue(v[8]), window = integer(v[9], "window");
         if (causal < 0) throw Raised();
-        const at::ScalarType type = scalar_type(v[10], "dtype");
-        if (v[11] == Py_None && type != at::kHalf && type != at::kBFloat16) wrong_type("dtype: expected float16 or bfloat16");
-        if (v[11] != Py_None) shaped(tensor(v[11], "out"), Q.sizes(), "out");
-        const at::Tensor O = v[11] == Py_None ? fresh(Q.sizes(), type, Q) : of_16_bits(v[11], "out");
-        const at::Tensor *lse = maybe(v[12], at::kFloat, "lse");
-        if (lse) shaped(*lse, {Q.size(0), Q.size(1)}, "lse");
-        void *st = stream_of("kv_attention", {&b.cache, &b.table, &b.lens, b.cu, &b.space, &Q, &O, lse});
-        const int rows = number(Q.size(0), "Q"), q_heads = number(Q.size(1), "Q");
+        const Attention a("kv_attention", v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[10], v[11], v[12]);
+        const Batch &b = a.b;
         w4a8_status status;
         Py_BEGIN_ALLOW_THREADS
-        status = w4a8_kv_attention(Q.data_ptr(), dtype_of(Q), stride, b.cache.data_ptr(), b.num_pages, b.page_size, heads, (int)D, b.table_at(),
-                                   b.max_pages, b.lens_at(), b.cu_at(), b.batch, rows, q_heads, scale, causal, window, O.data_ptr(),
-                                   dtype_of(O), static_cast<float *>(at_or_null(lse)), b.space.data_ptr(), b.space.numel(), st);
+        status = w4a8_kv_attention(a.Q.data_ptr(), dtype_of(a.Q), a.stride, b.cache.data_ptr(), b.num_pages, b.page_size, a.heads, (int)a.D, b.table_at(),
+                                   b.max_pages, b.lens_at(), b.cu_at(), b.batch, a.rows, a.q_heads, a.scale, causal, window, a.O.data_ptr(),
+                                   dtype_of(a.O), a.lse_at(), b.space.data_ptr(), b.space.numel(), a.st);
         Py_END_ALLOW_THREADS
         check(status, "w4a8_kv_attention");
-        return own(v[11], O);
+        return own(v[11], a.O);
     });
 }
 
@@ -329,6 +502,11 @@ PyMethodDef methods[] = {
     {"kv_append", (PyCFunction)(void (*)(void))kv_append, METH_FASTCALL, nullptr},
     {"kv_read", (PyCFunction)(void (*)(void))kv_read, METH_FASTCALL, nullptr},
     {"kv_attention", (PyCFunction)(void (*)(void))kv_attention, METH_FASTCALL, nullptr},
+    {"kv_attention_sinks", (PyCFunction)(void (*)(void))kv_attention_sinks, METH_FASTCALL, nullptr},
+    {"kv_attention_tree", (PyCFunction)(void (*)(void))kv_attention_tree, METH_FASTCALL, nullptr},
+    {"kv_accept", (PyCFunction)(void (*)(void))kv_accept, METH_FASTCALL, nullptr},
+    {"kv_plan", (PyCFunction)(void (*)(void))kv_plan, METH_FASTCALL, nullptr},
+    {"rope_kv_append", (PyCFunction)(void (*)(void))rope_kv_append, METH_FASTCALL, nullptr},
     {"set_errors", (PyCFunction)(void (*)(void))set_errors, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

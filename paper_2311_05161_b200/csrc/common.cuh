@@ -124,7 +124,7 @@ __host__ __device__ inline size_t code3_word_offset(const BlobLayout &L, int n, 
 // status block (first 256 bytes of a workspace)
 // ---------------------------------------------------------------------------
 struct StatusBlock {
-    int status;       // 0, W4A8_ERR_TIMEOUT, _BAD_BLOB or _BAD_TABLE: first failure wins
+    int status;       // 0, W4A8_ERR_TIMEOUT, _BAD_BLOB, _BAD_TABLE or _NO_PAGES: first failure wins
     int where;        // site code of the wait that gave up
     int block;        // CTA that reported
     int pad[61];

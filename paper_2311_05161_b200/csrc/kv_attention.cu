@@ -34,6 +34,8 @@
 // 131001 tokens 52.8 us; 32 ragged sequences with 32 heads of their own 56.1 us; 513 tokens 9.2 us.  Beside the main
 // loop (some 36 us of the 52.8 us, at 1200 cycles per 32 tokens and scheduler) stand 8 us until the first
 // unit is there (place on the list, page numbers, queries, copies, each waiting for the one before) and 4 us for the joins.
+#include <type_traits>
+
 #include "kv_attention.cuh"
 
 namespace w4a8 {
@@ -82,6 +84,7 @@ struct Schedule {
 // One sequence's part of the work list.
 struct Part : Seq {
     int first, units;          // units of 32 tokens that any of its rows can see
+    int few;                   // the extended form: that many of them hold sinks, the others follow from `first` on
     int tiles;                 // row tiles per key head
     // length of the work list: an item is `lead` places and then its units, at least one
     __device__ int item_length(int lead) const { return lead + max(units, 1); }
@@ -91,13 +94,19 @@ struct Part : Seq {
     }
 };
 
-template <int R>
+template <int R, bool WIDE>
 __device__ __forceinline__ Part load_part(const KvAttnArgs &a, int b, int group, StatusBlock *sb)
 {
     Part s;
     static_cast<Seq &>(s) = load_seq(a, b, sb);
     s.first = Sight(a, s).lo(0) >> 5;
     s.units = max(0, ((s.len + 31) >> 5) - s.first);
+    s.few = 0;
+    if constexpr (WIDE) {
+        s.few = sink_units(WideSight(a, s).sinks, s.first, 5);
+        s.units += s.few;
+        if (a.tree && s.n > 32 * a.tree_words) report_failure(sb, W4A8_ERR_BAD_TABLE, b);
+    }
     s.tiles = (int)(((long long)s.n * group + R - 1) / R);
     return s;
 }
@@ -123,7 +132,7 @@ struct Shape {
     static_assert(kCtas * (kSmem + 5 * 1024) <= 232448, "shared memory of an SM");
 };
 
-template <int D, int NT, int WARPS>
+template <int D, int NT, int WARPS, bool WIDE>
 __global__ void __launch_bounds__(WARPS * 32, Shape<D, NT, WARPS>::kCtas)
 kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
 {
@@ -133,7 +142,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     __shared__ long long warp_units[WARPS], found_off;
     __shared__ int found_b, last_part;
     __shared__ float row_m[WARPS][R], row_l[WARPS][R], tile_m[R], tile_l[R];
-    __shared__ int row_hi[R], row_lo[R];
+    __shared__ int row_hi[R], row_lo[R], row_no[WIDE ? R : 1];
     __shared__ __align__(16) uint4 q_frag[NT][KW][32];
     __shared__ float q_sum[R], q_unit[R];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -152,7 +161,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     const int chunk = (bt.batch + THREADS - 1) / THREADS;
     const int b_first = min(bt.batch, tid * chunk), b_last = min(bt.batch, b_first + chunk);
     long long mine = 0;
-    for (int b = b_first; b < b_last; ++b) mine += load_part<R>(a, b, group, sc.sb).list_length(heads, sc.lead);
+    for (int b = b_first; b < b_last; ++b) mine += load_part<R, WIDE>(a, b, group, sc.sb).list_length(heads, sc.lead);
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -173,7 +182,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     if (begin >= incl - mine && begin < incl) {
         long long at = incl - mine;
         for (int b = b_first; b < b_last; ++b) {
-            const long long u = load_part<R>(a, b, group, sc.sb).list_length(heads, sc.lead);
+            const long long u = load_part<R, WIDE>(a, b, group, sc.sb).list_length(heads, sc.lead);
             if (begin < at + u) {
                 found_b = b;
                 found_off = begin - at;
@@ -190,7 +199,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     bool dead = false;                     // a copy did not arrive in time: nothing more is requested
 
     for (long long u = begin; u < end;) {
-        const Part s = load_part<R>(a, b, group, sc.sb);
+        const Part s = load_part<R, WIDE>(a, b, group, sc.sb);
         const long long all = s.list_length(heads, sc.lead);
         if (off >= all) {
             off -= all;
@@ -212,18 +221,47 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         // rows of this tile: r = tile * R + i is row r / group of the sequence, query head r % group
         const int rows_here = (int)min((long long)R, (long long)s.n * group - (long long)tile * R);
         const int i_first = sc.group.div(tile * R), i_last = sc.group.div(tile * R + rows_here - 1);
-        const Sight sight(a, s);
-        const int hi_max = sight.hi(i_last), hi_min = sight.hi(i_first);
-        const int lo_min = sight.lo(i_first), lo_max = sight.lo(i_last);
-        if (tid < R) {
-            const int i = sc.group.div(tile * R + tid);
-            row_hi[tid] = tid < rows_here ? sight.hi(i) : s.len;
-            row_lo[tid] = tid < rows_here ? sight.lo(i) : 0;
+        using View = std::conditional_t<WIDE, WideSight, Sight>;
+        const View sight(a, s);
+        int hi_max, hi_min, lo_min, lo_max;
+        if constexpr (WIDE) {
+            hi_max = sight.tile_hi(i_last), hi_min = sight.all_hi(i_first);
+            lo_min = sight.tile_lo(i_first), lo_max = sight.all_lo(i_last);
+            if (tid < R) {                 // (a place without a row sees nothing: -1)
+                const int i = sc.group.div(tile * R + tid);
+                row_hi[tid] = tid < rows_here ? sight.row_hi(i) : 0;
+                row_lo[tid] = tid < rows_here ? sight.row_lo(i) : 0;
+                row_no[tid] = tid < rows_here ? i : -1;
+            }
+        } else {
+            hi_max = sight.hi(i_last), hi_min = sight.hi(i_first);
+            lo_min = sight.lo(i_first), lo_max = sight.lo(i_last);
+            if (tid < R) {
+                const int i = sc.group.div(tile * R + tid);
+                row_hi[tid] = tid < rows_here ? sight.hi(i) : s.len;
+                row_lo[tid] = tid < rows_here ? sight.lo(i) : 0;
+            }
         }
         // units of the share that some row of the tile sees, and this warp's among them
-        const int k0 = max(s.first + in_item, lo_min >> 5);
-        const int k1 = min(s.first + min(in_item + count, s.units), (hi_max + 31) >> 5);
-        const int nk = k1 > k0 + warp ? (k1 - k0 - warp + WARPS - 1) / WARPS : 0;
+        int k0 = max(s.first + in_item, lo_min >> 5);
+        const int k1 = min(s.first + min(in_item + count, s.units) - s.few, (hi_max + 31) >> 5);
+        int few = 0, few0 = 0, near = 0, sink_block = -1;    // units of sinks, the first of them; sinks, the last block with some
+        if constexpr (WIDE) {
+            few0 = in_item;
+            few = max(min(min(in_item + count, s.few), (min(sight.sinks, hi_max) + 31) >> 5) - few0, 0);
+            k0 = max(in_item - s.few, 0) + s.first;
+            // (where the window begins among the units of sinks, these are walked with it)
+            if (((sight.sinks + 31) >> 5) <= s.first) k0 = max(k0, lo_min >> 5);
+            near = sight.sinks;
+            sink_block = near > 0 ? (near - 1) >> 4 : -1;
+        }
+        const int units_here = few + max(k1 - k0, 0);
+        const int nk = units_here > warp ? (units_here - warp + WARPS - 1) / WARPS : 0;
+        auto unit_at = [&](int k) {        // this warp's k-th
+            const int u = warp + k * WARPS;
+            if constexpr (WIDE) return u < few ? few0 + u : k0 + u - few;
+            return k0 + u;
+        };
         const int last_block = (s.len - 1) >> 4;
         const int32_t *table = bt.page_table + (size_t)b * bt.max_pages;
         const uint8_t *head_base = a.cache.pages + ((size_t)h << a.cache.page_shift) * (D + 8);
@@ -234,7 +272,8 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         size_t where = 0;
         int requested = 0;                 // units of this item whose copies were started
         auto look_up = [&](int k) {
-            const int blk = max(min(2 * (k0 + warp + (k + (lane >> 1)) * WARPS) + (lane & 1), last_block), lo_min >> 4);
+            int blk = min(2 * unit_at(k + (lane >> 1)) + (lane & 1), last_block);
+            if (!WIDE || blk > sink_block) blk = max(blk, lo_min >> 4);
             int page = __ldca(table + (blk >> page_bits));
             if ((unsigned)page >= (unsigned)a.cache.num_pages) {
                 report_failure(sc.sb, W4A8_ERR_BAD_TABLE, b);
@@ -413,23 +452,39 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
                         wt[j][n][2 * i + 1] = fmaf(c[j][n][2 * i + 1] + cs[j][n][2 * i + 1], u * unit[n][1], v);
                     }
                 }
-            const int j0 = (k0 + warp + k * WARPS) * 32;
+            const int j0 = unit_at(k) * 32;
             if (j0 < lo_max || j0 + 32 > hi_min) {           // some row does not see all of the unit
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
+                    if constexpr (!WIDE) {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int r = n * 8 + 2 * t + (i & 1), at = j0 + 16 * j + g + (i >> 1) * 8;
-                            if (at < row_lo[r] || at >= row_hi[r]) wt[j][n][i] = -INFINITY;
-                        }
+                            for (int i = 0; i < 4; ++i) {
+                                const int r = n * 8 + 2 * t + (i & 1), at = j0 + 16 * j + g + (i >> 1) * 8;
+                                if (at < row_lo[r] || at >= row_hi[r]) wt[j][n][i] = -INFINITY;
+                            }
+                    }
                     // the words of a token that no row sees are anything (behind the end, in front of the window)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int at = j0 + 16 * j + g + 8 * i;
-                        if (at < lo_min || at >= s.len) inv[j][i] = 0.0f;
+                        if ((at < lo_min && at >= near) || at >= s.len) inv[j][i] = 0.0f;
                     }
+                }
+                if constexpr (WIDE) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int r = n * 8 + 2 * t + i;
+                            const uint32_t seen = row_no[r] < 0 ? 0u : sight.visible(row_no[r], row_lo[r], row_hi[r], j0) >> g;
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                if (!(seen >> (16 * j) & 1u)) wt[j][n][i] = -INFINITY;
+                                if (!(seen >> (16 * j + 8) & 1u)) wt[j][n][2 + i] = -INFINITY;
+                            }
+                        }
                 }
             }
             // ---- weights ----
@@ -712,14 +767,19 @@ bool use_prefill(int rows, int batch, int q_heads, int kv_heads)
     return (long long)(q_heads / kv_heads) * rows > 64ll * batch;
 }
 
-template <int D, int NT, int WARPS>
-cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
+template <int D, int NT, int WARPS, bool WIDE>
+cudaError_t launch_instance(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
 {
     using S = Shape<D, NT, WARPS>;
     static std::atomic<int> raised[kMaxDevices];
-    const cudaError_t e = raise_smem_limit(kv_decode_kernel<D, NT, WARPS>, S::kSmem, raised);
+    const cudaError_t e = raise_smem_limit(kv_decode_kernel<D, NT, WARPS, WIDE>, S::kSmem, raised);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(kv_decode_kernel<D, NT, WARPS>, dim3(ctas), dim3(WARPS * 32), S::kSmem, st, a, sc);
+    return launch_overlapped(kv_decode_kernel<D, NT, WARPS, WIDE>, dim3(ctas), dim3(WARPS * 32), S::kSmem, st, a, sc);
+}
+template <int D, int NT, int WARPS>
+cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
+{
+    return a.extended() ? launch_instance<D, NT, WARPS, true>(a, sc, ctas, st) : launch_instance<D, NT, WARPS, false>(a, sc, ctas, st);
 }
 template <int D>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, const Variant &v, cudaStream_t st)

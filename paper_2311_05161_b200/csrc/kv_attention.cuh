@@ -179,6 +179,53 @@ struct Sight {
     __device__ int lo(int i) const { return window > 0 ? (int)max(0ll, (long long)pos0 + i + 1 - window) : 0; }
 };
 
+// The same with what the extended form knows: `sinks` first tokens that stay visible beside the window, or the rows of a drafted
+// tree.  A row sees keys [0, sinks) and [lo, hi), the former below hi too; a drafted row sees, beside those of the tokens
+// in front of the drafts, the drafted rows of its mask.  It stands behind as many drafted tokens as its mask has bits (its own
+// among them): that is its position for the window.
+struct WideSight : Sight {
+    int n, sinks, row0, words;
+    const uint32_t *tree;
+    __device__ WideSight(const KvAttnArgs &a, const Seq &s)
+        : Sight(a, s), n(s.n), sinks(a.window > 0 ? min(a.sinks, s.len) : 0), row0(s.row0), words(a.tree_words), tree(a.tree) {}
+    // rows i .. of a tile: the first token in front of which none of them looks (sinks apart), and the end of what any sees
+    __device__ int tile_lo(int i_first) const { return lo(tree ? 0 : i_first); }
+    __device__ int tile_hi(int i_last) const { return !tree ? hi(i_last) : pos0 + i_last < 0 ? 0 : len; }
+    // bounds of the tokens that all rows of a tile see
+    __device__ int all_lo(int i_last) const { return lo(tree ? n - 1 : i_last); }
+    __device__ int all_hi(int i_first) const { return row_hi(i_first); }
+    // one row: the end of the tokens that the window governs, and their beginning
+    __device__ int row_hi(int i) const { return !tree ? hi(i) : pos0 + i < 0 ? 0 : max(pos0, 0); }
+    __device__ uint32_t tree_word(int i, int w) const        // bits of drafted rows 32 w .. 32 w + 31 of the sequence
+    {
+        if (w < 0 || w >= words || 32 * w >= n) return 0u;
+        const uint32_t v = __ldca(tree + (size_t)(row0 + i) * words + w);
+        return n - 32 * w >= 32 ? v : v & ((1u << (n - 32 * w)) - 1u);
+    }
+    __device__ int row_lo(int i) const
+    {
+        if (!tree || window == 0) return lo(i);
+        int behind = 0;
+        for (int w = 0; w < words && 32 * w < n; ++w) behind += __popc(tree_word(i, w));
+        return lo(max(behind - 1, 0));
+    }
+    // Tokens j0 .. j0 + 31 that row i sees, a bit each; (row_lo, row_hi) as above.
+    __device__ uint32_t visible(int i, int row_lo, int row_hi, int j0) const
+    {
+        auto below = [&](int end) { return end <= j0 ? 0u : end - j0 >= 32 ? 0xffffffffu : (1u << (end - j0)) - 1u; };
+        uint32_t v = below(row_hi) & (~below(row_lo) | below(sinks));
+        if (tree && pos0 + i >= 0) {
+            const int from = j0 - pos0;
+            v |= __funnelshift_r(tree_word(i, from >> 5), tree_word(i, (from >> 5) + 1), from & 31);
+        }
+        return v;
+    }
+};
+
+// Where the units of a tile lie that has sinks: `few` of them hold first tokens only and lie in front of the window's first
+// unit; none where the window begins among them.
+__device__ __forceinline__ int sink_units(int sinks, int first, int shift) { return min((sinks + (1 << shift) - 1) >> shift, first); }
+
 // Counters of shared items in the workspace, behind the status block.  Both kernels use this region and
 // leave it zero, so that calls of either kind can follow each other on one workspace.
 constexpr int kCountersPerSm = 8;

@@ -142,11 +142,73 @@ __device__ __forceinline__ void kv_levels(uint32_t w, int z, __half2 (&o)[4])
     }
 }
 
+template <typename T> __device__ __forceinline__ float2 to_float2(uint32_t v);
+template <> __device__ __forceinline__ float2 to_float2<__half>(uint32_t v)
+{
+    return __half22float2(*reinterpret_cast<const __half2 *>(&v));
+}
+template <> __device__ __forceinline__ float2 to_float2<__nv_bfloat16>(uint32_t v)
+{
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+
+// Rounded once, values beyond the type's range to its largest finite ones.
+template <typename T> __device__ __forceinline__ uint32_t pack2_sat(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2_sat<__half>(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(fminf(fmaxf(a, -65504.0f), 65504.0f),
+                                        fminf(fmaxf(b, -65504.0f), 65504.0f));
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack2_sat<__nv_bfloat16>(float a, float b)
+{
+    const float m = __uint_as_float(0x7f7f0000u);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(fminf(fmaxf(a, -m), m), fminf(fmaxf(b, -m), m));
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
 cudaError_t launch_kv_append(const void *K, const void *V, int bf16, long long k_stride,
                              long long v_stride, const KvCache &c, const KvBatch &bt,
                              StatusBlock *sb, cudaStream_t st);
 cudaError_t launch_kv_read(const KvCache &c, const KvBatch &bt, void *K, void *V, int bf16,
                            StatusBlock *sb, cudaStream_t st);
+
+// Rotary positions: element pairs of the first `rotary` elements, turned by position[axis of the pair] * inv_freq[pair].
+struct RopeArgs {
+    const void *Q, *K, *V;
+    long long q_stride, k_stride, v_stride;
+    const int32_t *positions;                // [axes][rows]
+    const int32_t *pair_axis;                // [rotary / 2] or NULL: axis 0
+    const float *inv_freq;                   // [rotary / 2]
+    void *Q_out;
+    long long q_out_stride;
+    const int64_t *slots;                    // [rows]: page * page_size + place, negative: no row
+    int axes, rotary, rows, q_heads;
+};
+cudaError_t launch_rope_kv_append(const RopeArgs &a, int bf16, int interleaved, const KvCache &c, StatusBlock *sb,
+                                  cudaStream_t st);
+
+// Accepted drafted rows, as places among the sequence's rows of the call.
+struct KvPaths {
+    const int32_t *accepted;                 // [batch][most]
+    const int32_t *accept_lens;              // [batch]
+    int32_t *kv_lens_out;                    // [batch] or NULL
+    int most;
+};
+cudaError_t launch_kv_accept(const KvCache &c, const KvBatch &bt, const KvPaths &paths, StatusBlock *sb, cudaStream_t st);
+
+// A step's plan.
+struct KvPlanArgs {
+    const int32_t *held, *kv_lens, *add;     // [batch]
+    int32_t *page_table;                     // [batch][max_pages]
+    int32_t *free_pages;                     // [num_pages]
+    const int32_t *free_count;
+    int32_t *free_count_out, *kv_lens_out, *cu_rows, *positions;
+    int64_t *slots;
+    int batch, max_pages, page_shift, num_pages, rows;
+};
+constexpr int kPlanMaxBatch = 16384;
+cudaError_t launch_kv_plan(const KvPlanArgs &a, StatusBlock *sb, int *ticket, cudaStream_t st);
 
 struct KvAttnArgs {
     const void *Q;
@@ -160,6 +222,11 @@ struct KvAttnArgs {
     void *O;
     int o_bf16;
     float *lse;
+    // the extended form only
+    int sinks;                               // first tokens that stay visible beside the window
+    const uint32_t *tree;                    // [rows][tree_words] or NULL: drafted rows that a row sees
+    int tree_words;
+    bool extended() const { return tree != nullptr || (sinks > 0 && window > 0); }
 };
 size_t kv_attention_workspace(int rows, int batch, int q_heads, int kv_heads, int D);
 cudaError_t launch_kv_attention(const KvAttnArgs &a, uint8_t *workspace, cudaStream_t st);

@@ -204,6 +204,7 @@ struct Piece {
     int row0, n, len;                          // of the sequence
     int unit0, count;                          // units to walk; count < 0: no more pieces
     int lo;                                    // first token that a row of the tile sees
+    int few, few0;                             // the extended form: its first `few` units hold sinks and lie from few0 on
     int whole;                                 // the item lies in this share alone
     int slot;                                  // else: where the part goes
 };
@@ -243,7 +244,9 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, Control
 
 // The share of the work list a CTA walks through: the list is, for every sequence, row tile and key
 // head in this order, kLead places and then the units that the tile's rows see (at least one place).
+template <bool WIDE>
 struct Walk {
+    using View = std::conditional_t<WIDE, WideSight, Sight>;
     const KvAttnArgs &a;
     const Schedule &sc;
     long long at, end, off;                    // place on the list, end of the share, place inside (sequence, tile)
@@ -251,7 +254,7 @@ struct Walk {
     Seq s;
     bool loaded;
     // the current piece
-    int h, rows, i_first, lo, first, units, from, count;
+    int h, rows, i_first, lo, first, few, units, from, count;     // few: units of sinks, among `units`
     long long first_unit;                      // the item's first unit on the list
     bool whole;
 
@@ -259,22 +262,31 @@ struct Walk {
 
     __device__ static int tiles_of(const Seq &s, int group) { return (int)(((long long)s.n * group + kRows - 1) / kRows); }
     __device__ static void span(const KvAttnArgs &a, const Schedule &sc, const Seq &s, int tile, int &i_first, int &i_last, int &rows,
-                                int &lo, int &first, int &units)
+                                int &lo, int &first, int &few, int &units)
     {
         rows = (int)min((long long)kRows, (long long)s.n * sc.group.d - (long long)tile * kRows);
         i_first = sc.group.div(tile * kRows);
         i_last = sc.group.div(tile * kRows + rows - 1);
-        const Sight sight(a, s);
-        lo = sight.lo(i_first);
-        first = lo >> kUnitShift;
-        units = max(0, ((sight.hi(i_last) + kUnit - 1) >> kUnitShift) - first);
+        const View sight(a, s);
+        few = 0;
+        if constexpr (WIDE) {
+            lo = sight.tile_lo(i_first);
+            first = lo >> kUnitShift;
+            const int hi = sight.tile_hi(i_last);
+            few = sink_units(min(sight.sinks, hi), first, kUnitShift);
+            units = few + max(0, ((hi + kUnit - 1) >> kUnitShift) - first);
+        } else {
+            lo = sight.lo(i_first);
+            first = lo >> kUnitShift;
+            units = max(0, ((sight.hi(i_last) + kUnit - 1) >> kUnitShift) - first);
+        }
     }
     // Places of the row tiles first_tile + lane of a sequence (0 behind the last).
     __device__ static long long tile_places(const KvAttnArgs &a, const Schedule &sc, const Seq &s, int t)
     {
         if (t >= tiles_of(s, (int)sc.group.d)) return 0;
-        int i0, i1, rows, lo, first, units;
-        span(a, sc, s, t, i0, i1, rows, lo, first, units);
+        int i0, i1, rows, lo, first, few, units;
+        span(a, sc, s, t, i0, i1, rows, lo, first, few, units);
         return (long long)a.cache.heads * (kLead + max(units, 1));
     }
     __device__ void start(int b0, int tile0, long long off0, long long begin, long long end_)
@@ -304,7 +316,7 @@ struct Walk {
                 continue;
             }
             int i_last;
-            span(a, sc, s, tile, i_first, i_last, rows, lo, first, units);
+            span(a, sc, s, tile, i_first, i_last, rows, lo, first, few, units);
             const int body = max(units, 1), length = kLead + body;
             if (off >= (long long)a.cache.heads * length) {
                 off -= (long long)a.cache.heads * length;
@@ -352,10 +364,12 @@ __device__ __forceinline__ void store_eight(const KvAttnArgs &a, size_t at, cons
     *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.O) + at) = o;
 }
 
-template <int D>
+template <int D, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_constant__ KvAttnArgs a, const __grid_constant__ Schedule sc)
 {
     using L = Layout<D>;
+    using Walk = Walk<WIDE>;
+    using View = typename Walk::View;
     extern __shared__ uint8_t raw_smem[];
     __shared__ Control ctl_store;
     Control *ctl = &ctl_store;
@@ -403,6 +417,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     long long mine = 0;
     for (int b = b_first; b < b_last; ++b) {
         const Seq s = load_seq(a, b, sc.sb);
+        if constexpr (WIDE)
+            if (a.tree && s.n > 32 * a.tree_words) report_failure(sc.sb, W4A8_ERR_BAD_TABLE, b);
         const int tiles = Walk::tiles_of(s, (int)sc.group.d);
         for (int t = 0; t < tiles; t += 32) mine += Walk::tile_places(a, sc, s, t + lane);
     }
@@ -469,11 +485,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             const int count = pc.count;
             if (count < 0) break;
             const Seq s = {pc.row0, pc.n, pc.len};
-            const Sight sight(a, s);
+            const View sight(a, s);
+            const int few = pc.few;
             const int flat = pc.tile * kRows + r, i = sc.group.div(flat);
             const int head = pc.h * (int)sc.group.d + flat - i * (int)sc.group.d;
             const bool in = r < pc.rows;
-            const int row_hi = in ? sight.hi(i) : s.len, row_lo = in ? sight.lo(i) : 0;
+            int row_hi, row_lo;
+            if constexpr (WIDE) row_hi = in ? sight.row_hi(i) : 0, row_lo = in ? sight.row_lo(i) : 0;
+            else row_hi = in ? sight.hi(i) : s.len, row_lo = in ? sight.lo(i) : 0;
             float m = kNoReference, l = 0.0f;
             if (count > 0) {
                 // ---- queries to the operand tile, scaled by a power of two to the top of binary16's range ----
@@ -550,9 +569,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 // rows of this warp's tile: what all of them see
                 const int t_first = sc.group.div(pc.tile * kRows + w * 128);
                 const int t_last = sc.group.div(pc.tile * kRows + max(w * 128, min(pc.rows, w * 128 + 128) - 1));
-                const int hi_min = sight.hi(t_first), lo_max = sight.lo(t_last);
-                int j0 = pc.unit0 * kUnit;
+                int hi_min, lo_max;
+                if constexpr (WIDE) hi_min = sight.all_hi(t_first), lo_max = sight.all_lo(t_last);
+                else hi_min = sight.hi(t_first), lo_max = sight.lo(t_last);
+                int j0 = (WIDE && few > 0 ? pc.few0 : pc.unit0) * kUnit;
                 for (int u = 0; u < count; ++u, ++unit_no, j0 += kUnit) {
+                    if (WIDE && u == few && few > 0) j0 = pc.unit0 * kUnit;
                     const uint32_t slot = unit_no % kConstSlots;
                     // (the scores were issued behind the unit's keys, and those behind its constants)
                     if (!(ok = wait_warp(bar(L::kSFull + 2 * w + (unit_no & 1)), (unit_no >> 1) & 1, ctl, sc.sb, kWaitSite + 2))) break;
@@ -576,7 +598,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                         x[k + 2] = fmaf(x[k + 2], f.z, g.z);
                         x[k + 3] = fmaf(x[k + 3], f.w, g.w);
                     }
-                    if (edge) {
+                    if (WIDE && edge) {
+                        if constexpr (WIDE) {
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                const uint32_t seen = in ? sight.visible(i, row_lo, row_hi, j0 + 32 * half) : 0u;
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) x[32 * half + k] = seen >> k & 1u ? x[32 * half + k] : -INFINITY;
+                            }
+                        }
+                    } else if (edge) {
                         const int lo_off = j0 - row_lo;
                         const uint32_t span = (uint32_t)max(row_hi - row_lo, 0);
 #pragma unroll
@@ -707,7 +738,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             const int32_t *table = a.batch.page_table + (size_t)seq * a.batch.max_pages;
             // Block of this thread's token of unit u of the piece; behind the end the last one.  In front of what the tile
             // sees, in the first unit only, the first one that it sees: the page of the other may be gone.
-            auto block_no = [&](int u) { return min((unit0 + u) * (kUnit / 16) + (tk >> 4), last_block); };
+            // (Extended: in front of the window as behind the sinks.)
+            const int near = WIDE ? WideSight(a, {pc.row0, pc.n, len}).sinks : 0, sink_block = near > 0 ? (near - 1) >> 4 : -1;
+            const int few = pc.few, few0 = pc.few0;
+            auto unit_at = [&](int u) { return !WIDE ? unit0 + u : u < few ? few0 + u : unit0 + u - few; };
+            auto block_no = [&](int u) {
+                int blk = min(unit_at(u) * (kUnit / 16) + (tk >> 4), last_block);
+                if (WIDE && blk > sink_block) blk = max(blk, lo >> 4);
+                return blk;
+            };
             auto page_of = [&](int blk) {
                 int page = __ldca(table + (blk >> page_bits));
                 if ((unsigned)page >= (unsigned)a.cache.num_pages) {
@@ -745,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     } else vc[k][0] = __ldca(reinterpret_cast<const uint32_t *>(q));
                 }
             };
-            const int blk0 = max(block_no(0), lo >> 4);
+            const int blk0 = WIDE ? block_no(0) : max(block_no(0), lo >> 4);
             const uint8_t *block = block_of(blk0, page_of(blk0));
             fetch_keys(block);
             fetch_values(block);
@@ -774,7 +813,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             };
             for (int u = 0; u < count; ++u, ++unit_no) {
                 const uint32_t buf = unit_no % kRing, use = unit_no / kRing & 1, slot = unit_no % kConstSlots;
-                const bool there = (uint32_t)(from_lo + u * kUnit) < seen;       // else its words are anything
+                bool there = (uint32_t)(from_lo + u * kUnit) < seen;             // else its words are anything
+                if constexpr (WIDE) {
+                    const int at = unit_at(u) * kUnit + tk;
+                    there = (at >= lo || at < near) && at < len;
+                }
                 // ---- keys ----
                 if (unit_no >= kRing && !(ok = wait_warp(bar(L::kKEmpty + buf), use ^ 1, ctl, sc.sb, kWaitSite + 5, 200))) break;
                 {
@@ -910,9 +953,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     p.row0 = walk.s.row0;
                     p.n = walk.s.n;
                     p.len = walk.s.len;
-                    p.unit0 = walk.first + walk.from;
+                    p.unit0 = walk.first + (WIDE ? max(walk.from - walk.few, 0) : walk.from);
                     p.count = walk.count;
                     p.lo = walk.lo;
+                    if constexpr (WIDE) {
+                        p.few0 = walk.from;
+                        p.few = max(min(walk.few - walk.from, walk.count), 0);
+                    }
                     p.whole = walk.whole;
                     p.slot = walk.first_unit <= begin ? 0 : 1;
                     if (!walk.whole && walk.first_unit >= begin) {       // begins here and ends in a later share
@@ -991,14 +1038,20 @@ __global__ void __launch_bounds__(D) kv_prefill_join_kernel(const __grid_constan
     if (a.lse && c == 0) a.lse[row] = lsum > 0.0f ? (top + lg2(lsum)) * kLn2 : -INFINITY;
 }
 
+template <int D, bool WIDE>
+cudaError_t launch_instance(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
+{
+    static std::atomic<int> raised[kMaxDevices];
+    cudaError_t e = raise_smem_limit(kv_prefill_kernel<D, WIDE>, Layout<D>::kSmem, raised);
+    if (e == cudaSuccess) e = launch_overlapped(kv_prefill_kernel<D, WIDE>, dim3(ctas), dim3(kThreads), Layout<D>::kSmem, st, a, sc);
+    if (e == cudaSuccess) e = launch_overlapped(kv_prefill_join_kernel<D>, dim3(kRows / 32, ctas), dim3(D), 0, st, a, sc);
+    return e;
+}
+
 template <int D>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
 {
-    static std::atomic<int> raised[kMaxDevices];
-    cudaError_t e = raise_smem_limit(kv_prefill_kernel<D>, Layout<D>::kSmem, raised);
-    if (e == cudaSuccess) e = launch_overlapped(kv_prefill_kernel<D>, dim3(ctas), dim3(kThreads), Layout<D>::kSmem, st, a, sc);
-    if (e == cudaSuccess) e = launch_overlapped(kv_prefill_join_kernel<D>, dim3(kRows / 32, ctas), dim3(D), 0, st, a, sc);
-    return e;
+    return a.extended() ? launch_instance<D, true>(a, sc, ctas, st) : launch_instance<D, false>(a, sc, ctas, st);
 }
 
 }  // namespace
