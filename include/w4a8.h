@@ -507,11 +507,11 @@ w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, con
  *   cu_rows     out [batch + 1] INT32, row offsets.
  *   positions   out [rows] INT32, position of every row, or NULL.
  *   slots       out [rows] INT64, page * page_size + place of every row, or NULL.
- *   rows        size of positions and slots; rows from cu_rows[batch] on get position 0 and slot -1.
+ *   rows        size of positions and slots, at most 2^30; rows from cu_rows[batch] on get position 0 and slot -1.
  * A step whose rows do not fit, whose lengths are out of range or whose free list is damaged (W4A8_ERR_BAD_TABLE), or
  * that needs more pages than are free (W4A8_ERR_NO_PAGES), is refused as a whole: cu_rows are 0, slots -1, kv_lens_out is held,
  * free_count_out is free_count, the table and the list are left alone; the status block reports it.
- * batch <= 16384.  workspace: 512 bytes, zero-filled once; one that the cache calls use will do. */
+ * batch <= 8192.  workspace: 512 bytes, zero-filled once; one that the cache calls use will do. */
 w4a8_status w4a8_kv_plan(const int32_t *held, const int32_t *kv_lens, const int32_t *add, int batch,
                          int32_t *page_table, int max_pages, int page_size, int32_t *free_pages,
                          int num_pages, const int32_t *free_count, int32_t *free_count_out,

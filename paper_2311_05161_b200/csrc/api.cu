@@ -658,7 +658,7 @@ w4a8_status w4a8_kv_plan(const int32_t *held, const int32_t *kv_lens, const int3
 {
     if (!kv_lens || !add || !page_table || !free_pages || !free_count || !free_count_out || !kv_lens_out || !cu_rows || !workspace)
         return W4A8_ERR_NULL;
-    if (batch < 1 || batch > kPlanMaxBatch || max_pages < 1 || num_pages < 1 || rows < 1 || !kv_shape_ok(page_size, 1, 64) ||
+    if (batch < 1 || batch > kPlanMaxBatch || max_pages < 1 || num_pages < 1 || rows < 1 || rows > (1 << 30) || !kv_shape_ok(page_size, 1, 64) ||
         (long long)max_pages * page_size > (1ll << 31) - 1024 || (held && kv_lens_out == kv_lens))
         return W4A8_ERR_SHAPE;
     for (const void *p : {(const void *)held, (const void *)kv_lens, (const void *)add, (const void *)page_table, (const void *)free_pages,
@@ -670,7 +670,7 @@ w4a8_status w4a8_kv_plan(const int32_t *held, const int32_t *kv_lens, const int3
     const w4a8_status arch = check_arch();
     if (arch != W4A8_OK) return arch;
     KvPlanArgs a = {held, kv_lens, add, page_table, free_pages, free_count, free_count_out, kv_lens_out, cu_rows, positions, slots,
-                    batch, max_pages, 0, num_pages, rows};
+                    batch, max_pages, 0, num_pages, rows, false};
     while ((1 << a.page_shift) < page_size) ++a.page_shift;
     const cudaError_t e = launch_kv_plan(a, static_cast<StatusBlock *>(workspace),
                                          reinterpret_cast<int *>(static_cast<uint8_t *>(workspace) + sizeof(StatusBlock)),

@@ -116,7 +116,7 @@ kv_append_kernel(const T *__restrict__ K, const T *__restrict__ V, long long k_s
                 }
                 float r;
                 int z;
-                const uint32_t word = kv_range_word(lo, hi, r, z), codes = kv_code_word(x, r, z);
+                const uint32_t word = kv_range_word(lo, hi, r, z), codes = kv_code_word(x, r, (float)z);
                 if (here) {
                     *reinterpret_cast<uint32_t *>(to + j * head_bytes + code_at) = codes;
                     if (l == 0) *reinterpret_cast<uint32_t *>(to + j * head_bytes + word_at) = word;

@@ -114,9 +114,9 @@ __device__ __forceinline__ uint32_t kv_rank_bits(float x, float r, float top, fl
     const float y = __fadd_rn(fminf(__fmaf_rn(fabsf(u), 0x1.fffffep0f, 12582911.0f), __fadd_rn(fabsf(u), 12582912.0f)), -12582911.0f);
     return __float_as_uint(__fadd_rn(fminf(copysignf(y, u), top), bias));
 }
-__device__ __forceinline__ uint32_t kv_code_word(const float (&x)[8], float r, int z)
+__device__ __forceinline__ uint32_t kv_code_word(const float (&x)[8], float r, float z)
 {
-    const float top = (float)(14 - z), bias = 12582913.0f + (float)z;
+    const float top = 14.0f - z, bias = 12582913.0f + z;
     uint32_t k[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) k[i] = kv_rank_bits(x[i], r, top, bias);
@@ -206,8 +206,9 @@ struct KvPlanArgs {
     int32_t *free_count_out, *kv_lens_out, *cu_rows, *positions;
     int64_t *slots;
     int batch, max_pages, page_shift, num_pages, rows;
+    bool wide_stores;                        // positions and slots take 16-byte stores
 };
-constexpr int kPlanMaxBatch = 16384;
+constexpr int kPlanMaxBatch = 8192;        // 24 bytes each in shared memory
 cudaError_t launch_kv_plan(const KvPlanArgs &a, StatusBlock *sb, int *ticket, cudaStream_t st);
 
 struct KvAttnArgs {

@@ -1,13 +1,13 @@
 // A step's plan on the device: from the requests' lengths the page table, row offsets, positions and slots.
 //
-// Every CTA computes the prefix sums of rows, pages taken and pages given back over the batch (three sums in one scan), so that each
-// can fill its share of the outputs by binary search without waiting for another.  The free list is a stack: what is given back
-// lies on top of it in the order of sequences and pages, and page number a of those taken is the a-th from the top, which
-// every thread finds by itself (on the list, or in the table of the sequence that gives it back).  The lengths and the
-// count may be updated in place, so they are written by the CTA that finishes last, when all others have read them.
+// Every CTA computes the prefix sums of rows, pages taken and pages given back over the batch (three sums in one scan) into
+// its shared memory, so that each can fill its share of the outputs without waiting for another.  The free list is a stack: what
+// is given back lies on top of it in the order of sequences and pages, and page number a of those taken is the a-th from the
+// top, which every thread finds by itself (on the list, or in the table of the sequence that gives it back).  The lengths and the
+// count may be updated in place: a CTA draws a ticket when it has read them, and the one that draws the last writes them.
 //
 // Twelve bytes per row and a few per sequence: the time is a launch, the scan's chain of dependent steps, and for many rows
-// their stores.
+// the search of each row's sequence, which four neighbouring rows share.
 #include "kv_cache.cuh"
 
 namespace w4a8 {
@@ -15,6 +15,8 @@ namespace w4a8 {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kRun = 4;                      // neighbouring rows of a thread
+constexpr int kAtOnce = 4;                   // sequences of a thread whose lengths are loaded together
 
 struct Sums {
     long long rows, taken, back;
@@ -25,6 +27,7 @@ struct Request {
     int held, kept, add;
     int had, has;                            // pages
     bool good;
+    __device__ Sums sums() const { return {good ? add : 0, max(has - had, 0), max(had - has, 0)}; }
 };
 __device__ __forceinline__ Request load_request(const KvPlanArgs &a, int b)
 {
@@ -32,21 +35,30 @@ __device__ __forceinline__ Request load_request(const KvPlanArgs &a, int b)
     q.kept = __ldca(a.kv_lens + b);
     q.held = a.held ? __ldca(a.held + b) : q.kept;
     q.add = __ldca(a.add + b);
+    return q;
+}
+__device__ __forceinline__ void count_pages(const KvPlanArgs &a, Request &q)
+{
     const long long most = (long long)a.max_pages << a.page_shift;
     q.good = q.kept >= 0 && q.add >= 0 && q.held >= q.kept && q.held <= most && (long long)q.kept + q.add <= most;
     const int round = (1 << a.page_shift) - 1;
     q.had = q.good ? (q.held + round) >> a.page_shift : 0;
     q.has = q.good ? (q.kept + q.add + round) >> a.page_shift : 0;
-    return q;
 }
 
-// The last of ends[0 .. n] (ascending from 0) that is <= x: the sequence with element x.
-__device__ __forceinline__ int owner(const int *ends, int n, int x)
+// What the outputs need to know of a sequence.
+struct __align__(16) Entry {
+    int row, kept, taken, had;               // first row, tokens, first page taken, pages before
+};
+
+// The last sequence whose number is <= x, where numbers ascend and the first is 0: the owner of element x.
+template <class F>
+__device__ __forceinline__ int owner(int batch, int x, F number)
 {
-    int lo = 0, hi = n - 1;
+    int lo = 0, hi = batch - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (ends[mid] <= x) lo = mid;
+        if (number(mid) <= x) lo = mid;
         else hi = mid - 1;
     }
     return lo;
@@ -54,22 +66,39 @@ __device__ __forceinline__ int owner(const int *ends, int n, int x)
 
 __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, StatusBlock *sb, int *ticket)
 {
-    extern __shared__ int first[];           // [3][batch]: first row, first page taken, first page given back
+    extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Sums warp_sums[kWarps];
     __shared__ int last;
     allow_dependents();
     dependent_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, batch = a.batch;
-    int *first_row = first, *first_taken = first + batch, *first_back = first + 2 * batch;
+    Entry *entry = reinterpret_cast<Entry *>(smem);                        // [batch]
+    int *first_back = reinterpret_cast<int *>(smem + sizeof(Entry) * batch);   // [batch]: first page given back; pages afterwards
+    int *pages_left = first_back + batch;
     const int chunk = (batch + kThreads - 1) / kThreads;
     const int b0 = min(batch, tid * chunk), b1 = min(batch, b0 + chunk);
+    const int count = __ldca(a.free_count);
     Sums mine = {0, 0, 0};
     bool bad = false;
-    for (int b = b0; b < b1; ++b) {
-        const Request q = load_request(a, b);
-        bad |= !q.good;
-        if (!q.good) report_failure(sb, W4A8_ERR_BAD_TABLE, b);
-        mine = plus(mine, {q.good ? q.add : 0, max(q.has - q.had, 0), max(q.had - q.has, 0)});
+    for (int b = b0; b < b1; b += kAtOnce) {
+        Request q[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            if (b + k < b1) q[k] = load_request(a, b + k);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            if (b + k >= b1) break;
+            count_pages(a, q[k]);
+            if (!q[k].good) {
+                bad = true;
+                report_failure(sb, W4A8_ERR_BAD_TABLE, b + k);
+            }
+            // (sums of this thread's sequences so far; what lies before them is added below)
+            entry[b + k] = {(int)mine.rows, q[k].kept, (int)mine.taken, q[k].had};
+            first_back[b + k] = (int)mine.back;
+            pages_left[b + k] = q[k].has;
+            mine = plus(mine, q[k].sums());
+        }
     }
     Sums upto = mine;
 #pragma unroll
@@ -79,12 +108,15 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, S
         if (lane >= o) upto = plus(upto, v);
     }
     if (lane == 31) warp_sums[warp] = upto;
-    const int count = __ldca(a.free_count);
-    bad = __syncthreads_or(bad);
-    Sums total = {0, 0, 0};
+    bad = __syncthreads_or(bad);             // also: this CTA has read the lengths and the count
+    int tickets = 0;                         // drawn before this CTA's
+    if (tid == 0 && gridDim.x > 1) asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(tickets) : "l"(ticket) : "memory");
+    Sums total = {0, 0, 0}, before = {upto.rows - mine.rows, upto.taken - mine.taken, upto.back - mine.back};
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) upto = plus(upto, warp_sums[w]);
-        total = plus(total, warp_sums[w]);
+        const Sums v = warp_sums[w];
+        if (w < warp) before = plus(before, v);
+        total = plus(total, v);
     }
     // ---- all or nothing ----
     if (!bad && (total.rows > a.rows || count < 0 || count > a.num_pages || count + total.back > a.num_pages)) {
@@ -97,21 +129,18 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, S
     }
     const int n_rows = bad ? 0 : (int)total.rows, n_taken = bad ? 0 : (int)total.taken, n_back = bad ? 0 : (int)total.back;
     const int top = count + n_back;          // of the stack with what is given back
-    Sums at = {upto.rows - mine.rows, upto.taken - mine.taken, upto.back - mine.back};
     for (int b = b0; b < b1; ++b) {
-        first_row[b] = bad ? 0 : (int)at.rows;
-        first_taken[b] = bad ? 0 : (int)at.taken;
-        first_back[b] = bad ? 0 : (int)at.back;
-        if (blockIdx.x == 0) a.cu_rows[b] = first_row[b];
-        const Request q = load_request(a, b);
-        at = plus(at, {q.add, max(q.has - q.had, 0), max(q.had - q.has, 0)});
+        entry[b].row += (int)before.rows;
+        entry[b].taken += (int)before.taken;
+        first_back[b] += (int)before.back;
+        if (blockIdx.x == 0) a.cu_rows[b] = bad ? 0 : entry[b].row;
     }
     if (blockIdx.x == 0 && tid == 0) a.cu_rows[batch] = n_rows;
     __syncthreads();
     // page of place f among those given back, and of place k from the top of the stack
     auto given_back = [&](int f) {
-        const int b = owner(first_back, batch, f);
-        return __ldca(a.page_table + (size_t)b * a.max_pages + load_request(a, b).has + f - first_back[b]);
+        const int b = owner(batch, f, [&](int i) { return first_back[i]; });
+        return __ldca(a.page_table + (size_t)b * a.max_pages + pages_left[b] + f - first_back[b]);
     };
     auto taken = [&](int k) {
         const int v = top - 1 - k;
@@ -120,35 +149,54 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, S
         return page;
     };
     const int thread = blockIdx.x * kThreads + tid, threads = gridDim.x * kThreads;
-    for (int k = thread; k < n_taken; k += threads) {
-        const int b = owner(first_taken, batch, k);
-        a.page_table[(size_t)b * a.max_pages + load_request(a, b).had + k - first_taken[b]] = taken(k);
+    // (pages from the last thread on, rows from the first)
+    for (int k = threads - 1 - thread; k < n_taken; k += threads) {
+        const int b = owner(batch, k, [&](int i) { return entry[i].taken; });
+        a.page_table[(size_t)b * a.max_pages + entry[b].had + k - entry[b].taken] = taken(k);
     }
-    for (int f = thread; f < n_back - n_taken; f += threads) a.free_pages[count + f] = given_back(f);
-    if (a.positions || a.slots) {
-        for (int r = thread; r < a.rows; r += threads) {
-            int pos = 0;
-            long long slot = -1;
-            if (r < n_rows) {
-                const int b = owner(first_row, batch, r);
-                const Request q = load_request(a, b);
-                pos = q.kept + r - first_row[b];
-                const int i = pos >> a.page_shift;
-                const int page = i < q.had ? __ldca(a.page_table + (size_t)b * a.max_pages + i) : taken(first_taken[b] + i - q.had);
-                if ((unsigned)page < (unsigned)a.num_pages) slot = ((long long)page << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
-                else report_failure(sb, W4A8_ERR_BAD_TABLE, b);
+    for (int f = threads - 1 - thread; f < n_back - n_taken; f += threads) a.free_pages[count + f] = given_back(f);
+    for (int r0 = thread * kRun; r0 < a.rows && (a.positions || a.slots); r0 += threads * kRun) {
+        int pos[kRun];
+        long long slot[kRun];
+        int b = r0 < n_rows ? owner(batch, r0, [&](int i) { return entry[i].row; }) : batch;
+        int at = -1, page = 0;               // the page looked up last
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+            pos[k] = 0;
+            slot[k] = -1;
+            if (r0 + k >= n_rows) continue;
+            while (b + 1 < batch && entry[b + 1].row <= r0 + k) {
+                ++b;
+                at = -1;
             }
-            if (a.positions) a.positions[r] = pos;
-            if (a.slots) a.slots[r] = slot;
+            const Entry e = entry[b];
+            pos[k] = e.kept + r0 + k - e.row;
+            const int i = pos[k] >> a.page_shift;
+            if (i != at) {
+                at = i;
+                page = i < e.had ? __ldca(a.page_table + (size_t)b * a.max_pages + i) : taken(e.taken + i - e.had);
+                if ((unsigned)page >= (unsigned)a.num_pages) report_failure(sb, W4A8_ERR_BAD_TABLE, b);
+            }
+            if ((unsigned)page < (unsigned)a.num_pages) slot[k] = ((long long)page << a.page_shift) + (pos[k] & ((1 << a.page_shift) - 1));
+        }
+        if (r0 + kRun <= a.rows && a.wide_stores) {
+            if (a.positions) *reinterpret_cast<int4 *>(a.positions + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+            if (a.slots) {
+                longlong2 *to = reinterpret_cast<longlong2 *>(a.slots + r0);
+                to[0] = make_longlong2(slot[0], slot[1]);
+                to[1] = make_longlong2(slot[2], slot[3]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                if (r0 + k >= a.rows) break;
+                if (a.positions) a.positions[r0 + k] = pos[k];
+                if (a.slots) a.slots[r0 + k] = slot[k];
+            }
         }
     }
-    // ---- lengths and count, when every CTA has read them ----
-    __syncthreads();
-    if (tid == 0) {
-        int before;
-        asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(ticket) : "memory");
-        last = before == (int)gridDim.x - 1;
-    }
+    // ---- lengths and count, by the CTA with the last ticket ----
+    if (tid == 0) last = tickets == (int)gridDim.x - 1;
     __syncthreads();
     if (!last) return;
     for (int b = tid; b < batch; b += kThreads) {
@@ -156,22 +204,25 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, S
         a.kv_lens_out[b] = bad ? q.held : q.kept + q.add;
     }
     if (tid == 0) {
-        *a.free_count_out = bad ? count : top - n_taken;
+        *a.free_count_out = top - n_taken;
         *ticket = 0;                         // ready for the next call
     }
 }
 
 }  // namespace
 
-cudaError_t launch_kv_plan(const KvPlanArgs &a, StatusBlock *sb, int *ticket, cudaStream_t st)
+cudaError_t launch_kv_plan(const KvPlanArgs &args, StatusBlock *sb, int *ticket, cudaStream_t st)
 {
-    const int smem = 3 * (int)sizeof(int) * a.batch;
+    KvPlanArgs a = args;
+    a.wide_stores = reinterpret_cast<uintptr_t>(a.positions) % 16 == 0 && reinterpret_cast<uintptr_t>(a.slots) % 16 == 0;
+    const int smem = (int)(sizeof(Entry) + 2 * sizeof(int)) * a.batch;
     static std::atomic<int> raised[kMaxDevices];
     const cudaError_t e = raise_smem_limit(kv_plan_kernel, smem, raised);
     if (e != cudaSuccess) return e;
-    const int work = a.rows > a.batch ? a.rows : a.batch, sms = device_sms();
-    const int ctas = (work + 4 * kThreads - 1) / (4 * kThreads);
-    return launch_overlapped(kv_plan_kernel, dim3(ctas < sms ? ctas : sms), dim3(kThreads), smem, st, a, sb, ticket);
+    // a thread for every run of rows, and for every page that so many rows of so many sequences may need
+    const long long threads = (a.rows + kRun - 1) / kRun + ((a.rows >> a.page_shift) + (a.batch > kThreads ? a.batch : 0));
+    const long long ctas = (threads + kThreads - 1) / kThreads, sms = device_sms();
+    return launch_overlapped(kv_plan_kernel, dim3((unsigned)(ctas < sms ? ctas : sms)), dim3(kThreads), smem, st, a, sb, ticket);
 }
 
 }  // namespace w4a8

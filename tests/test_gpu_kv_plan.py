@@ -106,7 +106,7 @@ def test_many_rows(P):
 
 
 def test_the_largest_batch():
-    c = Case(requests(16384, 3, 3, KINDS), 16)
+    c = Case(requests(8192, 3, 3, KINDS), 16)
     c.check(c.run(in_place=True))
 
 

@@ -34,7 +34,7 @@ def test_plan_refusals(w4a8):
     f = w4a8.lib.w4a8_kv_plan
     for k in ("lens", "add", "table", "free", "count", "left", "out", "cu", "ws"):
         assert f(*plan_args(**{k: None})) == 1, k
-    for kw in (dict(batch=0), dict(batch=16385), dict(mp=0), dict(mp=1 << 25), dict(P=8), dict(P=48), dict(P=2048), dict(pages=0), dict(rows=0), dict(rows=-1),
+    for kw in (dict(batch=0), dict(batch=8193), dict(mp=0), dict(mp=1 << 25), dict(P=8), dict(P=48), dict(P=2048), dict(pages=0), dict(rows=0), dict(rows=-1),
                dict(out=P(GOOD))):
         assert f(*plan_args(**kw)) == 2, kw
     for k in ("held", "lens", "add", "table", "free", "count", "left", "out", "cu", "pos"):
