@@ -166,16 +166,18 @@ def test_trees_with_a_window(rows, window, few):
     tree([300, 45, 130], rows, 16, 4, 2, 64, masks, window=window, few=few, drop=False)
 
 
-def test_a_chain_is_causal_attention():
-    """The same bits, where both forms walk the same units (one tile of rows per sequence in the many-row form)."""
-    for c in (5, 64):
-        bt = Batch([200, c], [c, c], 16)
-        cache = filled_cache(bt, 2, 128)
-        Q = torch.randn(bt.rows, 8, 128, dtype=F16, device="cuda")
-        ws = w4a8.new_kv_workspace(bt.rows, 2, 8, 2, 128)
-        bits = mask_words([(2 << i) - 1 for i in range(c)] * 2, 3).cuda()
-        want = w4a8.kv_attention(Q, cache, bt.table, bt.kv_lens, 2, ws, cu_rows=bt.cu)
-        assert torch.equal(w4a8.kv_attention_tree(Q, cache, bt.table, bt.kv_lens, 2, ws, bits, cu_rows=bt.cu), want)
+@pytest.mark.parametrize("window,few", [(0, 0), (33, 4)])
+def test_a_chain_sees_what_causal_rows_see(window, few):
+    """(Within a window, a drafted row sees all of its own path: the chain is shorter than the window.)  The two calls share their work
+    differently, so each is held to binary64."""
+    for c in (5, 33, 64):
+        if window and c > window:
+            continue
+        masks = [(2 << i) - 1 for i in range(c)] * 2
+        for n in (200, c):
+            for i in range(c):
+                assert seen_in_tree(n, c, i, masks[i], window, few) == seen_with_sinks(n, c, i, True, window, few)
+        tree([200, c], [c, c], 16, 8, 2, 128, masks, window=window, few=few)
 
 
 def test_too_many_rows_for_the_mask_are_reported():
