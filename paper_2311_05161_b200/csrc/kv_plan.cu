@@ -14,7 +14,6 @@ namespace w4a8 {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kRun = 4;                      // neighbouring rows of a thread
 constexpr int kAtOnce = 4;                   // sequences of a thread whose lengths are loaded together
 
@@ -64,10 +63,12 @@ __device__ __forceinline__ int owner(int batch, int x, F number)
     return lo;
 }
 
-__global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, StatusBlock *sb, int *ticket)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) kv_plan_kernel(const KvPlanArgs a, StatusBlock *sb, int *ticket)
 {
+    constexpr int WARPS = THREADS / 32;
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ Sums warp_sums[kWarps];
+    __shared__ Sums warp_sums[WARPS];
     __shared__ int last;
     allow_dependents();
     dependent_wait();
@@ -75,7 +76,7 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, S
     Entry *entry = reinterpret_cast<Entry *>(smem);                        // [batch]
     int *first_back = reinterpret_cast<int *>(smem + sizeof(Entry) * batch);   // [batch]: first page given back; pages afterwards
     int *pages_left = first_back + batch;
-    const int chunk = (batch + kThreads - 1) / kThreads;
+    const int chunk = (batch + THREADS - 1) / THREADS;
     const int b0 = min(batch, tid * chunk), b1 = min(batch, b0 + chunk);
     const int count = __ldca(a.free_count);
     Sums mine = {0, 0, 0};
@@ -113,7 +114,7 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, S
     if (tid == 0 && gridDim.x > 1) asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(tickets) : "l"(ticket) : "memory");
     Sums total = {0, 0, 0}, before = {upto.rows - mine.rows, upto.taken - mine.taken, upto.back - mine.back};
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
         const Sums v = warp_sums[w];
         if (w < warp) before = plus(before, v);
         total = plus(total, v);
@@ -140,7 +141,9 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, S
     // page of place f among those given back, and of place k from the top of the stack
     auto given_back = [&](int f) {
         const int b = owner(batch, f, [&](int i) { return first_back[i]; });
-        return __ldca(a.page_table + (size_t)b * a.max_pages + pages_left[b] + f - first_back[b]);
+        const int page = __ldca(a.page_table + (size_t)b * a.max_pages + pages_left[b] + f - first_back[b]);
+        if ((unsigned)page >= (unsigned)a.num_pages) report_failure(sb, W4A8_ERR_BAD_TABLE, b);
+        return page;
     };
     auto taken = [&](int k) {
         const int v = top - 1 - k;
@@ -148,7 +151,7 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, S
         if ((unsigned)page >= (unsigned)a.num_pages) report_failure(sb, W4A8_ERR_BAD_TABLE, -2);
         return page;
     };
-    const int thread = blockIdx.x * kThreads + tid, threads = gridDim.x * kThreads;
+    const int thread = blockIdx.x * THREADS + tid, threads = gridDim.x * THREADS;
     // (pages from the last thread on, rows from the first)
     for (int k = threads - 1 - thread; k < n_taken; k += threads) {
         const int b = owner(batch, k, [&](int i) { return entry[i].taken; });
@@ -199,7 +202,7 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, S
     if (tid == 0) last = tickets == (int)gridDim.x - 1;
     __syncthreads();
     if (!last) return;
-    for (int b = tid; b < batch; b += kThreads) {
+    for (int b = tid; b < batch; b += THREADS) {
         const Request q = load_request(a, b);
         a.kv_lens_out[b] = bad ? q.held : q.kept + q.add;
     }
@@ -209,20 +212,27 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(const KvPlanArgs a, S
     }
 }
 
+template <int THREADS>
+cudaError_t launch(const KvPlanArgs &a, StatusBlock *sb, int *ticket, cudaStream_t st)
+{
+    const int smem = (int)(sizeof(Entry) + 2 * sizeof(int)) * a.batch;
+    static std::atomic<int> raised[kMaxDevices];
+    const cudaError_t e = raise_smem_limit(kv_plan_kernel<THREADS>, smem, raised);
+    if (e != cudaSuccess) return e;
+    // a thread for every run of rows, and for every page that so many rows of so many sequences may need
+    const long long threads = (a.rows + kRun - 1) / kRun + (a.rows >> a.page_shift) + (a.batch > THREADS ? a.batch : 0);
+    const long long ctas = (threads + THREADS - 1) / THREADS, sms = device_sms();
+    return launch_overlapped(kv_plan_kernel<THREADS>, dim3((unsigned)(ctas < sms ? ctas : sms)), dim3(THREADS), smem, st, a, sb, ticket);
+}
+
 }  // namespace
 
 cudaError_t launch_kv_plan(const KvPlanArgs &args, StatusBlock *sb, int *ticket, cudaStream_t st)
 {
     KvPlanArgs a = args;
     a.wide_stores = reinterpret_cast<uintptr_t>(a.positions) % 16 == 0 && reinterpret_cast<uintptr_t>(a.slots) % 16 == 0;
-    const int smem = (int)(sizeof(Entry) + 2 * sizeof(int)) * a.batch;
-    static std::atomic<int> raised[kMaxDevices];
-    const cudaError_t e = raise_smem_limit(kv_plan_kernel, smem, raised);
-    if (e != cudaSuccess) return e;
-    // a thread for every run of rows, and for every page that so many rows of so many sequences may need
-    const long long threads = (a.rows + kRun - 1) / kRun + ((a.rows >> a.page_shift) + (a.batch > kThreads ? a.batch : 0));
-    const long long ctas = (threads + kThreads - 1) / kThreads, sms = device_sms();
-    return launch_overlapped(kv_plan_kernel, dim3((unsigned)(ctas < sms ? ctas : sms)), dim3(kThreads), smem, st, a, sb, ticket);
+    // a decode step fits one small CTA, whose barriers and sums are short
+    return a.batch <= 128 && a.rows <= 128 * kRun ? launch<128>(a, sb, ticket, st) : launch<512>(a, sb, ticket, st);
 }
 
 }  // namespace w4a8
