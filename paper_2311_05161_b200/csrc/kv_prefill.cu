@@ -989,48 +989,70 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
 
 // Joins the parts of the items that several CTAs shared, in list order.  A kernel of its own spreads this over
 // the GPU: left to the CTA that finishes an item last, the parts (131 KB each) pass through one SM, some 1.2 us
-// per part.  Block (x, y): rows 32 x .. 32 x + 31 of the item that begins in share y; a warp takes 32 columns.
+// per part.  Block (x, y): rows 32 x .. 32 x + 31 of the item that begins in share y; a warp takes 16 columns.
+constexpr int kJoinColumns = 16;
 template <int D>
-__global__ void __launch_bounds__(D) kv_prefill_join_kernel(const __grid_constant__ KvAttnArgs a, const __grid_constant__ Schedule sc)
+__global__ void __launch_bounds__(2 * D) kv_prefill_join_kernel(const __grid_constant__ KvAttnArgs a, const __grid_constant__ Schedule sc)
 {
     allow_dependents();
     dependent_wait();
     const Shared item = sc.shared[blockIdx.y];
-    const int lane = threadIdx.x & 31, c = threadIdx.x & ~31, r = blockIdx.x * 32 + lane;
+    const int lane = threadIdx.x & 31, c = threadIdx.x / 32 * kJoinColumns, r = blockIdx.x * 32 + lane;
     if (item.parts == 0 || r >= item.rows) return;
     constexpr size_t kPart = kRows * (D + 2);
+    constexpr int kQuads = kJoinColumns / 4;
     const float *rest = sc.partials + (size_t)blockIdx.y * 2 * kPart, *first = rest + (item.inside ? kPart : 0);
     auto part = [&](int k) { return k == 0 ? first : rest + (size_t)k * 2 * kPart; };
-    float top = kNoReference, most = 0.0f;
+    struct Slice {
+        float m, l;
+        float4 y[kQuads];
+    };
+    auto load = [&](int k, Slice &x) {
+        const float *from = part(k);
+        x.m = __ldcg(from + r);
+        x.l = __ldcg(from + kRows + r);
+        const float4 *at = reinterpret_cast<const float4 *>(from + 2 * kRows) + (blockIdx.x * (D / 4) + c / 4) * 32 + lane;
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) x.y[q] = __ldcg(at + q * 32);
+    };
+    // (an item has two parts as a rule: both are loaded before anything is computed)
+    Slice x0, x1;
+    load(0, x0);
+    if (item.parts > 1) load(1, x1);
+    else x1.m = kNoReference, x1.l = 0.0f;
+    float top = fmaxf(x0.m, x1.m), most = fmaxf(fmaxf(x0.l, x1.l), 0.0f);
 #pragma unroll 4
-    for (int k = 0; k < item.parts; ++k) {
+    for (int k = 2; k < item.parts; ++k) {
         top = fmaxf(top, __ldcg(part(k) + r));
         most = fmaxf(most, __ldcg(part(k) + kRows + r));
     }
     if (most > kFull) top += kLift;            // the sums below fit whatever the parts hold
-    float acc[32], lsum = 0.0f;
+    float acc[kJoinColumns], lsum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) acc[k] = 0.0f;
-#pragma unroll 2
-    for (int k = 0; k < item.parts; ++k) {
-        const float *x = part(k);
-        const float f = ex2(__ldcg(x + r) - top);
-        lsum = fmaf(__ldcg(x + kRows + r), f, lsum);
-        const float4 *from = reinterpret_cast<const float4 *>(x + 2 * kRows) + (blockIdx.x * (D / 4) + c / 4) * 32 + lane;
+    for (int k = 0; k < kJoinColumns; ++k) acc[k] = 0.0f;
+    auto add = [&](const Slice &x) {
+        const float f = ex2(x.m - top);
+        lsum = fmaf(x.l, f, lsum);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const float4 y = __ldcg(from + q * 32);
-            acc[4 * q] = fmaf(y.x, f, acc[4 * q]);
-            acc[4 * q + 1] = fmaf(y.y, f, acc[4 * q + 1]);
-            acc[4 * q + 2] = fmaf(y.z, f, acc[4 * q + 2]);
-            acc[4 * q + 3] = fmaf(y.w, f, acc[4 * q + 3]);
+        for (int q = 0; q < kQuads; ++q) {
+            acc[4 * q] = fmaf(x.y[q].x, f, acc[4 * q]);
+            acc[4 * q + 1] = fmaf(x.y[q].y, f, acc[4 * q + 1]);
+            acc[4 * q + 2] = fmaf(x.y[q].z, f, acc[4 * q + 2]);
+            acc[4 * q + 3] = fmaf(x.y[q].w, f, acc[4 * q + 3]);
         }
+    };
+    add(x0);
+    if (item.parts > 1) add(x1);
+#pragma unroll 2
+    for (int k = 2; k < item.parts; ++k) {
+        load(k, x0);
+        add(x0);
     }
     const float inv = lsum > 0.0f ? __fdiv_rn(-2.0f, lsum) : 0.0f;
     const int flat = item.tile * kRows + r, i = sc.group.div(flat);
     const size_t row = (size_t)(item.row0 + i) * a.q_heads + item.h * (int)sc.group.d + flat - i * (int)sc.group.d;
 #pragma unroll
-    for (int k = 0; k < 32; k += 8) {
+    for (int k = 0; k < kJoinColumns; k += 8) {
         const float y[8] = {acc[k] * inv, acc[k + 2] * inv, acc[k + 4] * inv, acc[k + 6] * inv,
                             acc[k + 1] * inv, acc[k + 3] * inv, acc[k + 5] * inv, acc[k + 7] * inv};
         store_eight(a, row * D + c + k, y);
@@ -1044,7 +1066,7 @@ cudaError_t launch_instance(const KvAttnArgs &a, const Schedule &sc, int ctas, c
     static std::atomic<int> raised[kMaxDevices];
     cudaError_t e = raise_smem_limit(kv_prefill_kernel<D, WIDE>, Layout<D>::kSmem, raised);
     if (e == cudaSuccess) e = launch_overlapped(kv_prefill_kernel<D, WIDE>, dim3(ctas), dim3(kThreads), Layout<D>::kSmem, st, a, sc);
-    if (e == cudaSuccess) e = launch_overlapped(kv_prefill_join_kernel<D>, dim3(kRows / 32, ctas), dim3(D), 0, st, a, sc);
+    if (e == cudaSuccess) e = launch_overlapped(kv_prefill_join_kernel<D>, dim3(kRows / 32, ctas), dim3(2 * D), 0, st, a, sc);
     return e;
 }
 
