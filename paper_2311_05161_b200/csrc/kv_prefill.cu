@@ -28,9 +28,17 @@
 // pipe 28 %, issue slots 56 % busy; 4 prompts of 2048: 285 us.  From runs of several lengths (items of 256 rows, one or
 // more per CTA): 1.47 us per unit (2890 cycles at 1965 MHz; D = 64: 1.34 us), 17 us for the launch and a CTA's first
 // piece, 10 to 13 us for each further piece.  A unit's time is the softmax's chain of wait, load, maximum, exponentials and
-// store.  A piece's is what does not overlap between pieces: queries, first keys, output or parts.  The chunk is 49 units
+// store.  A piece's is what does not overlap between pieces: queries (4 us to their common maximum, 1.5 us to the operand
+// tile), first keys, output or parts (2.7 us).  The chunk is 49 units
 // and 1.9 pieces per CTA, the prompts 114 units and 7.9 pieces: a quarter and two fifths of the time lie
 // outside the units.  (Sixteen softmax warps, two threads per row, were slower for their exchange of maxima: 120 us.)
+// Leaving out exponentials, token constants, expansion and moved references all together takes 13 us off the chunk, three of four
+// MMAs 8 us: no pipe is a unit's time, the hand-overs are.
+//
+// The extended form (WIDE) takes its units from the sinks and then from the window, and masks a unit that some row does not
+// see whole by 64 bits per row, made from bounds and the row's tree mask.  A chunk of 1024 rows at 9000, window 4096, 4 sinks: 126.5 us
+// (120.9 without the sinks in the plain form); 16 trees of 40 to 64 nodes, 32 / 8 heads, 1000 to 6000 tokens: 124.0 us (causal
+// rows in the plain form 122.5).
 #include <type_traits>
 
 #include "kv_attention.cuh"

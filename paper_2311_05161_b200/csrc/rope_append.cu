@@ -14,6 +14,12 @@
 // rotation further on, so that no element changes lanes), else eight consecutive elements.  The four vectors of a unit are
 // quantized together: their ranges are reduced side by side, so that a lane is left with one vector's and the two
 // divisions of a step are done once for four.
+//
+// Four prompts (10348 rows, 32 query and 8 key heads of 128, 223 MB): 48.6 us, 4.6 TB/s, 0.70 of the copy rate; issue slots 64 %
+// busy, and the same walk without sines, quantizer and cache stores still takes 45 us.  Measured and left: a row's vectors
+// split over CTAs, with a lane's partner elements by shuffles 53.9 us; rows in CTAs with barriers 54.7; asynchronous copies into
+// shared memory instead of registers 52.4; packed binary32 products 52.7; 5 or 6 CTAs per SM (fewer registers) 50.6 and
+// 53.5; stores that stay in L2 54.0.  Eight rows: 3.2 us, a launch and the chain of slot, position, sine, range and code.
 #include <type_traits>
 
 #include "kv_cache.cuh"
