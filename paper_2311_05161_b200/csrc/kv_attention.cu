@@ -199,29 +199,41 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     }
     __syncthreads();
     int b = found_b;
-    long long off = found_off;             // units of sequence b in front of this CTA's next one
+    Part s = load_part<R, WIDE>(a, b, group, sc.sb);
+    // place in the sequence: key head, row tile, place in the item
+    int h, tile, at;
+    {
+        const int length = s.item_length(sc.lead), item = (int)quotient(found_off, length);
+        at = (int)(found_off - (long long)item * length);
+        h = s.tiles == 1 ? item : (int)quotient(item, s.tiles);
+        tile = item - h * s.tiles;
+    }
     int stage = 0;
     uint32_t parity = 0;
     bool dead = false;                     // a copy did not arrive in time: nothing more is requested
 
     for (long long u = begin; u < end;) {
-        const Part s = load_part<R, WIDE>(a, b, group, sc.sb);
-        const long long all = s.list_length(heads, sc.lead);
-        if (off >= all) {
-            off -= all;
-            ++b;
-            continue;
-        }
         const int length = s.item_length(sc.lead), item_units = length - sc.lead;
-        const int item = (int)quotient(off, length), at = (int)(off - (long long)item * length);
-        const int h = (int)quotient(item, s.tiles), tile = item - h * s.tiles;
         // this CTA's units [in_item, in_item + count) of the item
         const int here = (int)min((long long)(length - at), end - u);
         const int in_item = max(at - sc.lead, 0), count = max(at + here - sc.lead, 0) - in_item;
         const long long first_unit = u - at + sc.lead;       // the item's units on the list
         u += here;
-        off += here;
-        if (count <= 0) continue;          // its share ends inside the item's lead
+        auto advance = [&] {               // to the next item (only the last one of a share ends in the middle)
+            at = 0;
+            if (++tile < s.tiles) return;
+            tile = 0;
+            if (++h < heads) return;
+            h = 0;
+            while (u < end) {
+                s = load_part<R, WIDE>(a, ++b, group, sc.sb);
+                if (s.n > 0) return;
+            }
+        };
+        if (count <= 0) {                  // its share ends inside the item's lead
+            advance();
+            continue;
+        }
         const bool whole = count == item_units;
 
         // rows of this tile: r = tile * R + i is row r / group of the sequence, query head r % group
@@ -739,6 +751,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         // the join buffer was written by ordinary stores: order them before the next copies into the ring
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
+        advance();
     }
 }
 
