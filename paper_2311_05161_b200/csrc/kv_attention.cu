@@ -40,8 +40,6 @@
 // cost what they cost without it, but for a few registers.  64 sequences, window 2047 and 5 sinks, 8 query heads per key head, 139 MB:
 // 53.8 us (52.0 without the sinks in the plain form); 12 trees of 3 to 13 nodes, 32 heads of their own, 97 MB: 56.9 us (causal rows in
 // the plain form 55.2); one sequence of 100001 tokens, window 4096: 12.2 us; a tree of 7 nodes at 2049 tokens: 14.2 us.
-#include <type_traits>
-
 #include "kv_attention.cuh"
 
 namespace w4a8 {
@@ -100,7 +98,7 @@ struct Part : Seq {
     }
 };
 
-template <int R, bool WIDE>
+template <int R, int FORM>
 __device__ __forceinline__ Part load_part(const KvAttnArgs &a, int b, int group, StatusBlock *sb)
 {
     Part s;
@@ -108,10 +106,10 @@ __device__ __forceinline__ Part load_part(const KvAttnArgs &a, int b, int group,
     s.first = Sight(a, s).lo(0) >> 5;
     s.units = max(0, ((s.len + 31) >> 5) - s.first);
     s.few = 0;
-    if constexpr (WIDE) {
-        s.few = sink_units(WideSight(a, s).sinks, s.first, 5);
+    if constexpr (FORM != kPlain) {
+        s.few = sink_units(View<FORM>(a, s).sinks, s.first, 5);
         s.units += s.few;
-        if (a.tree && s.n > 32 * a.tree_words) report_failure(sb, W4A8_ERR_BAD_TABLE, b);
+        if (FORM == kTree && s.n > 32 * a.tree_words) report_failure(sb, W4A8_ERR_BAD_TABLE, b);
     }
     s.tiles = (int)(((long long)s.n * group + R - 1) / R);
     return s;
@@ -138,11 +136,12 @@ struct Shape {
     static_assert(kCtas * (kSmem + 5 * 1024) <= 232448, "shared memory of an SM");
 };
 
-template <int D, int NT, int WARPS, bool WIDE>
+template <int D, int NT, int WARPS, int FORM>
 __global__ void __launch_bounds__(WARPS * 32, Shape<D, NT, WARPS>::kCtas)
 kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
 {
     using S = Shape<D, NT, WARPS>;
+    constexpr bool WIDE = FORM != kPlain;                  // sinks or a tree
     constexpr int R = S::R, KW = D / 32, KT = D / 16, BB = S::kBlockBytes, UB = S::kUnitBytes, THREADS = WARPS * 32, LPV = D / 8;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long warp_units[WARPS], found_off;
@@ -167,7 +166,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     const int chunk = (bt.batch + THREADS - 1) / THREADS;
     const int b_first = min(bt.batch, tid * chunk), b_last = min(bt.batch, b_first + chunk);
     long long mine = 0;
-    for (int b = b_first; b < b_last; ++b) mine += load_part<R, WIDE>(a, b, group, sc.sb).list_length(heads, sc.lead);
+    for (int b = b_first; b < b_last; ++b) mine += load_part<R, FORM>(a, b, group, sc.sb).list_length(heads, sc.lead);
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -188,7 +187,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     if (begin >= incl - mine && begin < incl) {
         long long at = incl - mine;
         for (int b = b_first; b < b_last; ++b) {
-            const long long u = load_part<R, WIDE>(a, b, group, sc.sb).list_length(heads, sc.lead);
+            const long long u = load_part<R, FORM>(a, b, group, sc.sb).list_length(heads, sc.lead);
             if (begin < at + u) {
                 found_b = b;
                 found_off = begin - at;
@@ -199,7 +198,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
     }
     __syncthreads();
     int b = found_b;
-    Part s = load_part<R, WIDE>(a, b, group, sc.sb);
+    Part s = load_part<R, FORM>(a, b, group, sc.sb);
     // place in the sequence: key head, row tile, place in the item
     int h, tile, at;
     {
@@ -226,7 +225,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
             if (++h < heads) return;
             h = 0;
             while (u < end) {
-                s = load_part<R, WIDE>(a, ++b, group, sc.sb);
+                s = load_part<R, FORM>(a, ++b, group, sc.sb);
                 if (s.n > 0) return;
             }
         };
@@ -239,8 +238,7 @@ kv_decode_kernel(const KvAttnArgs a, const Schedule sc)
         // rows of this tile: r = tile * R + i is row r / group of the sequence, query head r % group
         const int rows_here = (int)min((long long)R, (long long)s.n * group - (long long)tile * R);
         const int i_first = sc.group.div(tile * R), i_last = sc.group.div(tile * R + rows_here - 1);
-        using View = std::conditional_t<WIDE, WideSight, Sight>;
-        const View sight(a, s);
+        const View<FORM> sight(a, s);
         int hi_max, hi_min, lo_min, lo_max;
         if constexpr (WIDE) {
             hi_max = sight.tile_hi(i_last), hi_min = sight.all_hi(i_first);
@@ -786,19 +784,23 @@ bool use_prefill(int rows, int batch, int q_heads, int kv_heads)
     return (long long)(q_heads / kv_heads) * rows > 64ll * batch;
 }
 
-template <int D, int NT, int WARPS, bool WIDE>
-cudaError_t launch_instance(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
+template <int D, int NT, int WARPS, int FORM>
+cudaError_t launch_form(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
 {
     using S = Shape<D, NT, WARPS>;
     static std::atomic<int> raised[kMaxDevices];
-    const cudaError_t e = raise_smem_limit(kv_decode_kernel<D, NT, WARPS, WIDE>, S::kSmem, raised);
+    const cudaError_t e = raise_smem_limit(kv_decode_kernel<D, NT, WARPS, FORM>, S::kSmem, raised);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(kv_decode_kernel<D, NT, WARPS, WIDE>, dim3(ctas), dim3(WARPS * 32), S::kSmem, st, a, sc);
+    return launch_overlapped(kv_decode_kernel<D, NT, WARPS, FORM>, dim3(ctas), dim3(WARPS * 32), S::kSmem, st, a, sc);
 }
 template <int D, int NT, int WARPS>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
 {
-    return a.extended() ? launch_instance<D, NT, WARPS, true>(a, sc, ctas, st) : launch_instance<D, NT, WARPS, false>(a, sc, ctas, st);
+    switch (form_of(a)) {
+    case kTree: return launch_form<D, NT, WARPS, kTree>(a, sc, ctas, st);
+    case kSinks: return launch_form<D, NT, WARPS, kSinks>(a, sc, ctas, st);
+    default: return launch_form<D, NT, WARPS, kPlain>(a, sc, ctas, st);
+    }
 }
 template <int D>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, const Variant &v, cudaStream_t st)

@@ -2,6 +2,8 @@
 // kv_prefill.cu: many): waits, the expansion of the codes, sequences as the kernels see them.
 #pragma once
 
+#include <type_traits>
+
 #include "kv_cache.cuh"
 
 namespace w4a8 {
@@ -183,28 +185,29 @@ struct Sight {
 // tree.  A row sees keys [0, sinks) and [lo, hi), the former below hi too; a drafted row sees, beside those of the tokens
 // in front of the drafts, the drafted rows of its mask.  It stands behind as many drafted tokens as its mask has bits (its own
 // among them): that is its position for the window.
+template <bool TREE>
 struct WideSight : Sight {
     int n, sinks, row0, words;
-    const uint32_t *tree;
+    const uint32_t *mask;
     __device__ WideSight(const KvAttnArgs &a, const Seq &s)
-        : Sight(a, s), n(s.n), sinks(a.window > 0 ? min(a.sinks, s.len) : 0), row0(s.row0), words(a.tree_words), tree(a.tree) {}
+        : Sight(a, s), n(s.n), sinks(a.window > 0 ? min(a.sinks, s.len) : 0), row0(s.row0), words(a.tree_words), mask(a.tree) {}
     // rows i .. of a tile: the first token in front of which none of them looks (sinks apart), and the end of what any sees
-    __device__ int tile_lo(int i_first) const { return lo(tree ? 0 : i_first); }
-    __device__ int tile_hi(int i_last) const { return !tree ? hi(i_last) : pos0 + i_last < 0 ? 0 : len; }
+    __device__ int tile_lo(int i_first) const { return lo(TREE ? 0 : i_first); }
+    __device__ int tile_hi(int i_last) const { return !TREE ? hi(i_last) : pos0 + i_last < 0 ? 0 : len; }
     // bounds of the tokens that all rows of a tile see
-    __device__ int all_lo(int i_last) const { return lo(tree ? n - 1 : i_last); }
+    __device__ int all_lo(int i_last) const { return lo(TREE ? n - 1 : i_last); }
     __device__ int all_hi(int i_first) const { return row_hi(i_first); }
     // one row: the end of the tokens that the window governs, and their beginning
-    __device__ int row_hi(int i) const { return !tree ? hi(i) : pos0 + i < 0 ? 0 : max(pos0, 0); }
+    __device__ int row_hi(int i) const { return !TREE ? hi(i) : pos0 + i < 0 ? 0 : max(pos0, 0); }
     __device__ uint32_t tree_word(int i, int w) const        // bits of drafted rows 32 w .. 32 w + 31 of the sequence
     {
         if (w < 0 || w >= words || 32 * w >= n) return 0u;
-        const uint32_t v = __ldca(tree + (size_t)(row0 + i) * words + w);
+        const uint32_t v = __ldca(mask + (size_t)(row0 + i) * words + w);
         return n - 32 * w >= 32 ? v : v & ((1u << (n - 32 * w)) - 1u);
     }
     __device__ int row_lo(int i) const
     {
-        if (!tree || window == 0) return lo(i);
+        if (!TREE || window == 0) return lo(i);
         int behind = 0;
         for (int w = 0; w < words && 32 * w < n; ++w) behind += __popc(tree_word(i, w));
         return lo(max(behind - 1, 0));
@@ -214,13 +217,19 @@ struct WideSight : Sight {
     {
         auto below = [&](int end) { return end <= j0 ? 0u : end - j0 >= 32 ? 0xffffffffu : (1u << (end - j0)) - 1u; };
         uint32_t v = below(row_hi) & (~below(row_lo) | below(sinks));
-        if (tree && pos0 + i >= 0) {
+        if (TREE && pos0 + i >= 0) {
             const int from = j0 - pos0;
             v |= __funnelshift_r(tree_word(i, from >> 5), tree_word(i, (from >> 5) + 1), from & 31);
         }
         return v;
     }
 };
+
+// The forms that the kernels are compiled in, and what a row sees in each.
+enum { kPlain = 0, kSinks = 1, kTree = 2 };
+template <int FORM> using View = std::conditional_t<FORM == kPlain, Sight, WideSight<FORM == kTree>>;
+
+inline int form_of(const KvAttnArgs &a) { return a.tree ? kTree : a.sinks > 0 && a.window > 0 ? kSinks : kPlain; }
 
 // Where the units of a tile lie that has sinks: `few` of them hold first tokens only and lie in front of the window's first
 // unit; none where the window begins among them.

@@ -227,7 +227,6 @@ struct KvAttnArgs {
     int sinks;                               // first tokens that stay visible beside the window
     const uint32_t *tree;                    // [rows][tree_words] or NULL: drafted rows that a row sees
     int tree_words;
-    bool extended() const { return tree != nullptr || (sinks > 0 && window > 0); }
 };
 size_t kv_attention_workspace(int rows, int batch, int q_heads, int kv_heads, int D);
 cudaError_t launch_kv_attention(const KvAttnArgs &a, uint8_t *workspace, cudaStream_t st);

@@ -39,8 +39,6 @@
 // see whole by 64 bits per row, made from bounds and the row's tree mask.  A chunk of 1024 rows at 9000, window 4096, 4 sinks: 126.5 us
 // (120.9 without the sinks in the plain form); 16 trees of 40 to 64 nodes, 32 / 8 heads, 1000 to 6000 tokens: 124.0 us (causal
 // rows in the plain form 122.5).
-#include <type_traits>
-
 #include "kv_attention.cuh"
 
 namespace w4a8 {
@@ -252,9 +250,10 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, Control
 
 // The share of the work list a CTA walks through: the list is, for every sequence, row tile and key
 // head in this order, kLead places and then the units that the tile's rows see (at least one place).
-template <bool WIDE>
+template <int FORM>
 struct Walk {
-    using View = std::conditional_t<WIDE, WideSight, Sight>;
+    static constexpr bool WIDE = FORM != kPlain;
+    using View = View<FORM>;
     const KvAttnArgs &a;
     const Schedule &sc;
     long long at, end, off;                    // place on the list, end of the share, place inside (sequence, tile)
@@ -372,12 +371,13 @@ __device__ __forceinline__ void store_eight(const KvAttnArgs &a, size_t at, cons
     *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.O) + at) = o;
 }
 
-template <int D, bool WIDE>
+template <int D, int FORM>
 __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_constant__ KvAttnArgs a, const __grid_constant__ Schedule sc)
 {
     using L = Layout<D>;
-    using Walk = Walk<WIDE>;
-    using View = typename Walk::View;
+    using Walk = Walk<FORM>;
+    using View = View<FORM>;
+    constexpr bool WIDE = FORM != kPlain;                  // sinks or a tree
     extern __shared__ uint8_t raw_smem[];
     __shared__ Control ctl_store;
     Control *ctl = &ctl_store;
@@ -425,8 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     long long mine = 0;
     for (int b = b_first; b < b_last; ++b) {
         const Seq s = load_seq(a, b, sc.sb);
-        if constexpr (WIDE)
-            if (a.tree && s.n > 32 * a.tree_words) report_failure(sc.sb, W4A8_ERR_BAD_TABLE, b);
+        if (FORM == kTree && s.n > 32 * a.tree_words) report_failure(sc.sb, W4A8_ERR_BAD_TABLE, b);
         const int tiles = Walk::tiles_of(s, (int)sc.group.d);
         for (int t = 0; t < tiles; t += 32) mine += Walk::tile_places(a, sc, s, t + lane);
     }
@@ -747,7 +746,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             // Block of this thread's token of unit u of the piece; behind the end the last one.  In front of what the tile
             // sees, in the first unit only, the first one that it sees: the page of the other may be gone.
             // (Extended: in front of the window as behind the sinks.)
-            const int near = WIDE ? WideSight(a, {pc.row0, pc.n, len}).sinks : 0, sink_block = near > 0 ? (near - 1) >> 4 : -1;
+            int near = 0;
+            if constexpr (WIDE) near = View(a, {pc.row0, pc.n, len}).sinks;
+            const int sink_block = near > 0 ? (near - 1) >> 4 : -1;
             const int few = pc.few, few0 = pc.few0;
             auto unit_at = [&](int u) { return !WIDE ? unit0 + u : u < few ? few0 + u : unit0 + u - few; };
             auto block_no = [&](int u) {
@@ -1068,20 +1069,23 @@ __global__ void __launch_bounds__(2 * D) kv_prefill_join_kernel(const __grid_con
     if (a.lse && c == 0) a.lse[row] = lsum > 0.0f ? (top + lg2(lsum)) * kLn2 : -INFINITY;
 }
 
-template <int D, bool WIDE>
-cudaError_t launch_instance(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
+template <int D, int FORM>
+cudaError_t launch_form(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
 {
     static std::atomic<int> raised[kMaxDevices];
-    cudaError_t e = raise_smem_limit(kv_prefill_kernel<D, WIDE>, Layout<D>::kSmem, raised);
-    if (e == cudaSuccess) e = launch_overlapped(kv_prefill_kernel<D, WIDE>, dim3(ctas), dim3(kThreads), Layout<D>::kSmem, st, a, sc);
+    cudaError_t e = raise_smem_limit(kv_prefill_kernel<D, FORM>, Layout<D>::kSmem, raised);
+    if (e == cudaSuccess) e = launch_overlapped(kv_prefill_kernel<D, FORM>, dim3(ctas), dim3(kThreads), Layout<D>::kSmem, st, a, sc);
     if (e == cudaSuccess) e = launch_overlapped(kv_prefill_join_kernel<D>, dim3(kRows / 32, ctas), dim3(2 * D), 0, st, a, sc);
     return e;
 }
-
 template <int D>
 cudaError_t launch(const KvAttnArgs &a, const Schedule &sc, int ctas, cudaStream_t st)
 {
-    return a.extended() ? launch_instance<D, true>(a, sc, ctas, st) : launch_instance<D, false>(a, sc, ctas, st);
+    switch (form_of(a)) {
+    case kTree: return launch_form<D, kTree>(a, sc, ctas, st);
+    case kSinks: return launch_form<D, kSinks>(a, sc, ctas, st);
+    default: return launch_form<D, kPlain>(a, sc, ctas, st);
+    }
 }
 
 }  // namespace
