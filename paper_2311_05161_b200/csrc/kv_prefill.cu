@@ -51,6 +51,9 @@ constexpr int kWarps = 20, kThreads = 32 * kWarps;         // the last one only 
 constexpr int kRing = 4;                                   // units of expanded keys, and of values
 constexpr int kConstSlots = 8;                             // more than kRing: a slot is rewritten after its unit's softmax
 constexpr int kLead = 6;                                   // an item's fixed cost, in units
+// What a CTA loses where its share is parts of two items instead of one item, in units.  (A chunk of 1024 rows, window 4096, 128 items of 67
+// units on 148 CTAs: one by one 122.0 us, in even shares 124.9 us.)
+constexpr int kTwoParts = 10;
 constexpr int kWaitSite = 950;
 constexpr int kApart = 16;                                 // a row at most 2^16 below its tile's largest is good to 2^-23 of its own largest element
 
@@ -221,6 +224,7 @@ struct Control {
     int found_b, found_tile;
     long long found_off;
     long long warp_len[kWarps];
+    int warp_items[kWarps], warp_longest[kWarps];
     Piece piece[2];
 };
 
@@ -256,6 +260,7 @@ struct Walk {
     using View = View<FORM>;
     const KvAttnArgs &a;
     const Schedule &sc;
+    const bool by_items;                       // the list is that of whole items, a place each
     long long at, end, off;                    // place on the list, end of the share, place inside (sequence, tile)
     int b, tile;
     Seq s;
@@ -265,7 +270,7 @@ struct Walk {
     long long first_unit;                      // the item's first unit on the list
     bool whole;
 
-    __device__ Walk(const KvAttnArgs &a_, const Schedule &sc_) : a(a_), sc(sc_), loaded(false) {}
+    __device__ Walk(const KvAttnArgs &a_, const Schedule &sc_, bool by_items_) : a(a_), sc(sc_), by_items(FORM == kSinks && by_items_), loaded(false) {}
 
     __device__ static int tiles_of(const Seq &s, int group) { return (int)(((long long)s.n * group + kRows - 1) / kRows); }
     __device__ static void span(const KvAttnArgs &a, const Schedule &sc, const Seq &s, int tile, int &i_first, int &i_last, int &rows,
@@ -288,13 +293,18 @@ struct Walk {
             units = max(0, ((sight.hi(i_last) + kUnit - 1) >> kUnitShift) - first);
         }
     }
-    // Places of the row tiles first_tile + lane of a sequence (0 behind the last).
-    __device__ static long long tile_places(const KvAttnArgs &a, const Schedule &sc, const Seq &s, int t)
+    // Places of an item of row tile t of a sequence (0 behind the last tile), of all items of it.
+    __device__ static int item_places(const KvAttnArgs &a, const Schedule &sc, const Seq &s, int t)
     {
         if (t >= tiles_of(s, (int)sc.group.d)) return 0;
         int i0, i1, rows, lo, first, few, units;
         span(a, sc, s, t, i0, i1, rows, lo, first, few, units);
-        return (long long)a.cache.heads * (kLead + max(units, 1));
+        return kLead + max(units, 1);
+    }
+    __device__ static long long tile_places(const KvAttnArgs &a, const Schedule &sc, const Seq &s, int t, bool by_items = false)
+    {
+        const int places = item_places(a, sc, s, t);
+        return (long long)a.cache.heads * (by_items ? min(places, 1) : places);
     }
     __device__ void start(int b0, int tile0, long long off0, long long begin, long long end_)
     {
@@ -324,7 +334,7 @@ struct Walk {
             }
             int i_last;
             span(a, sc, s, tile, i_first, i_last, rows, lo, first, few, units);
-            const int body = max(units, 1), length = kLead + body;
+            const int body = max(units, 1), length = by_items ? 1 : kLead + body;
             if (off >= (long long)a.cache.heads * length) {
                 off -= (long long)a.cache.heads * length;
                 ++tile;
@@ -334,7 +344,7 @@ struct Walk {
             const int in = (int)(off - (long long)h * length);
             const int here = (int)min((long long)(length - in), end - at);
             from = max(in - kLead, 0);
-            count = max(in + here - kLead, 0) - from;
+            count = by_items ? body : max(in + here - kLead, 0) - from;
             first_unit = at - in + kLead;
             at += here;
             off += here;
@@ -423,11 +433,24 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     const int chunk = (batch + kWarps - 1) / kWarps;
     const int b_first = min(batch, warp * chunk), b_last = min(batch, b_first + chunk);
     long long mine = 0;
+    int my_items = 0, longest = 0;
     for (int b = b_first; b < b_last; ++b) {
         const Seq s = load_seq(a, b, sc.sb);
         if (FORM == kTree && s.n > 32 * a.tree_words) report_failure(sc.sb, W4A8_ERR_BAD_TABLE, b);
         const int tiles = Walk::tiles_of(s, (int)sc.group.d);
-        for (int t = 0; t < tiles; t += 32) mine += Walk::tile_places(a, sc, s, t + lane);
+        for (int t = 0; t < tiles; t += 32) {
+            const int places = Walk::item_places(a, sc, s, t + lane);
+            mine += (long long)a.cache.heads * places;
+            if (FORM == kSinks) longest = max(longest, places);
+        }
+        if (FORM == kSinks) my_items = min(my_items + (int)min((long long)tiles * a.cache.heads, 1ll << 20), 1 << 20);     // (as many as matter)
+    }
+    if (FORM == kSinks) {
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        if (lane == 0) {
+            ctl->warp_items[warp] = my_items;
+            ctl->warp_longest[warp] = longest;
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
@@ -441,7 +464,24 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         if (w < warp) before += ctl->warp_len[w];
         total += ctl->warp_len[w];
     }
-    const long long per = max(quotient(total + gridDim.x - 1, gridDim.x), 4ll);
+    long long per = max(quotient(total + gridDim.x - 1, gridDim.x), 4ll);
+    bool by_items = false;
+    if (FORM == kSinks) {
+        // Where items are alike (every row tile lies beyond its window) and about as many as CTAs, a CTA takes one item: nothing is joined.
+        int n_items = 0, items_before = 0;
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) items_before += ctl->warp_items[w];
+            n_items += ctl->warp_items[w];
+            longest = max(longest, ctl->warp_longest[w]);
+        }
+        if (n_items <= (int)gridDim.x && longest <= per + kTwoParts) {
+            by_items = true;
+            per = 1;
+            total = n_items;
+            before = items_before;
+            mine = my_items;
+        }
+    }
     const long long begin = (long long)blockIdx.x * per, end = min(total, begin + per);
     if (begin < total && begin >= before && begin < before + mine) {
         long long at = before;
@@ -450,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             const Seq s = load_seq(a, b, sc.sb);
             const int tiles = Walk::tiles_of(s, (int)sc.group.d);
             for (int t = 0; t < tiles && !found; t += 32) {
-                const long long n = Walk::tile_places(a, sc, s, t + lane);
+                const long long n = Walk::tile_places(a, sc, s, t + lane, by_items);
                 long long upto = n;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -943,7 +983,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         }
         if (warp == kListWarp && lane == 0) {
             // -------------------------------------------------------------- the pieces of this CTA's share
-            Walk walk(a, sc);
+            Walk walk(a, sc, by_items);
             walk.start(ctl->found_b, ctl->found_tile, ctl->found_off, begin, max(begin, end));
             Shared shared = {};
             for (uint32_t piece_no = 0;; ++piece_no) {
