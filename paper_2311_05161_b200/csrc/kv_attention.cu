@@ -31,15 +31,16 @@
 //
 // Measured (8 key heads of 128 unless said): 64 ragged sequences of 1000 to 6000 tokens, 8 query heads per key
 // head, 248 MB: 80 us, 3.1 TB/s, issue slots 66 %, binary16 pipe 53 %, logic pipe 48 % busy.  One sequence of
-// 131001 tokens 52.8 us; 32 ragged sequences with 32 heads of their own 56.1 us; 513 tokens 9.2 us.  Beside the main
+// 131001 tokens 52.8 us; 32 ragged sequences with 32 heads of their own 56.1 us; 513 tokens 8.6 us.  Beside the main
 // loop (some 36 us of the 52.8 us, at 1200 cycles per 32 tokens and scheduler) stand 8 us until the first
 // unit is there (place on the list, page numbers, queries, copies, each waiting for the one before) and 4 us for the joins.
 //
-// The extended form (WIDE; first tokens that stay visible beside the window, rows of a drafted tree) walks the units with sinks and
-// then those of the window, and makes a unit that some row does not see whole a mask of 32 bits per row: the others
+// The extended forms (kSinks: first tokens that stay visible beside the window; kTree: rows of a drafted tree) walk the units with sinks and
+// then those of the window, and make a unit that some row does not see whole a mask of 32 bits per row: the others
 // cost what they cost without it, but for a few registers.  64 sequences, window 2047 and 5 sinks, 8 query heads per key head, 139 MB:
-// 53.8 us (52.0 without the sinks in the plain form); 12 trees of 3 to 13 nodes, 32 heads of their own, 97 MB: 56.9 us (causal rows in
-// the plain form 55.2); one sequence of 100001 tokens, window 4096: 12.2 us; a tree of 7 nodes at 2049 tokens: 14.2 us.
+// 52.5 us (52.0 without the sinks in the plain form); 12 trees of 3 to 13 nodes, 32 heads of their own, 97 MB: 55.0 us (causal rows in
+// the plain form the same); one sequence of 100001 tokens, window 4096: 11.8 us; a tree of 7 nodes at 2049 tokens: 14.1 us.
+// (One form for sinks and trees together: 53.4 and 56.4 us.)
 #include "kv_attention.cuh"
 
 namespace w4a8 {

@@ -4,9 +4,9 @@
 // codes and one word: 2 D + D/2 + 4 bytes, so the kernel is bound by memory for prompts and by
 // latency for decode steps.  A group of D/8 lanes owns a vector: a lane has eight elements in one
 // 16-byte load and writes one code word; the range is reduced over the group by shuffles.  The places
-// of a CTA's rows are found once, by a thread each.  Arithmetic is close to being the bound (182 instructions executed per
+// of a CTA's rows are found once, by a thread each.  Arithmetic is close to being the bound (157 instructions executed per
 // 8 elements of a lane), hence the group that keeps one row and advances by constants.  Four prompts (611 to 4097 tokens, 8
-// heads of 128, 54 MB): 24 us under the profiler, logic pipe 52 % and issue slots 71 % busy; 31.9 us with their read.
+// heads of 128, 54 MB): 24 us under the profiler, logic pipe 47 % and issue slots 61 % busy; 29.9 us with their read.
 // Read is the same walk the other way: 16 sequences (231 MB, 8 heads of 128) 46 us, 5.0 TB/s, issue slots
 // 69 % busy.  (A thread per eight elements that found its row by itself took 77 us there.)
 #include "kv_cache.cuh"
@@ -116,7 +116,7 @@ kv_append_kernel(const T *__restrict__ K, const T *__restrict__ V, long long k_s
                 }
                 float r;
                 int z;
-                const uint32_t word = kv_range_word(lo, hi, r, z), codes = kv_code_word(x, r, (float)z);
+                const uint32_t word = kv_range_word(lo, hi, r, z), codes = kv_code_word(x, r, kv_twice(z));
                 if (here) {
                     *reinterpret_cast<uint32_t *>(to + j * head_bytes + code_at) = codes;
                     if (l == 0) *reinterpret_cast<uint32_t *>(to + j * head_bytes + word_at) = word;

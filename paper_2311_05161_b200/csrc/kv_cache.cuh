@@ -105,26 +105,27 @@ __device__ __forceinline__ uint32_t kv_range_word(float lo, float hi, float &r, 
 // Eight consecutive elements as a code word: Eq. 5, the levels numbered in ascending order.  With u = x r, the place y
 // of a level counted from zero is 0 for |u| <= 1/4, +-1 for |u| <= 3/4 (the specials) and
 // +-(rint|u| + 1) beyond; the rank is y + z + 1.  The clamp of Eq. 5 acts at the upper end only: the least element's u is
-// -z before rounding.  y is the smaller of rint(f |u|) and rint|u| + 1, where f is the binary32 number in front of 2 (with 2
-// itself, 3/4 would be a tie): equal to the definition for every binary32 |u| below 16.  Rounding and conversion are additions of 1.5 * 2^23 (minus one), which leave the integer in the mantissa's low bits (the
-// constant's own low 16 bits are zero).
-__device__ __forceinline__ uint32_t kv_rank_bits(float x, float r, float top, float bias)
+// -z before rounding.  y is the one of rint(f u), rint(u) - 1 and rint(u) + 1 that lies between the others, where f is the binary32
+// number in front of 2 (with 2 itself, 3/4 would be a tie): equal to the definition for every binary32 |u| below 16.  Rounding and
+// conversion are additions of 1.5 * 2^23, which leave the integer in the mantissa's low bits (the constant's own low 16 bits
+// are zero); from there on two elements share an instruction.  (In binary32 throughout: eight instructions per element, here five.)
+__device__ __forceinline__ uint32_t kv_two_ranks(float x0, float x1, float r, uint32_t zz)
 {
-    const float u = __fmul_rn(x, r);
-    const float y = __fadd_rn(fminf(__fmaf_rn(fabsf(u), 0x1.fffffep0f, 12582911.0f), __fadd_rn(fabsf(u), 12582912.0f)), -12582911.0f);
-    return __float_as_uint(__fadd_rn(fminf(copysignf(y, u), top), bias));
+    const float u0 = __fmul_rn(x0, r), u1 = __fmul_rn(x1, r);
+    const uint32_t twice = __byte_perm(__float_as_uint(__fmaf_rn(u0, 0x1.fffffep0f, 12582912.0f)), __float_as_uint(__fmaf_rn(u1, 0x1.fffffep0f, 12582912.0f)), 0x5410);
+    const uint32_t once = __byte_perm(__float_as_uint(__fadd_rn(u0, 12582912.0f)), __float_as_uint(__fadd_rn(u1, 12582912.0f)), 0x5410);
+    const uint32_t y = __viaddmin_s16x2(once, 0x00010001u, __viaddmax_s16x2(once, 0xffffffffu, twice));
+    return __viaddmin_s16x2(y, zz, 0x000f000fu);
 }
-__device__ __forceinline__ uint32_t kv_code_word(const float (&x)[8], float r, float z)
+// zz = z + 1 in both halves.
+__device__ __forceinline__ uint32_t kv_code_word(const float (&x)[8], float r, uint32_t zz)
 {
-    const float top = 14.0f - z, bias = 12582913.0f + z;
-    uint32_t k[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) k[i] = kv_rank_bits(x[i], r, top, bias);
-    const uint32_t lo = (k[3] * 16u + k[2]) * 256u + (k[1] * 16u + k[0]);
-    const uint32_t hi = (k[7] * 16u + k[6]) * 256u + (k[5] * 16u + k[4]);
-    const uint32_t w = __byte_perm(lo, hi, 0x5410);
+    const uint32_t lo = kv_two_ranks(x[1], x[3], r, zz) * 16u + kv_two_ranks(x[0], x[2], r, zz);
+    const uint32_t hi = kv_two_ranks(x[5], x[7], r, zz) * 16u + kv_two_ranks(x[4], x[6], r, zz);
+    const uint32_t w = __byte_perm(lo, hi, 0x6420);
     return ((w << 2) & 0xFFFCFFFCu) | ((w >> 14) & 0x00030003u);         // both halves rotated left by two
 }
+__device__ __forceinline__ uint32_t kv_twice(int z) { return (uint32_t)(z + 1) * 0x00010001u; }
 
 // The eight levels of a code word, halved: pair k holds elements k and k + 4.  (x = rank - z - 1;
 // level / 2 = (x + 1) / 2 - sat(x / 4 + 1/2), packed binary16, exact.)

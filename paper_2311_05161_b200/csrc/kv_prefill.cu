@@ -35,9 +35,9 @@
 // Leaving out exponentials, token constants, expansion and moved references all together takes 13 us off the chunk, three of four
 // MMAs 8 us: no pipe is a unit's time, the hand-overs are.
 //
-// The extended form (WIDE) takes its units from the sinks and then from the window, and masks a unit that some row does not
-// see whole by 64 bits per row, made from bounds and the row's tree mask.  A chunk of 1024 rows at 9000, window 4096, 4 sinks: 126.5 us
-// (120.9 without the sinks in the plain form); 16 trees of 40 to 64 nodes, 32 / 8 heads, 1000 to 6000 tokens: 124.0 us (causal
+// The extended forms (kSinks, kTree) take their units from the sinks and then from the window, and mask a unit that some row does not
+// see whole by 64 bits per row, made from bounds and the row's tree mask.  A chunk of 1024 rows at 9000, window 4096, 4 sinks: 122 us
+// (120.9 without the sinks in the plain form); 16 trees of 40 to 64 nodes, 32 / 8 heads, 1000 to 6000 tokens: 124 us (causal
 // rows in the plain form 122.5).
 #include "kv_attention.cuh"
 

@@ -263,7 +263,7 @@ rope_append_kernel(const RopeArgs a, const KvCache c, const Units units, StatusB
         float my_r;
         int my_z;
         const uint32_t my_word = kv_range_word(lo[0], hi[0], my_r, my_z);
-        const float my_zero = (float)my_z;
+        const uint32_t my_zz = kv_twice(my_z);
         // four elements' codes are two bytes; the places of this lane's two halves
         const int a0 = VALUE ? 8 * l : e0, a1 = VALUE ? 8 * l + 4 : e1;
         uint8_t *to = block + h0 * head_bytes;
@@ -275,14 +275,15 @@ rope_append_kernel(const RopeArgs a, const KvCache c, const Units units, StatusB
         uint8_t *to0 = to + kv_code_offset(D, VALUE, s, a0 / 8) + (a0 & 4) / 2, *to1 = to + kv_code_offset(D, VALUE, s, a1 / 8) + (a1 & 4) / 2;
 #pragma unroll
         for (int j = 0; j < UNIT; ++j) {
-            float zero = my_zero, r_step = my_r;
+            uint32_t zz = my_zz;
+            float r_step = my_r;
             if constexpr (UNIT == 4) {
                 const int source = (j >> 1) * A + (j & 1) * B;
-                zero = __shfl_sync(0xffffffffu, my_zero, source, LPV);
+                zz = __shfl_sync(0xffffffffu, my_zz, source, LPV);
                 r_step = __shfl_sync(0xffffffffu, my_r, source, LPV);
             }
             if (here && j < n) {
-                const uint32_t codes = kv_code_word(x[j], r_step, zero);
+                const uint32_t codes = kv_code_word(x[j], r_step, zz);
                 if (VALUE || INTERLEAVED || !turned) *reinterpret_cast<uint32_t *>(to0) = codes;
                 else {
                     *reinterpret_cast<uint16_t *>(to0) = (uint16_t)codes;
