@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(THREADS) kv_plan_kernel(const KvPlanArgs a, St
     Entry *entry = reinterpret_cast<Entry *>(smem);                        // [batch]
     int *first_back = reinterpret_cast<int *>(smem + sizeof(Entry) * batch);   // [batch]: first page given back; pages afterwards
     int *pages_left = first_back + batch;
-    const int chunk = (batch + THREADS - 1) / THREADS;
+    const int chunk = (batch + THREADS - 1) / THREADS | 1;     // odd: the threads' entries lie in different banks
     const int b0 = min(batch, tid * chunk), b1 = min(batch, b0 + chunk);
     const int count = __ldca(a.free_count);
     Sums mine = {0, 0, 0};
