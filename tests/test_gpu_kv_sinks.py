@@ -211,3 +211,35 @@ def test_pages_between_sinks_and_window_may_hold_anything(rows):
     blocks[..., 16 * D:] = words.view(torch.uint8).view(bt.num_pages, H, 128)
     got = w4a8.kv_attention_sinks(Q, cache, bt.table, bt.kv_lens, H, ws, window, few, cu_rows=bt.cu)
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("rows", [None, [40, 33]])
+def test_queries_that_are_slices_and_one_row_per_sequence(rows):
+    """Q as a slice of a wider projection output; without cu_rows a tree has one node per sequence, its mask any."""
+    bt = Batch([300, 170], rows, 16)
+    cache = filled_cache(bt, 2, 64)
+    wide = torch.randn(bt.rows, 12, 64, dtype=BF16, device="cuda")
+    Q, ws = wide[:, 2:10], w4a8.new_kv_workspace(bt.rows, 2, 8, 2, 64)
+    bits = mask_words([1, 0] if rows is None else [m for c in rows for m in random_tree(c, c)], 2).cuda()
+    for call in (lambda q: w4a8.kv_attention_sinks(q, cache, bt.table, bt.kv_lens, 2, ws, 70, 5, cu_rows=bt.cu),
+                 lambda q: w4a8.kv_attention_tree(q, cache, bt.table, bt.kv_lens, 2, ws, bits, cu_rows=bt.cu)):
+        assert torch.equal(call(Q), call(Q.contiguous()))
+    if rows is None:
+        seen = [seen_in_tree(n, 1, 0, m, 0, 0) for n, m in zip(bt.lens, (1, 0))]
+        o, _, allow = attention_where(Q.contiguous(), cache, bt, 2, 0.125, seen)
+        check_attention(w4a8.kv_attention_tree(Q, cache, bt.table, bt.kv_lens, 2, ws, bits), o, allow, F16)
+    w4a8.check_status(ws)
+
+
+def test_large_scores_and_far_tokens():
+    """Weights that differ by thousands of powers of two: a sink far above the window's tokens, and far below them."""
+    for few in (1, 4):
+        for rows in (None, [70, 70]):
+            sinks([400, 90 if rows else 33], rows, 16, 4, 2, 64, 50, few, q_scale=60.0, scale=4.0)
+
+
+def test_items_alike_go_one_to_a_workgroup():
+    """Row tiles of one length, as many as workgroups and a little fewer, a few more (the many-row form); single rows likewise."""
+    for heads in (37, 36, 38):                 # 4 tiles of 64 tokens each
+        sinks([600], [256], 64, 4 * heads, heads, 64, 100, 4)
+    sinks([400] * 24, None, 16, 16, 16, 64, 100, 4)
