@@ -17,6 +17,21 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// Rounded once, values beyond the type's range to its largest finite ones.
+template <typename T> __device__ __forceinline__ uint32_t pack2_sat(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2_sat<__half>(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(fminf(fmaxf(a, -65504.0f), 65504.0f),
+                                        fminf(fmaxf(b, -65504.0f), 65504.0f));
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack2_sat<__nv_bfloat16>(float a, float b)
+{
+    const float m = __uint_as_float(0x7f7f0000u);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(fminf(fmaxf(a, -m), m), fminf(fmaxf(b, -m), m));
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
 // Where a row's vectors live: byte offset of its block of head 0, and the token's place in the block.
 struct RowPlace {
     long long at;                            // -1: the row reads as zeros; -2: it is left alone

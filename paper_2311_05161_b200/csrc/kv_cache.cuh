@@ -153,21 +153,6 @@ template <> __device__ __forceinline__ float2 to_float2<__nv_bfloat16>(uint32_t 
     return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
 }
 
-// Rounded once, values beyond the type's range to its largest finite ones.
-template <typename T> __device__ __forceinline__ uint32_t pack2_sat(float a, float b);
-template <> __device__ __forceinline__ uint32_t pack2_sat<__half>(float a, float b)
-{
-    const __half2 h = __floats2half2_rn(fminf(fmaxf(a, -65504.0f), 65504.0f),
-                                        fminf(fmaxf(b, -65504.0f), 65504.0f));
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-template <> __device__ __forceinline__ uint32_t pack2_sat<__nv_bfloat16>(float a, float b)
-{
-    const float m = __uint_as_float(0x7f7f0000u);
-    const __nv_bfloat162 h = __floats2bfloat162_rn(fminf(fmaxf(a, -m), m), fminf(fmaxf(b, -m), m));
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-
 cudaError_t launch_kv_append(const void *K, const void *V, int bf16, long long k_stride,
                              long long v_stride, const KvCache &c, const KvBatch &bt,
                              StatusBlock *sb, cudaStream_t st);
