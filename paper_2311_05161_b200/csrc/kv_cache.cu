@@ -67,7 +67,7 @@ __device__ RowPlace place_of(const KvCache &c, const KvBatch &bt, int row, Statu
 // A group of D/8 lanes owns a row and walks over `vecs` of its 2 * heads vectors (keys of all heads, then values),
 // so that its addresses advance by constants; the groups of a CTA own consecutive rows, which are
 // neighbours in the cache's blocks.
-constexpr int kUnroll = 4;                   // vectors of a group whose loads are in flight together
+constexpr int kUnroll = 4;                   // vectors of a group whose loads are in flight together, and that are quantized together
 
 // Sub-range [h0, h1) of the heads that a CTA's vectors v0 .. v0 + nv - 1 cover, for keys (0) or values (1).
 __device__ __forceinline__ void heads_of(int v0, int nv, int heads, int value, int &h0, int &h1)
@@ -76,7 +76,8 @@ __device__ __forceinline__ void heads_of(int v0, int nv, int heads, int value, i
     h1 = min(v0 + nv - value * heads, heads);
 }
 
-template <typename T, int D>
+// FOUR: kUnroll vectors are quantized together, else one by one.
+template <typename T, int D, bool FOUR>
 __global__ void __launch_bounds__(kThreads)
 kv_append_kernel(const T *__restrict__ K, const T *__restrict__ V, long long k_stride,
                  long long v_stride, KvCache c, KvBatch bt, int vecs, StatusBlock *sb)
@@ -108,33 +109,49 @@ kv_append_kernel(const T *__restrict__ K, const T *__restrict__ V, long long k_s
                 raw[j] = make_uint4(0u, 0u, 0u, 0u);
                 if (here && h + j < h1) raw[j] = __ldcs(reinterpret_cast<const uint4 *>(from + j * D));
             }
+            float x[kUnroll][8], lo[kUnroll], hi[kUnroll];
 #pragma unroll
             for (int j = 0; j < kUnroll; ++j) {
-                if (h + j >= h1) break;
-                float x[8];
+                if (!FOUR && h + j >= h1) break;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const float2 f = to_float2<T>((&raw[j].x)[k]);
-                    x[2 * k] = f.x;
-                    x[2 * k + 1] = f.y;
+                    x[j][2 * k] = f.x;
+                    x[j][2 * k + 1] = f.y;
                 }
-                float lo = 0.0f, hi = 0.0f;
+                lo[j] = hi[j] = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 8; k += 2) {
-                    lo = min3(lo, x[k], x[k + 1]);
-                    hi = max3(hi, x[k], x[k + 1]);
+                    lo[j] = min3(lo[j], x[j][k], x[j][k + 1]);
+                    hi[j] = max3(hi[j], x[j][k], x[j][k + 1]);
                 }
+                if constexpr (!FOUR) {
 #pragma unroll
-                for (int o = LPV / 2; o > 0; o >>= 1) {
-                    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-                    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+                    for (int o = LPV / 2; o > 0; o >>= 1) {
+                        lo[j] = fminf(lo[j], __shfl_xor_sync(0xffffffffu, lo[j], o));
+                        hi[j] = fmaxf(hi[j], __shfl_xor_sync(0xffffffffu, hi[j], o));
+                    }
+                    float r;
+                    int z;
+                    const uint32_t word = kv_range_word(lo[j], hi[j], r, z), codes = kv_code_word(x[j], r, kv_twice(z));
+                    if (here) {
+                        *reinterpret_cast<uint32_t *>(to + j * head_bytes + code_at) = codes;
+                        if (l == 0) *reinterpret_cast<uint32_t *>(to + j * head_bytes + word_at) = word;
+                    }
                 }
-                float r;
-                int z;
-                const uint32_t word = kv_range_word(lo, hi, r, z), codes = kv_code_word(x, r, kv_twice(z));
-                if (here) {
-                    *reinterpret_cast<uint32_t *>(to + j * head_bytes + code_at) = codes;
-                    if (l == 0) *reinterpret_cast<uint32_t *>(to + j * head_bytes + word_at) = word;
+            }
+            if constexpr (FOUR) {
+                float my_r;
+                int my_z;
+                const uint32_t my_word = kv_four_words<LPV>(lo, hi, l, my_r, my_z), my_zz = kv_twice(my_z);
+                constexpr int OWN = LPV / kUnroll;           // the words, by one lane each
+                const int mine = (l / OWN & 1) + (l / OWN & 2);
+                if (l % OWN == 0 && here && h + mine < h1) *reinterpret_cast<uint32_t *>(to + mine * head_bytes + word_at) = my_word;
+#pragma unroll
+                for (int j = 0; j < kUnroll; ++j) {
+                    const uint32_t zz = __shfl_sync(0xffffffffu, my_zz, kv_owner_of<LPV>(j), LPV);
+                    const float r = __shfl_sync(0xffffffffu, my_r, kv_owner_of<LPV>(j), LPV);
+                    if (here && h + j < h1) *reinterpret_cast<uint32_t *>(to + j * head_bytes + code_at) = kv_code_word(x[j], r, zz);
                 }
             }
             from += kUnroll * D;
@@ -216,9 +233,15 @@ template <typename T, int D>
 cudaError_t append(const void *K, const void *V, long long ks, long long vs, const KvCache &c,
                    const KvBatch &bt, StatusBlock *sb, cudaStream_t st)
 {
-    const Shape s = shape_of(D, c.heads, bt.rows);
-    return launch_overlapped(kv_append_kernel<T, D>, s.grid, dim3(kThreads), 0, st,
-                             static_cast<const T *>(K), static_cast<const T *>(V), ks, vs, c, bt, s.vecs, sb);
+    Shape s = shape_of(D, c.heads, bt.rows);
+    const T *k = static_cast<const T *>(K), *v = static_cast<const T *>(V);
+    // (four at a time where a CTA has as many of a row: 10348 rows of 8 heads 17.4 us, one by one 19.0; 128 rows, a vector or two a row: 3.4 us
+    // four at a time, 2.9 one by one)
+    if (s.vecs < kUnroll || c.heads < kUnroll)
+        return launch_overlapped(kv_append_kernel<T, D, false>, s.grid, dim3(kThreads), 0, st, k, v, ks, vs, c, bt, s.vecs, sb);
+    s.vecs = (s.vecs + kUnroll - 1) / kUnroll * kUnroll;
+    s.grid.y = (2 * c.heads + s.vecs - 1) / s.vecs;
+    return launch_overlapped(kv_append_kernel<T, D, true>, s.grid, dim3(kThreads), 0, st, k, v, ks, vs, c, bt, s.vecs, sb);
 }
 template <typename T, int D>
 cudaError_t read(const KvCache &c, const KvBatch &bt, void *K, void *V, StatusBlock *sb,

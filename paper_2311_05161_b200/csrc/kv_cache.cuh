@@ -127,6 +127,31 @@ __device__ __forceinline__ uint32_t kv_code_word(const float (&x)[8], float r, u
 }
 __device__ __forceinline__ uint32_t kv_twice(int z) { return (uint32_t)(z + 1) * 0x00010001u; }
 
+// The words of four vectors whose elements LPV lanes hold, from the lanes' ranges: the four are reduced side by side, so that a lane
+// is left with one vector's and the divisions of a step are done once for four.  Vector j's lanes: kv_owner_of(j) and the LPV / 4 - 1 behind it.
+template <int LPV> __device__ __forceinline__ int kv_owner_of(int j) { return (j >> 1) * (LPV / 2) + (j & 1) * (LPV / 4); }
+template <int LPV>
+__device__ __forceinline__ uint32_t kv_four_words(float (&lo)[4], float (&hi)[4], int lane, float &r, int &z)
+{
+    constexpr int A = LPV / 2, B = LPV / 4;
+    const bool up_a = lane & A, up_b = lane & B;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float send_lo = up_a ? lo[j] : lo[j + 2], send_hi = up_a ? hi[j] : hi[j + 2];
+        lo[j] = fminf(up_a ? lo[j + 2] : lo[j], __shfl_xor_sync(0xffffffffu, send_lo, A));
+        hi[j] = fmaxf(up_a ? hi[j + 2] : hi[j], __shfl_xor_sync(0xffffffffu, send_hi, A));
+    }
+    const float send_lo = up_b ? lo[0] : lo[1], send_hi = up_b ? hi[0] : hi[1];
+    float l = fminf(up_b ? lo[1] : lo[0], __shfl_xor_sync(0xffffffffu, send_lo, B));
+    float h = fmaxf(up_b ? hi[1] : hi[0], __shfl_xor_sync(0xffffffffu, send_hi, B));
+#pragma unroll
+    for (int o = B / 2; o > 0; o >>= 1) {
+        l = fminf(l, __shfl_xor_sync(0xffffffffu, l, o));
+        h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, o));
+    }
+    return kv_range_word(l, h, r, z);
+}
+
 // The eight levels of a code word, halved: pair k holds elements k and k + 4.  (x = rank - z - 1;
 // level / 2 = (x + 1) / 2 - sat(x / 4 + 1/2), packed binary16, exact.)
 __device__ __forceinline__ void kv_levels(uint32_t w, int z, __half2 (&o)[4])

@@ -240,37 +240,27 @@ rope_append_kernel(const RopeArgs a, const KvCache c, const Units units, StatusB
                 hi[j] = max3(hi[j], x[j][k], x[j][k + 1]);
             }
         }
-        // ranges: a lane is left with that of vector 2 (bit LPV / 2 of its number) + (bit LPV / 4)
-        constexpr int A = UNIT == 4 ? LPV / 2 : 0, B = UNIT == 4 ? LPV / 4 : LPV;
-        if constexpr (UNIT == 4) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const bool up = lane & A;
-                const float send_lo = up ? lo[j] : lo[j + 2], send_hi = up ? hi[j] : hi[j + 2];
-                lo[j] = fminf(up ? lo[j + 2] : lo[j], __shfl_xor_sync(0xffffffffu, send_lo, A));
-                hi[j] = fmaxf(up ? hi[j + 2] : hi[j], __shfl_xor_sync(0xffffffffu, send_hi, A));
-            }
-            const bool up = lane & B;
-            const float send_lo = up ? lo[0] : lo[1], send_hi = up ? hi[0] : hi[1];
-            lo[0] = fminf(up ? lo[1] : lo[0], __shfl_xor_sync(0xffffffffu, send_lo, B));
-            hi[0] = fmaxf(up ? hi[1] : hi[0], __shfl_xor_sync(0xffffffffu, send_hi, B));
-        }
-#pragma unroll
-        for (int o = B / 2; o > 0; o >>= 1) {
-            lo[0] = fminf(lo[0], __shfl_xor_sync(0xffffffffu, lo[0], o));
-            hi[0] = fmaxf(hi[0], __shfl_xor_sync(0xffffffffu, hi[0], o));
-        }
         float my_r;
         int my_z;
-        const uint32_t my_word = kv_range_word(lo[0], hi[0], my_r, my_z);
+        uint32_t my_word;
+        if constexpr (UNIT == 4) my_word = kv_four_words<LPV>(lo, hi, lane, my_r, my_z);
+        else {
+#pragma unroll
+            for (int o = LPV / 2; o > 0; o >>= 1) {
+                lo[0] = fminf(lo[0], __shfl_xor_sync(0xffffffffu, lo[0], o));
+                hi[0] = fmaxf(hi[0], __shfl_xor_sync(0xffffffffu, hi[0], o));
+            }
+            my_word = kv_range_word(lo[0], hi[0], my_r, my_z);
+        }
         const uint32_t my_zz = kv_twice(my_z);
         // four elements' codes are two bytes; the places of this lane's two halves
         const int a0 = VALUE ? 8 * l : e0, a1 = VALUE ? 8 * l + 4 : e1;
         uint8_t *to = block + h0 * head_bytes;
         const int n = c.heads - h0;
         {                                    // the words, by one lane each
-            const int j = UNIT == 4 ? (lane & A ? 2 : 0) + (lane & B ? 1 : 0) : 0;
-            if ((lane & (B - 1)) == 0 && here && j < n) *reinterpret_cast<uint32_t *>(to + j * head_bytes + kv_word_offset(D, VALUE, s)) = my_word;
+            constexpr int OWN = LPV / UNIT;
+            const int j = UNIT == 1 ? 0 : (l / OWN & 1) + (l / OWN & 2);
+            if (l % OWN == 0 && here && j < n) *reinterpret_cast<uint32_t *>(to + j * head_bytes + kv_word_offset(D, VALUE, s)) = my_word;
         }
         uint8_t *to0 = to + kv_code_offset(D, VALUE, s, a0 / 8) + (a0 & 4) / 2, *to1 = to + kv_code_offset(D, VALUE, s, a1 / 8) + (a1 & 4) / 2;
 #pragma unroll
@@ -278,9 +268,8 @@ rope_append_kernel(const RopeArgs a, const KvCache c, const Units units, StatusB
             uint32_t zz = my_zz;
             float r_step = my_r;
             if constexpr (UNIT == 4) {
-                const int source = (j >> 1) * A + (j & 1) * B;
-                zz = __shfl_sync(0xffffffffu, my_zz, source, LPV);
-                r_step = __shfl_sync(0xffffffffu, my_r, source, LPV);
+                zz = __shfl_sync(0xffffffffu, my_zz, kv_owner_of<LPV>(j), LPV);
+                r_step = __shfl_sync(0xffffffffu, my_r, kv_owner_of<LPV>(j), LPV);
             }
             if (here && j < n) {
                 const uint32_t codes = kv_code_word(x[j], r_step, zz);
