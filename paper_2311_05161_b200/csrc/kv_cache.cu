@@ -4,9 +4,10 @@
 // codes and one word: 2 D + D/2 + 4 bytes, so the kernel is bound by memory for prompts and by
 // latency for decode steps.  A group of D/8 lanes owns a vector: a lane has eight elements in one
 // 16-byte load and writes one code word; the range is reduced over the group by shuffles.  The places
-// of a CTA's rows are found once, by a thread each.  Arithmetic is close to being the bound (157 instructions executed per
-// 8 elements of a lane), hence the group that keeps one row and advances by constants.  Four prompts (611 to 4097 tokens, 8
-// heads of 128, 54 MB): 24 us under the profiler, logic pipe 47 % and issue slots 61 % busy; 29.9 us with their read.
+// of a CTA's rows are found once, by a thread each.  Arithmetic was the bound at 182 instructions executed per
+// 8 elements of a lane and is no longer at 119 (four vectors quantized together, ranks two to an instruction); hence too the group that
+// keeps one row and advances by constants.  Four prompts (611 to 4097 tokens, 8
+// heads of 128, 54 MB): 20 us under the profiler, logic pipe 47 % and issue slots 55 % busy; 28.2 us with their read.
 // Read is the same walk the other way: 16 sequences (231 MB, 8 heads of 128) 46 us, 5.0 TB/s, issue slots
 // 69 % busy.  (A thread per eight elements that found its row by itself took 77 us there.)
 #include "kv_cache.cuh"

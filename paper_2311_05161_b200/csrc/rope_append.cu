@@ -15,7 +15,7 @@
 // quantized together: their ranges are reduced side by side, so that a lane is left with one vector's and the two
 // divisions of a step are done once for four.
 //
-// Four prompts (10348 rows, 32 query and 8 key heads of 128, 223 MB): 48.6 us, 4.6 TB/s, 0.70 of the copy rate; issue slots 64 %
+// Four prompts (10348 rows, 32 query and 8 key heads of 128, 223 MB): 48.0 us, 4.6 TB/s, 0.71 of the copy rate; issue slots 62 %
 // busy, and the same walk without sines, quantizer and cache stores still takes 45 us.  Measured and left: a row's vectors
 // split over CTAs, with a lane's partner elements by shuffles 53.9 us; rows in CTAs with barriers 54.7; asynchronous copies into
 // shared memory instead of registers 52.4; packed binary32 products 52.7; 5 or 6 CTAs per SM (fewer registers) 50.6 and
