@@ -558,7 +558,7 @@ w4a8_status w4a8_kv_attention_sinks(const void *Q, int q_type, long long q_strid
 /* Attention of drafted rows: the rows of a sequence are the nodes of a tree (or several) behind its tokens.  Row i of
  * sequence b, whose rows begin at position base = kv_lens[b] - n_b, sees
  *   - the tokens in front of base, all of them or, with a window, those j with j > p - window or j < sinks, where
- *     p = base + (bits of its mask) - 1 (its mask names its ancestors and itself);
+ *     p = base + (bits of its mask, at least 1) - 1 (its mask names its ancestors and itself);
  *   - the drafted rows j (at position base + j) of its mask: bit j % 32 of tree_mask[row][j / 32].
  * Bits of rows that the sequence does not have are ignored; any mask is allowed, an empty one too.
  *   tree_mask   [rows][mask_words] UINT32; a sequence may have up to 32 * mask_words rows (more are reported as

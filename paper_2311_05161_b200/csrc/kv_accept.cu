@@ -4,8 +4,8 @@
 // A moved vector is D/2 bytes of codes and a word, copied as they are.  A group of D/8 lanes owns one vector (a head's key or value) of a
 // sequence and walks along its path, so that every byte is read and written by the same lane; as the path ascends, path[i] >= i and the
 // slot that the i-th copy fills is the source of no later copy: the copies need no order among lanes, and a lane may
-// load several in front of its first store.  Few bytes move: the time is a launch and four dependent accesses (path, page
-// table, source, destination).  Eight sequences of 8 heads 2.9 us, 64 of 32 heads with up to nine accepted rows 5.1 us (5 MB).
+// load several in front of its first store.  Few bytes move: the time is a launch and four dependent accesses (lengths with
+// the path, page table, source, destination).  Eight sequences of 8 heads 2.9 us, 64 of 32 heads with up to nine accepted rows 5.1 us (5 MB).
 #include "kv_cache.cuh"
 
 namespace w4a8 {
@@ -37,6 +37,9 @@ __global__ void __launch_bounds__(kThreads) kv_accept_kernel(const KvCache c, co
     allow_dependents();
     dependent_wait();
     const int b = blockIdx.x, tid = threadIdx.x;
+    const int32_t *path = paths.accepted + (size_t)b * paths.most;
+    // (the first places travel with the lengths)
+    const int first = tid < min(kBatch, paths.most) ? __ldca(path + tid) : 0;
     const int len = __ldca(bt.kv_lens + b);
     const int row0 = bt.cu_rows ? __ldca(bt.cu_rows + b) : b, row1 = bt.cu_rows ? __ldca(bt.cu_rows + b + 1) : b + 1;
     int count = __ldca(paths.accept_lens + b);
@@ -47,7 +50,6 @@ __global__ void __launch_bounds__(kThreads) kv_accept_kernel(const KvCache c, co
         count = 0;
     }
     if (paths.kv_lens_out && blockIdx.y == 0 && tid == 0) paths.kv_lens_out[b] = max(base, 0) + count;
-    const int32_t *path = paths.accepted + (size_t)b * paths.most;
     const size_t head_bytes = ((size_t)1 << c.page_shift) * (D + 8);
     const int l = tid % LPV, vec = blockIdx.y * GROUPS + tid / LPV;
     const int head = vec >> 1, value = vec & 1;
@@ -56,7 +58,7 @@ __global__ void __launch_bounds__(kThreads) kv_accept_kernel(const KvCache c, co
         const int here = min(kBatch, count - i0);
         if (i0) __syncthreads();             // the places of the copies before are no longer needed
         for (int k = tid; k < here; k += kThreads) {
-            const int i = i0 + k, j = __ldca(path + i), before = i ? __ldca(path + i - 1) : -1;
+            const int i = i0 + k, j = i0 ? __ldca(path + i) : first, before = i ? __ldca(path + i - 1) : -1;
             Slot x = {-1, 0}, y = {-1, 0};
             if (j <= before || j >= n) report_failure(sb, W4A8_ERR_BAD_TABLE, b);
             else if (j != i) {

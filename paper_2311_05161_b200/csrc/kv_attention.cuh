@@ -183,8 +183,8 @@ struct Sight {
 
 // The same with what the extended form knows: `sinks` first tokens that stay visible beside the window, or the rows of a drafted
 // tree.  A row sees keys [0, sinks) and [lo, hi), the former below hi too; a drafted row sees, beside those of the tokens
-// in front of the drafts, the drafted rows of its mask.  It stands behind as many drafted tokens as its mask has bits (its own
-// among them): that is its position for the window.
+// in front of the drafts, the drafted rows of its mask.  Its position for the window is that of the
+// last of as many drafted tokens as its mask has bits (its own among them; at least one).
 template <bool TREE>
 struct WideSight : Sight {
     int n, sinks, row0, words;

@@ -175,3 +175,20 @@ def test_refusals_in_python():
         w4a8.kv_plan(held, kept, add, table, free, count, 17, 5, ws)
     with pytest.raises(w4a8.W4A8Error):
         w4a8.kv_plan(held, kept, add, table, free, count, 16, 5, ws, out=(kept, None, None, None, None))
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_outputs_off_the_16_byte_grid(shift):
+    """Positions and slots that begin anywhere: the wide stores are left out."""
+    c = Case(requests(20, 90, shift, KINDS), 16, spare_rows=3)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    ws = guarded_workspace(512)
+    pos, slots = torch.full((c.rows + 8,), 77, dtype=torch.int32, device="cuda"), torch.full((c.rows + 8,), 77, dtype=torch.int64, device="cuda")
+    table, free = torch.from_numpy(c.table).cuda(), torch.from_numpy(c.free).cuda()
+    out = w4a8.kv_plan(i32(c.held), i32(c.kept), i32(c.add), table, free, i32([c.count]), 16, c.rows, ws.t,
+                       out=(None, None, pos[shift:shift + c.rows], slots[shift:shift + c.rows], None))
+    c.status = w4a8.poll_status(ws.t)
+    c.check(dict(table=table.cpu().numpy(), free=free.cpu().numpy(), lens=out[0].cpu().numpy(), cu=out[1].cpu().numpy(),
+                 positions=out[2].cpu().numpy(), slots=out[3].cpu().numpy(), count=out[4].cpu().numpy()))
+    for t in (pos, slots):
+        assert (t[:shift] == 77).all() and (t[shift + c.rows:] == 77).all()
