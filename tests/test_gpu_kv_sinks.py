@@ -243,3 +243,37 @@ def test_items_alike_go_one_to_a_workgroup():
     for heads in (37, 36, 38):                 # 4 tiles of 64 tokens each
         sinks([600], [256], 64, 4 * heads, heads, 64, 100, 4)
     sinks([400] * 24, None, 16, 16, 16, 64, 100, 4)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("pages", [0, 900])
+def test_the_width_of_the_page_table(D, pages):
+    """Pages that no sequence reaches yet: the tiles of rows may differ, the result does not."""
+    def widen(bt):
+        more = torch.full((len(bt.lens), pages), -7, dtype=torch.int32, device="cuda")
+        return torch.cat([bt.table, more], 1)
+
+    lens, rows, P, Hq, H = [130, 5, 77, 300], [5, 3, 0, 7], 16, 16, 4
+    bt = Batch(lens, rows, P, 0)
+    seen = [seen_with_sinks(n, c, i, True, 40, 3) for n, c in zip(lens, rows) for i in range(c)]
+    run(lambda Q, cache, ws, out, lse, scale: w4a8.kv_attention_sinks(Q, cache, widen(bt), bt.kv_lens, H, ws, 40, 3, cu_rows=bt.cu, scale=scale, out=out, lse=lse),
+        seen, bt, Hq, H, D)
+    bt = Batch(lens, rows, P, 0)
+    seen = [seen_with_sinks(n, c, i, True, 5000, 3) for n, c in zip(lens, rows) for i in range(c)]
+    run(lambda Q, cache, ws, out, lse, scale: w4a8.kv_attention_sinks(Q, cache, widen(bt), bt.kv_lens, H, ws, 5000, 3, cu_rows=bt.cu, scale=scale, out=out, lse=lse),
+        seen, bt, Hq, H, D)
+    bt = Batch(lens, rows, P, 0)
+    masks = [m for b, n in enumerate(rows) for m in random_tree(n, b)]
+    seen = [seen_in_tree(n, c, i, masks[bt.start[b] + i], 0, 0) for b, (n, c) in enumerate(zip(lens, rows)) for i in range(c)]
+    bits = mask_words(masks, 1).cuda()
+    run(lambda Q, cache, ws, out, lse, scale: w4a8.kv_attention_tree(Q, cache, widen(bt), bt.kv_lens, H, ws, bits, cu_rows=bt.cu, scale=scale, out=out, lse=lse),
+        seen, bt, Hq, H, D)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("window,few", [(1, 1), (20, 4), (33, 20), (64, 0)])
+def test_a_few_rows_of_many_sequences(D, window, few):
+    lens, rows = [90, 17, 64, 33, 5, 70, 32, 81, 48, 16, 0, 77], [7, 8, 5, 6, 5, 8, 3, 7, 8, 4, 0, 1]
+    sinks(lens, rows, 16, 24, 12, D, window, few)
+    masks = [m for b, n in enumerate(rows) for m in random_tree(n, b)]
+    tree(lens, rows, 16, 24, 12, D, masks, window, few)
