@@ -581,7 +581,9 @@ w4a8_status w4a8_kv_attention_tree(const void *Q, int q_type, long long q_stride
  *   accept_lens [batch] INT32, at most max_accept and the sequence's rows.
  *   kv_lens_out out [batch] INT32: base + accept_lens[b], or NULL.  Not kv_lens itself.
  * A sequence with lengths or offsets out of range, or with more accepted rows than it has, keeps its slots
- * as they are; a place that does not ascend or names no row is left out; both are reported (W4A8_ERR_BAD_TABLE).
+ * as they are.  A place accepted[b][i] that names no row (a negative one among them), that is not above the one in front of it
+ * or that is below i (in an ascending path none is) is left out: slot base + i keeps what it holds.  Both are
+ * reported (W4A8_ERR_BAD_TABLE).
  *   workspace   its first 256 bytes, for the reports. */
 w4a8_status w4a8_kv_accept(void *cache, int num_pages, int page_size, int kv_heads, int head_dim,
                            const int32_t *page_table, int max_pages, const int32_t *kv_lens,

@@ -52,11 +52,11 @@ __device__ __forceinline__ int kv_position_of(const KvBatch &bt, int b, int row,
     return ok ? len - (end - row) : -1;
 }
 
-// Page number of position pos (>= 0), or -1.
+// Page number of position pos, or -1 (as of a position in front of the sequence or behind its table).
 __device__ __forceinline__ int kv_page_of(const KvCache &c, const KvBatch &bt, int b, int pos)
 {
     const int i = pos >> c.page_shift;
-    if (i >= bt.max_pages) return -1;
+    if ((unsigned)i >= (unsigned)bt.max_pages) return -1;
     const int p = __ldca(bt.page_table + (size_t)b * bt.max_pages + i);
     return (unsigned)p < (unsigned)c.num_pages ? p : -1;
 }
