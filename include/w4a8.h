@@ -510,7 +510,8 @@ w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, con
  *   rows        size of positions and slots, at most 2^30; rows from cu_rows[batch] on get position 0 and slot -1.
  * A step whose rows do not fit, whose lengths are out of range or whose free list is damaged (W4A8_ERR_BAD_TABLE), or
  * that needs more pages than are free (W4A8_ERR_NO_PAGES), is refused as a whole: cu_rows are 0, slots -1, kv_lens_out is held,
- * free_count_out is free_count, the table and the list are left alone; the status block reports it.
+ * free_count_out is free_count, the table and the list are left alone; the status block reports it.  (What the sequences keep is then
+ * in kv_lens alone: held may count more.)
  * batch <= 8192.  workspace: 512 bytes, zero-filled once; one that the cache calls use will do. */
 w4a8_status w4a8_kv_plan(const int32_t *held, const int32_t *kv_lens, const int32_t *add, int batch,
                          int32_t *page_table, int max_pages, int page_size, int32_t *free_pages,
@@ -584,12 +585,25 @@ w4a8_status w4a8_kv_attention_tree(const void *Q, int q_type, long long q_stride
  * as they are.  A place accepted[b][i] that names no row (a negative one among them), that is not above the one in front of it
  * or that is below i (in an ascending path none is) is left out: slot base + i keeps what it holds.  Both are
  * reported (W4A8_ERR_BAD_TABLE).
- *   workspace   its first 256 bytes, for the reports. */
+ *   workspace   its first 256 bytes, for the reports.
+ * Behind a plan that was refused no sequence has rows, and the lengths that it left are those that the pages were taken for, an earlier
+ * step's drafts that were not accepted among them: kv_lens_out is then what the plan left, and not what
+ * the sequences keep.  A step that may be refused passes the kept lengths to w4a8_kv_accept_ex (or, where the host looks
+ * at the status of every step, plans again with them). */
 w4a8_status w4a8_kv_accept(void *cache, int num_pages, int page_size, int kv_heads, int head_dim,
                            const int32_t *page_table, int max_pages, const int32_t *kv_lens,
                            const int32_t *cu_rows, int batch, int rows, const int32_t *accepted, int max_accept,
                            const int32_t *accept_lens, int32_t *kv_lens_out, void *workspace,
                            size_t workspace_bytes, void *stream);
+/* w4a8_kv_accept with
+ *   kept        [batch] INT32, what the step's plan took as kv_lens, or NULL: kv_lens_out[b] of a sequence without rows in the
+ *               call, or with lengths, offsets or a number of accepted rows out of range.  May be kv_lens_out itself, so that a
+ *               captured loop of plan, attention and accept loses nothing in a step that was refused. */
+w4a8_status w4a8_kv_accept_ex(void *cache, int num_pages, int page_size, int kv_heads, int head_dim,
+                              const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                              const int32_t *cu_rows, int batch, int rows, const int32_t *accepted,
+                              int max_accept, const int32_t *accept_lens, const int32_t *kept,
+                              int32_t *kv_lens_out, void *workspace, size_t workspace_bytes, void *stream);
 
 /* w4a8_linear_asym for any group_size: with group_size 128 the token's zero-point leaves every
  * group's integer sum before that sum is scaled,

@@ -39,6 +39,7 @@ EXPORTS = (
     "w4a8_add_norm_quantize_act", "w4a8_kv_page_bytes", "w4a8_kv_append", "w4a8_kv_read",
     "w4a8_kv_attention", "w4a8_kv_attention_workspace_bytes",
     "w4a8_kv_plan", "w4a8_rope_kv_append", "w4a8_kv_attention_sinks", "w4a8_kv_attention_tree", "w4a8_kv_accept",
+    "w4a8_kv_accept_ex",
 )
 
 
@@ -147,6 +148,8 @@ def _load() -> ctypes.CDLL:
                                         vp, ci, ci, vp, sz, vp]
     lib.w4a8_kv_accept.restype = ci
     lib.w4a8_kv_accept.argtypes = [vp, ci, ci, ci, ci, vp, ci, vp, vp, ci, ci, vp, ci, vp, vp, vp, sz, vp]
+    lib.w4a8_kv_accept_ex.restype = ci
+    lib.w4a8_kv_accept_ex.argtypes = [vp, ci, ci, ci, ci, vp, ci, vp, vp, ci, ci, vp, ci, vp, vp, vp, vp, sz, vp]
     lib.w4a8_linear_acc_i32.restype = ci
     lib.w4a8_linear_acc_i32.argtypes = [vp, vp, ci, ci, ci, ci, vp, vp, sz, vp, op]
     lib.w4a8_unpack_codes.restype = ci
@@ -601,10 +604,12 @@ def kv_attention_tree(Q, cache, page_table, kv_lens, kv_heads: int, workspace, t
     return _calls.kv_attention_tree(Q, cache, page_table, kv_lens, kv_heads, workspace, tree_mask, cu_rows, scale, window, sinks, dtype, out, lse)
 
 
-def kv_accept(cache, page_table, kv_lens, accepted, accept_lens, kv_heads: int, head_dim: int, workspace, cu_rows=None, out=None):
+def kv_accept(cache, page_table, kv_lens, accepted, accept_lens, kv_heads: int, head_dim: int, workspace, cu_rows=None, out=None, kept=None):
     """Moves the accepted drafted rows, places accepted [batch, max_accept] int32 among the sequence's rows in ascending order, to
-    the front of the sequence's drafted slots, accept_lens [batch] int32 of them.  Returns the sequences' new lengths."""
-    return _calls.kv_accept(cache, page_table, kv_lens, accepted, accept_lens, kv_heads, head_dim, workspace, cu_rows, out)
+    the front of the sequence's drafted slots, accept_lens [batch] int32 of them.  Returns the sequences' new lengths; `kept` [batch]
+    int32, what the step's plan took as kv_lens, are those of sequences without rows in the call, as all are behind a refused
+    plan (in place with `out=kept`)."""
+    return _calls.kv_accept(cache, page_table, kv_lens, accepted, accept_lens, kv_heads, head_dim, workspace, cu_rows, out, kept)
 
 
 def linear_static(Xq, tok_scale, packed, bias, N: int, group: int, out):

@@ -717,6 +717,16 @@ w4a8_status w4a8_kv_accept(void *cache, int num_pages, int page_size, int kv_hea
                            const int32_t *accept_lens, int32_t *kv_lens_out, void *workspace,
                            size_t workspace_bytes, void *stream)
 {
+    return w4a8_kv_accept_ex(cache, num_pages, page_size, kv_heads, head_dim, page_table, max_pages, kv_lens, cu_rows, batch, rows, accepted,
+                             max_accept, accept_lens, nullptr, kv_lens_out, workspace, workspace_bytes, stream);
+}
+
+w4a8_status w4a8_kv_accept_ex(void *cache, int num_pages, int page_size, int kv_heads, int head_dim,
+                              const int32_t *page_table, int max_pages, const int32_t *kv_lens,
+                              const int32_t *cu_rows, int batch, int rows, const int32_t *accepted, int max_accept,
+                              const int32_t *accept_lens, const int32_t *kept, int32_t *kv_lens_out, void *workspace,
+                              size_t workspace_bytes, void *stream)
+{
     if (!accepted || !accept_lens) return W4A8_ERR_NULL;
     KvCache c;
     KvBatch bt;
@@ -724,10 +734,10 @@ w4a8_status w4a8_kv_accept(void *cache, int num_pages, int page_size, int kv_hea
                                     kv_lens, cu_rows, batch, rows, workspace, workspace_bytes, &c, &bt);
     if (s != W4A8_OK) return s;
     if (max_accept < 1 || kv_lens_out == kv_lens) return W4A8_ERR_SHAPE;
-    if (!aligned(accepted, 4) || !aligned(accept_lens, 4) || !aligned(kv_lens_out, 4)) return W4A8_ERR_ALIGN;
+    if (!aligned(accepted, 4) || !aligned(accept_lens, 4) || !aligned(kept, 4) || !aligned(kv_lens_out, 4)) return W4A8_ERR_ALIGN;
     const w4a8_status arch = check_arch();
     if (arch != W4A8_OK) return arch;
-    const cudaError_t e = launch_kv_accept(c, bt, {accepted, accept_lens, kv_lens_out, max_accept}, static_cast<StatusBlock *>(workspace),
+    const cudaError_t e = launch_kv_accept(c, bt, {accepted, accept_lens, kept, kv_lens_out, max_accept}, static_cast<StatusBlock *>(workspace),
                                            static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
 }

@@ -355,26 +355,29 @@ PyObject *kv_attention_tree(PyObject *, PyObject *const *v, Py_ssize_t n)
     });
 }
 
-// cache, page_table, kv_lens, accepted, accept_lens, kv_heads, head_dim, workspace, cu_rows, out
+// cache, page_table, kv_lens, accepted, accept_lens, kv_heads, head_dim, workspace, cu_rows, out, kept
 PyObject *kv_accept(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
-    if (!counted("kv_accept", n, 10)) return nullptr;
+    if (!counted("kv_accept", n, 11)) return nullptr;
     return guarded([&] {
         const int heads = integer(v[5], "kv_heads"), D = integer(v[6], "head_dim");
         const Batch b("kv_accept", v[0], v[1], v[2], v[8], v[7], heads, D);
         const at::Tensor &accepted = of_type(v[3], at::kInt, "accepted"), &lens = of_type(v[4], at::kInt, "accept_lens");
         if (accepted.dim() != 2 || accepted.size(0) != b.batch) wrong_value("accepted: expected [batch, max_accept]");
+        const at::Tensor *kept = maybe(v[10], at::kInt, "kept");
         shaped(lens, {b.batch}, "accept_lens");
+        if (kept) shaped(*kept, {b.batch}, "kept");
         const at::Tensor out = v[9] == Py_None ? fresh({b.batch}, at::kInt, b.lens) : of_type(v[9], at::kInt, "out");
         shaped(out, {b.batch}, "out");
-        void *st = stream_of("kv_accept", {&b.cache, &b.table, &b.lens, b.cu, &b.space, &accepted, &lens, &out});
+        void *st = stream_of("kv_accept", {&b.cache, &b.table, &b.lens, b.cu, &b.space, &accepted, &lens, kept, &out});
         // (no row of the call is read here: with cu_rows any number of them will do)
         const int most = number(accepted.size(1), "accepted"), rows = b.cu ? INT_MAX / heads : b.batch;
         w4a8_status status;
         Py_BEGIN_ALLOW_THREADS
-        status = w4a8_kv_accept(b.cache.data_ptr(), b.num_pages, b.page_size, heads, D, b.table_at(), b.max_pages, b.lens_at(), b.cu_at(), b.batch, rows,
-                                static_cast<const int32_t *>(accepted.data_ptr()), most, static_cast<const int32_t *>(lens.data_ptr()),
-                                static_cast<int32_t *>(out.data_ptr()), b.space.data_ptr(), b.space.numel(), st);
+        status = w4a8_kv_accept_ex(b.cache.data_ptr(), b.num_pages, b.page_size, heads, D, b.table_at(), b.max_pages, b.lens_at(), b.cu_at(), b.batch, rows,
+                                   static_cast<const int32_t *>(accepted.data_ptr()), most, static_cast<const int32_t *>(lens.data_ptr()),
+                                   static_cast<const int32_t *>(at_or_null(kept)), static_cast<int32_t *>(out.data_ptr()), b.space.data_ptr(),
+                                   b.space.numel(), st);
         Py_END_ALLOW_THREADS
         check(status, "w4a8_kv_accept");
         return own(v[9], out);

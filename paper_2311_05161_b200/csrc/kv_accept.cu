@@ -43,13 +43,16 @@ __global__ void __launch_bounds__(kThreads) kv_accept_kernel(const KvCache c, co
     const int len = __ldca(bt.kv_lens + b);
     const int row0 = bt.cu_rows ? __ldca(bt.cu_rows + b) : b, row1 = bt.cu_rows ? __ldca(bt.cu_rows + b + 1) : b + 1;
     int count = __ldca(paths.accept_lens + b);
+    const int kept = paths.kept ? __ldca(paths.kept + b) : 0;
     const int n = row1 - row0, base = len - n;
-    if (row0 < 0 || n < 0 || row1 > bt.rows || base < 0 || (long long)len > (long long)bt.max_pages << c.page_shift || count < 0 || count > paths.most ||
-        count > n) {
+    const bool good = row0 >= 0 && n >= 0 && row1 <= bt.rows && base >= 0 && (long long)len <= (long long)bt.max_pages << c.page_shift && count >= 0 &&
+                      count <= paths.most && count <= n;
+    if (!good) {
         if (tid == 0) report_failure(sb, W4A8_ERR_BAD_TABLE, b);
         count = 0;
     }
-    if (paths.kv_lens_out && blockIdx.y == 0 && tid == 0) paths.kv_lens_out[b] = max(base, 0) + count;
+    // (a plan that was refused gives no sequence rows, and as their lengths those that the pages were taken for)
+    if (paths.kv_lens_out && blockIdx.y == 0 && tid == 0) paths.kv_lens_out[b] = paths.kept && (n == 0 || !good) ? kept : max(base, 0) + count;
     const size_t head_bytes = ((size_t)1 << c.page_shift) * (D + 8);
     const int l = tid % LPV, vec = blockIdx.y * GROUPS + tid / LPV;
     const int head = vec >> 1, value = vec & 1;

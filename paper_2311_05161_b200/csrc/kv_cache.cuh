@@ -203,6 +203,7 @@ cudaError_t launch_rope_kv_append(const RopeArgs &a, int bf16, int interleaved, 
 struct KvPaths {
     const int32_t *accepted;                 // [batch][most]
     const int32_t *accept_lens;              // [batch]
+    const int32_t *kept;                     // [batch] or NULL: lengths of sequences without rows in the call
     int32_t *kv_lens_out;                    // [batch] or NULL
     int most;
 };
