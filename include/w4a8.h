@@ -580,7 +580,7 @@ w4a8_status w4a8_kv_attention_tree(const void *Q, int q_type, long long q_stride
  * it once per layer's cache, then plan the next step with kv_lens_out (and held = the lengths of this one).
  *   accepted    [batch][max_accept] INT32, places among the sequence's rows, ascending.
  *   accept_lens [batch] INT32, at most max_accept and the sequence's rows.
- *   kv_lens_out out [batch] INT32: base + accept_lens[b], or NULL.  Not kv_lens itself.
+ *   kv_lens_out out [batch] INT32: base + accept_lens[b], or NULL.  It may overlap no input (W4A8_ERR_SHAPE).
  * A sequence with lengths or offsets out of range, or with more accepted rows than it has, keeps its slots
  * as they are.  A place accepted[b][i] that names no row (a negative one among them), that is not above the one in front of it
  * or that is below i (in an ascending path none is) is left out: slot base + i keeps what it holds.  Both are

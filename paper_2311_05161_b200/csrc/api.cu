@@ -735,6 +735,14 @@ w4a8_status w4a8_kv_accept_ex(void *cache, int num_pages, int page_size, int kv_
     if (s != W4A8_OK) return s;
     if (max_accept < 1 || kv_lens_out == kv_lens) return W4A8_ERR_SHAPE;
     if (!aligned(accepted, 4) || !aligned(accept_lens, 4) || !aligned(kept, 4) || !aligned(kv_lens_out, 4)) return W4A8_ERR_ALIGN;
+    // A sequence has several CTAs: one writes its length while others may still read what it goes by.
+    const long long n = batch;
+    auto meets = [&](const int32_t *p, long long count) {
+        return p && kv_lens_out && kv_lens_out < p + count && p < kv_lens_out + n;
+    };
+    if (meets(kv_lens, n) || meets(accept_lens, n) || meets(accepted, n * max_accept) || meets(cu_rows, n + 1) || meets(page_table, n * max_pages) ||
+        (kept != kv_lens_out && meets(kept, n)))
+        return W4A8_ERR_SHAPE;
     const w4a8_status arch = check_arch();
     if (arch != W4A8_OK) return arch;
     const cudaError_t e = launch_kv_accept(c, bt, {accepted, accept_lens, kept, kv_lens_out, max_accept}, static_cast<StatusBlock *>(workspace),

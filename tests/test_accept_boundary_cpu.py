@@ -14,3 +14,18 @@ def test_refusals(w4a8):  # noqa: F811
     for kw in (dict(cache=P(GOOD + 8)), dict(kept=P(GOOD + 2)), dict(out=P(GOOD + 2)), dict(n=P(GOOD + 1)), dict(ws=P(GOOD + 128))):
         assert f(*ex_args(**kw)) == 3, kw
     assert f(*ex_args(wsb=255)) == 4
+
+
+def test_lengths_over_an_input(w4a8):  # noqa: F811
+    """kv_lens_out shares an element or more with something that the call reads."""
+    f, out = w4a8.lib.w4a8_kv_accept_ex, 0x80000
+    apart = dict(table=P(GOOD), lens=P(GOOD + 0x1000), cu=P(GOOD + 0x2000), acc=P(GOOD + 0x3000), n=P(GOOD + 0x4000), kept=P(GOOD + 0x5000), out=P(out))
+    sizes = dict(table=2 * 2, lens=2, cu=3, acc=2 * 3, n=2, kept=2)             # batch 2, 2 pages, 3 places
+    for k, size in sizes.items():
+        for shift in (1 - size, -1, 0, 1):
+            if k == "kept" and shift == 0:
+                continue
+            assert f(*ex_args(**{**apart, k: P(out + 4 * shift)})) == 2, (k, shift)
+    g = w4a8.lib.w4a8_kv_accept
+    for k in ("lens", "acc", "n", "cu", "table"):
+        assert g(*accept_args(**{**{x: v for x, v in apart.items() if x != "kept"}, k: P(out)})) == 2, k
