@@ -498,6 +498,8 @@ w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, con
  *   page_table  [batch][max_pages] INT32, in and out: with P = page_size, entries
  *               ceil(held / P) .. ceil((kv_lens + add) / P) - 1 are taken from the free list; where there are fewer pages
  *               than before, the surplus ones are given back (their entries stay as they are and count no longer).
+ *               Entries that are neither given back nor hold one of the step's rows are not read.  A row whose
+ *               entry below ceil(held / P) names no page gets slot -1 and is reported (W4A8_ERR_BAD_TABLE); all else is as planned.
  *   free_pages  [num_pages] INT32, in and out: a stack, its first *free_count numbers are the free pages.
  *               The pages given back lie on top of it in the order of sequences and pages, then pages are
  *               taken from the top in that order.
@@ -508,10 +510,13 @@ w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, con
  *   positions   out [rows] INT32, position of every row, or NULL.
  *   slots       out [rows] INT64, page * page_size + place of every row, or NULL.
  *   rows        size of positions and slots, at most 2^30; rows from cu_rows[batch] on get position 0 and slot -1.
- * A step whose rows do not fit, whose lengths are out of range or whose free list is damaged (W4A8_ERR_BAD_TABLE), or
- * that needs more pages than are free (W4A8_ERR_NO_PAGES), is refused as a whole: cu_rows are 0, slots -1, kv_lens_out is held,
+ * A step whose rows do not fit, whose lengths or count are out of range, that would take a number from the list or give one back that
+ * is no page (W4A8_ERR_BAD_TABLE), or that needs more pages than are free (W4A8_ERR_NO_PAGES), is refused as a whole: cu_rows are 0, slots -1, kv_lens_out is held,
  * free_count_out is free_count, the table and the list are left alone; the status block reports it.  (What the sequences keep is then
  * in kv_lens alone: held may count more.)
+ * Pages are given back from the end only.  A caller that takes pages out of the middle itself, as those between the sinks and the window
+ * of w4a8_kv_attention_sinks, puts them on the list itself, and when the sequence ends the others too: it
+ * then passes held = kv_lens = 0 for it.
  * batch <= 8192.  workspace: 512 bytes, zero-filled once; one that the cache calls use will do. */
 w4a8_status w4a8_kv_plan(const int32_t *held, const int32_t *kv_lens, const int32_t *add, int batch,
                          int32_t *page_table, int max_pages, int page_size, int32_t *free_pages,

@@ -5,11 +5,15 @@
 // is given back lies on top of it in the order of sequences and pages, and page number a of those taken is the a-th from the
 // top, which every thread finds by itself (on the list, or in the table of the sequence that gives it back).  The lengths and the
 // count may be updated in place: a CTA draws a ticket when it has read them, and the one that draws the last writes them.
+// A step is taken or refused as a whole, so every CTA looks at all numbers that change hands before it writes: to leave that to the CTA that moves
+// a number would mean to wait for one another, or to undo.
 //
 // Twelve bytes per row and a few per sequence: the time is a launch, the scan's chain of dependent steps, and for many rows
 // the search of each row's sequence, which four neighbouring rows share.  Eight requests of a token each 4.1 us; 1500 requests with
-// 252 thousand rows 10.1 us (3.2 MB, 0.5 us of memory; a search and scattered stores for every row took 17.7 us).
-// 8000 requests of a token each 14.9 us, the scan (45 us where the threads' entries met in one bank).
+// 252 thousand rows, 7900 pages taken and 4000 given back 14.1 us (3.2 MB, 0.5 us of memory; a search and scattered stores for every row took
+// 7.5 us more), 4 us of it for the look at the numbers that change hands: 0.5 those from the list, 3.5 those given back, each of which every CTA reads
+// from the same lines of L2 behind a search of its sequence (one by one, instead of eight side by side, 8 us).  8000 requests of a token each
+// 14.5 us, the scan (45 us where the threads' entries met in one bank).
 #include "kv_cache.cuh"
 
 namespace w4a8 {
@@ -17,6 +21,7 @@ namespace w4a8 {
 namespace {
 
 constexpr int kRun = 4;                      // neighbouring rows of a thread
+constexpr int kChecked = 8;                  // pages of a thread that are looked at together
 constexpr int kAtOnce = 4;                   // sequences of a thread whose lengths are loaded together
 
 struct Sums {
@@ -52,11 +57,10 @@ struct __align__(16) Entry {
     int row, kept, taken, had;               // first row, tokens, first page taken, pages before
 };
 
-// The last sequence whose number is <= x, where numbers ascend and the first is 0: the owner of element x.
+// The last sequence of lo .. hi whose number is <= x, where numbers ascend and lo's is <= x: the owner of element x.
 template <class F>
-__device__ __forceinline__ int owner(int batch, int x, F number)
+__device__ __forceinline__ int owner(int lo, int hi, int x, F number)
 {
-    int lo = 0, hi = batch - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (number(mid) <= x) lo = mid;
@@ -130,40 +134,77 @@ __global__ void __launch_bounds__(THREADS) kv_plan_kernel(const KvPlanArgs a, St
         bad = true;
         if (tid == 0) report_failure(sb, W4A8_ERR_NO_PAGES, -1);
     }
-    const int n_rows = bad ? 0 : (int)total.rows, n_taken = bad ? 0 : (int)total.taken, n_back = bad ? 0 : (int)total.back;
-    const int top = count + n_back;          // of the stack with what is given back
     for (int b = b0; b < b1; ++b) {
         entry[b].row += (int)before.rows;
         entry[b].taken += (int)before.taken;
         first_back[b] += (int)before.back;
-        if (blockIdx.x == 0) a.cu_rows[b] = bad ? 0 : entry[b].row;
     }
-    if (blockIdx.x == 0 && tid == 0) a.cu_rows[batch] = n_rows;
     __syncthreads();
+    // page that sequence b gives back as place f
+    auto back_page = [&](int b, int f) { return __ldca(a.page_table + (size_t)b * a.max_pages + pages_left[b] + f - first_back[b]); };
+    // Every CTA looks at all pages that change hands before it writes anything.  (What it looks at is written by none: table entries in
+    // front of `had`, the list below `count`.)
+    const int n_popped = bad ? 0 : (int)max(total.taken - total.back, 0ll);      // from the list itself
+    if (!bad && (n_popped > 0 || total.back > 0)) {
+        int lost = 0;                        // a page number that is none: 1 + its sequence, or -1 (the list)
+        int page[kChecked];                  // their loads in flight together
+        for (uint32_t k0 = tid; k0 < (uint32_t)n_popped; k0 += kChecked * THREADS) {
+#pragma unroll
+            for (int k = 0; k < kChecked; ++k) page[k] = k0 + k * THREADS < (uint32_t)n_popped ? __ldca(a.free_pages + count - 1 - (k0 + k * THREADS)) : 0;
+#pragma unroll
+            for (int k = 0; k < kChecked; ++k)
+                if ((unsigned)page[k] >= (unsigned)a.num_pages) lost = -1;
+        }
+        // A warp takes a part of those given back, its lanes neighbours; they belong to sequences lo .. hi.
+        const int all = (int)total.back;
+        const long long part = ((all + WARPS - 1) / WARPS + 31) / 32 * 32;
+        const int f0 = (int)min((long long)all, warp * part), f1 = (int)min((long long)all, f0 + part);
+        if (f0 < f1) {
+            const int end = owner(0, batch - 1, lane & 1 ? f1 - 1 : f0, [&](int i) { return first_back[i]; });
+            const int lo = __shfl_sync(0xffffffffu, end, 0), hi = __shfl_sync(0xffffffffu, end, 1);
+            const int step0 = hi > lo ? 1 << (31 - __clz(hi - lo)) : 0;
+            for (int f = f0 + lane; f < f1; f += kChecked * 32) {
+                int b[kChecked];
+#pragma unroll
+                for (int k = 0; k < kChecked; ++k) b[k] = lo;
+                for (int step = step0; step > 0; step >>= 1) {             // (side by side)
+#pragma unroll
+                    for (int k = 0; k < kChecked; ++k)
+                        if (b[k] + step <= hi && first_back[b[k] + step] <= f + 32 * k) b[k] += step;
+                }
+#pragma unroll
+                for (int k = 0; k < kChecked; ++k) page[k] = f + 32 * k < f1 ? back_page(b[k], f + 32 * k) : 0;
+#pragma unroll
+                for (int k = 0; k < kChecked; ++k)
+                    if ((unsigned)page[k] >= (unsigned)a.num_pages) lost = b[k] + 1;
+            }
+        }
+        if (lost) report_failure(sb, W4A8_ERR_BAD_TABLE, lost > 0 ? lost - 1 : -2);
+        bad = __syncthreads_or(lost);
+    }
+    const int n_rows = bad ? 0 : (int)total.rows, n_taken = bad ? 0 : (int)total.taken, n_back = bad ? 0 : (int)total.back;
+    const int top = count + n_back;          // of the stack with what is given back
+    if (blockIdx.x == 0) {
+        for (int b = tid; b < batch; b += THREADS) a.cu_rows[b] = bad ? 0 : entry[b].row;
+        if (tid == 0) a.cu_rows[batch] = n_rows;
+    }
     // page of place f among those given back, and of place k from the top of the stack
-    auto given_back = [&](int f) {
-        const int b = owner(batch, f, [&](int i) { return first_back[i]; });
-        const int page = __ldca(a.page_table + (size_t)b * a.max_pages + pages_left[b] + f - first_back[b]);
-        if ((unsigned)page >= (unsigned)a.num_pages) report_failure(sb, W4A8_ERR_BAD_TABLE, b);
-        return page;
-    };
+    auto given_back = [&](int f) { return back_page(owner(0, batch - 1, f, [&](int i) { return first_back[i]; }), f); };
     auto taken = [&](int k) {
         const int v = top - 1 - k;
-        const int page = v < count ? __ldca(a.free_pages + v) : given_back(v - count);
-        if ((unsigned)page >= (unsigned)a.num_pages) report_failure(sb, W4A8_ERR_BAD_TABLE, -2);
-        return page;
+        return v < count ? __ldca(a.free_pages + v) : given_back(v - count);
     };
     const int thread = blockIdx.x * THREADS + tid, threads = gridDim.x * THREADS;
     // (pages from the last thread on, rows from the first)
     for (int k = threads - 1 - thread; k < n_taken; k += threads) {
-        const int b = owner(batch, k, [&](int i) { return entry[i].taken; });
+        const int b = owner(0, batch - 1, k, [&](int i) { return entry[i].taken; });
         a.page_table[(size_t)b * a.max_pages + entry[b].had + k - entry[b].taken] = taken(k);
     }
     for (int f = threads - 1 - thread; f < n_back - n_taken; f += threads) a.free_pages[count + f] = given_back(f);
     for (int r0 = thread * kRun; r0 < a.rows && (a.positions || a.slots); r0 += threads * kRun) {
         int pos[kRun];
         long long slot[kRun];
-        int b = r0 < n_rows ? owner(batch, r0, [&](int i) { return entry[i].row; }) : batch;
+        int b = r0 < n_rows ? owner(0, batch - 1, r0, [&](int i) { return entry[i].row; }) : batch;
         int at = -1, page = 0;               // the page looked up last
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
@@ -180,7 +221,7 @@ __global__ void __launch_bounds__(THREADS) kv_plan_kernel(const KvPlanArgs a, St
             if (i != at) {
                 at = i;
                 page = i < e.had ? __ldca(a.page_table + (size_t)b * a.max_pages + i) : taken(e.taken + i - e.had);
-                if ((unsigned)page >= (unsigned)a.num_pages) report_failure(sb, W4A8_ERR_BAD_TABLE, b);
+                if ((unsigned)page >= (unsigned)a.num_pages) report_failure(sb, W4A8_ERR_BAD_TABLE, b);      // the table lost it
             }
             if ((unsigned)page < (unsigned)a.num_pages) slot[k] = ((long long)page << a.page_shift) + (pos[k] & ((1 << a.page_shift) - 1));
         }
