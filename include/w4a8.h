@@ -553,7 +553,9 @@ w4a8_status w4a8_rope_kv_append(const void *Q, const void *K, const void *V, int
 
 /* w4a8_kv_attention with a window and first tokens that stay visible: a row at position p sees the keys j (j <= p if
  * causal) with j > p - window or j < sinks.  window 0: no limit.  Pages without a token that a row sees, those between
- * the sinks and the oldest row's window among them, are not read, and their table entries neither. */
+ * the sinks and the oldest row's window among them, are not read, and their table entries neither.
+ * Positions are those of the sequence: keys are cached as they were turned, the sinks' with their own positions far behind the window
+ * (not counted anew inside the cache, for which stored keys would have to be turned again). */
 w4a8_status w4a8_kv_attention_sinks(const void *Q, int q_type, long long q_stride, const void *cache,
                                     int num_pages, int page_size, int kv_heads, int head_dim,
                                     const int32_t *page_table, int max_pages, const int32_t *kv_lens,
@@ -565,7 +567,9 @@ w4a8_status w4a8_kv_attention_sinks(const void *Q, int q_type, long long q_strid
  * sequence b, whose rows begin at position base = kv_lens[b] - n_b, sees
  *   - the tokens in front of base, all of them or, with a window, those j with j > p - window or j < sinks, where
  *     p = base + (bits of its mask, at least 1) - 1 (its mask names its ancestors and itself);
- *   - the drafted rows j (at position base + j) of its mask: bit j % 32 of tree_mask[row][j / 32].
+ *   - the drafted rows j (at position base + j) of its mask: bit j % 32 of tree_mask[row][j / 32].  The window does not govern
+ *     these: a row whose path is longer than the window sees all of it, where the tokens one by one would see
+ *     the last `window` of it (for that, set these bits only: no token in front of base is then in the window either).
  * Bits of rows that the sequence does not have are ignored; any mask is allowed, an empty one too.
  *   tree_mask   [rows][mask_words] UINT32; a sequence may have up to 32 * mask_words rows (more are reported as
  *               W4A8_ERR_BAD_TABLE, and the rows behind are seen by none).

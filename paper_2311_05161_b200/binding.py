@@ -593,14 +593,16 @@ def rope_kv_append(Q, K, V, positions, inv_freq, cache, slots, workspace, pair_a
 
 def kv_attention_sinks(Q, cache, page_table, kv_lens, kv_heads: int, workspace, window: int, sinks: int, cu_rows=None, scale=None,
                        causal: bool = True, dtype=torch.float16, out=None, lse=None):
-    """kv_attention with a window of `window` tokens (0: no limit) and the first `sinks` tokens visible beside it."""
+    """kv_attention with a window of `window` tokens (0: no limit) and the first `sinks` tokens visible beside it, at the positions that
+    they were cached with."""
     return _calls.kv_attention_sinks(Q, cache, page_table, kv_lens, kv_heads, workspace, window, sinks, cu_rows, scale, causal, dtype, out, lse)
 
 
 def kv_attention_tree(Q, cache, page_table, kv_lens, kv_heads: int, workspace, tree_mask, cu_rows=None, scale=None, window: int = 0,
                       sinks: int = 0, dtype=torch.float16, out=None, lse=None):
     """Attention of drafted rows: a row sees the tokens in front of its sequence's rows (with a window and sinks, if given) and
-    those of the sequence's rows whose bits are set in its mask, tree_mask [rows, words] int32 (bit j % 32 of word j / 32)."""
+    those of the sequence's rows whose bits are set in its mask, tree_mask [rows, words] int32 (bit j % 32 of word j / 32), these
+    whatever the window."""
     return _calls.kv_attention_tree(Q, cache, page_table, kv_lens, kv_heads, workspace, tree_mask, cu_rows, scale, window, sinks, dtype, out, lse)
 
 

@@ -39,7 +39,8 @@
 // then those of the window, and make a unit that some row does not see whole a mask of 32 bits per row: the others
 // cost what they cost without it, but for a few registers.  64 sequences, window 2047 and 5 sinks, 8 query heads per key head, 139 MB:
 // 52.5 us (52.0 without the sinks in the plain form); 12 trees of 3 to 13 nodes, 32 heads of their own, 97 MB: 55.0 us (causal rows in
-// the plain form the same); one sequence of 100001 tokens, window 4096: 11.8 us; a tree of 7 nodes at 2049 tokens: 11.5 us.
+// the plain form the same); one sequence of 100001 tokens, window 4096: 11.8 us; a tree of 7 nodes at 2049 tokens: 11.5 us with a table of
+// 33 pages, 14.1 us with a wider one (Variant).
 // (One form for sinks and trees together: 53.4 and 56.4 us.)
 #include "kv_attention.cuh"
 
@@ -766,7 +767,7 @@ Variant pick(const KvAttnArgs &a, int sms)
     const long long rows = (long long)group * ((a.batch.rows + a.batch.batch - 1) / a.batch.batch);
     Variant v;
     v.nt = rows > 8 ? 2 : 1;
-    // Where even the longest sequences that the tables (or the window) allow leave the list of eight-row tiles no longer than one
+    // Where even the longest sequences that the tables (or the window) allow (the host knows no other bound) leave the list of eight-row tiles no longer than one
     // place per warp, the time is one item's chain of steps, and a chain of eight rows is shorter.  8 key heads of 128, four query heads
     // to a key head, eight rows / sixteen, us: a tree of 7 nodes at 2049 tokens 11.5 / 14.1; 8 of 3 nodes at 300 tokens 11.3 / 13.2;
     // at twice as many places 4 trees of 3 at 2049 16.9 / 15.8; with a window of 500 of 1000 tokens, 4 of 3 rows 11.3 / 12.9, 8 of 3 rows
