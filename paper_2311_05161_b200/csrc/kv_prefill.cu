@@ -51,9 +51,11 @@ constexpr int kWarps = 20, kThreads = 32 * kWarps;         // the last one only 
 constexpr int kRing = 4;                                   // units of expanded keys, and of values
 constexpr int kConstSlots = 8;                             // more than kRing: a slot is rewritten after its unit's softmax
 constexpr int kLead = 6;                                   // an item's fixed cost, in units
-// What a CTA loses where its share is parts of two items instead of one item, in units.  (A chunk of 1024 rows, window 4096, 128 items of 67
-// units on 148 CTAs: one by one 122.0 us, in even shares 124.9 us.)
-constexpr int kTwoParts = 10;
+// What a CTA loses where its share is parts of two items instead of one item, in units: a second piece and the join; and where it is a part
+// of one, as with fewer items than half the CTAs: the join alone.  In us, 4 sinks, items of head dimension 128 one by one / in even shares: 128
+// items of 73 places (units and lead, window 4096) 122.0 / 124.9, of 9 to 48 places 21.7 / 28.7 to 79.3 / 85.0; 64 items of 10 places 22.9 / 23.5, of 12
+// 25.4 / 26.0, of 16 29.8 / 29.6; 48 of 12 25.1 / 24.4, of 15 29.0 / 26.2; 2 to 32 items of 9 places 20.3 / 21.8, of 10 22.1 / 23.5, of 12 24.3 / 21.7.
+constexpr int kTwoParts = 10, kOnePart = 6;
 constexpr int kWaitSite = 950;
 constexpr int kApart = 16;                                 // a row at most 2^16 below its tile's largest is good to 2^-23 of its own largest element
 
@@ -474,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             n_items += ctl->warp_items[w];
             longest = max(longest, ctl->warp_longest[w]);
         }
-        if (n_items <= (int)gridDim.x && longest <= per + kTwoParts) {
+        if (n_items <= (int)gridDim.x && longest <= per + (2 * n_items > (int)gridDim.x ? kTwoParts : kOnePart)) {
             by_items = true;
             per = 1;
             total = n_items;
