@@ -437,7 +437,8 @@ w4a8_status w4a8_attn_pv(const int8_t *Pq, const float *p_scale, const void *pac
 size_t w4a8_kv_page_bytes(int page_size, int kv_heads, int head_dim);
 
 /* Quantizes the rows' keys and values into their slots.  K, V: [rows][kv_heads][D] W4A8_F16 or
- * W4A8_BF16. */
+ * W4A8_BF16.  An element that is NaN is stored as some level, the others of its vector as without it; a vector with
+ * an infinity is stored as anything, other vectors are not touched by it. */
 w4a8_status w4a8_kv_append(const void *K, const void *V, int dtype, long long k_stride,
                            long long v_stride, void *cache, int num_pages, int page_size,
                            int kv_heads, int head_dim, const int32_t *page_table, int max_pages,
@@ -513,7 +514,9 @@ w4a8_status w4a8_kv_attention(const void *Q, int q_type, long long q_stride, con
  * A step whose rows do not fit, whose lengths or count are out of range, that would take a number from the list or give one back that
  * is no page (W4A8_ERR_BAD_TABLE), or that needs more pages than are free (W4A8_ERR_NO_PAGES), is refused as a whole: cu_rows are 0, slots -1, kv_lens_out is held,
  * free_count_out is free_count, the table and the list are left alone; the status block reports it.  (What the sequences keep is then
- * in kv_lens alone: held may count more.)
+ * in kv_lens alone: held may count more.)  Calls that go by cu_rows or slots then do nothing; one without cu_rows takes a row of every
+ * sequence all the same, an append the place of its last token: behind a plan that may be refused, pass cu_rows.
+ * No output may overlap an input or another output but where it says so.
  * Pages are given back from the end only.  A caller that takes pages out of the middle itself, as those between the sinks and the window
  * of w4a8_kv_attention_sinks, puts them on the list itself, and when the sequence ends the others too: it
  * then passes held = kv_lens = 0 for it.

@@ -79,3 +79,27 @@ def test_kept_lengths_of_sequences_without_rows():
         call([2, 0, 2], kept=kept.long())
     with pytest.raises(ValueError):
         call([2, 0, 2], kept=kept[:2])
+
+
+@pytest.mark.parametrize("nodes", [4, 40])
+def test_calls_behind_a_refused_plan_do_nothing(nodes):
+    """With its row offsets: nothing is cached, read back, attended to or moved."""
+    e = Engine(2, 16, 2, 4, 64, 12, 10, 2 * nodes)
+    e.add.copy_(i32([nodes, 3]))
+    e.plan()
+    w4a8.check_status(e.ws)
+    e.cache.random_(0, 200)
+    before, held = e.cache.clone(), e.held.tolist()
+    e.add.copy_(i32([150, 3]))
+    e.plan()
+    assert w4a8.poll_status(e.ws) == 9 and e.cu.tolist() == [0, 0, 0] and e.held.tolist() == held
+    K, V, Q = (vectors((e.rows, h, 64), k, F16).cuda() for k, h in enumerate((2, 2, 4)))
+    outs = [torch.full_like(Q, 9.0) for _ in range(4)]
+    w4a8.kv_append(K, V, e.cache, e.table, e.held, e.ws, cu_rows=e.cu)
+    w4a8.rope_kv_append(Q, K, V, e.positions, e.freq, e.cache, e.slots, e.ws, out=outs[0])
+    w4a8.kv_attention(Q, e.cache, e.table, e.held, 2, e.ws, cu_rows=e.cu, out=outs[1])
+    w4a8.kv_attention_sinks(Q, e.cache, e.table, e.held, 2, e.ws, 9, 2, cu_rows=e.cu, out=outs[2])
+    w4a8.kv_attention_tree(Q, e.cache, e.table, e.held, 2, e.ws, torch.full((e.rows, 2), -1, dtype=torch.int32, device="cuda"), cu_rows=e.cu, out=outs[3])
+    w4a8.kv_accept(e.cache, e.table, e.held, i32([[1, 2], [1, 2]]), i32([0, 0]), 2, 64, e.ws, cu_rows=e.cu)
+    w4a8.check_status(e.ws)
+    assert torch.equal(e.cache, before) and all(bool((o == 9.0).all()) for o in outs)
